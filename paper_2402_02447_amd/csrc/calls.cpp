@@ -8,6 +8,8 @@
 
 #include "bca.h"
 
+PyMethodDef* lmt_methods();  // of the calls of lmt.h (lmt_calls.cpp)
+
 namespace {
 
 struct Functions {
@@ -309,5 +311,8 @@ PyMODINIT_FUNC PyInit__calls(void) {
   if (!bases) return nullptr;
   e_argument = PyErr_NewException("paper_2402_02447_amd._calls.ArgumentError", bases, nullptr);
   Py_DECREF(bases);
-  return e_argument ? PyModule_Create(&module) : nullptr;
+  PyMethodDef* lmt = e_argument ? lmt_methods() : nullptr;
+  PyObject* m = lmt ? PyModule_Create(&module) : nullptr;
+  if (m && PyModule_AddFunctions(m, lmt) != 0) Py_CLEAR(m);
+  return m;
 }

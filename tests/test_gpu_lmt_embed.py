@@ -1,0 +1,243 @@
+"""Embedding lookup and the gradient of its table against their formulas in 64 bits (GPU)."""
+import numpy as np
+import pytest
+import torch
+
+import lmt_reference as R
+from lmt_gpu import DT, Mat, typed, within
+from paper_2402_02447_amd import lmt
+
+pytestmark = pytest.mark.gpu
+
+
+def ids(tokens, kind, offset=0):
+    n = len(tokens)
+    buf = torch.zeros(n + offset + 1, dtype=DT[kind], device="cuda")
+    buf[offset:offset + n] = torch.as_tensor(np.asarray(tokens, np.int64)).to(DT[kind])
+    return buf[offset:offset + n]
+
+
+def zipf(rng, n, vocab, mask=0.15, pad=0.2):
+    t = np.minimum(vocab - 1, np.exp(rng.random(n) * np.log(vocab + 1)).astype(np.int64) - 1)
+    t = rng.permutation(vocab)[t]
+    u = rng.random(n)
+    t[u < mask] = vocab // 2
+    t[u > 1 - pad] = 0
+    return t
+
+
+def check_embed(tokens, vocab, width, dtype, out, id_kind, scale=1.0, gaps=(0, 0), offsets=(0, 0, 0), seed=0):
+    rng = np.random.default_rng(seed)
+    table = typed(rng.normal(0, 0.02, (vocab, width)), dtype)
+    t = Mat(vocab, width, dtype, gaps[0], offsets[0], table)
+    o = Mat(len(tokens), width, out, gaps[1], offsets[1])
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    lmt.embed(t.view, ids(tokens, id_kind, offsets[2]), o.view, scale, status)
+    torch.cuda.synchronize()
+    want = R.embed(table, np.asarray(tokens), scale)
+    within(o.numpy(), want, R.rounded(want, "f32") + R.rounded(want, out) * (1 + 2 * R.U32))
+    assert o.untouched_outside() and t.untouched_outside()
+    bad = any(not 0 <= v < vocab for v in tokens)
+    assert int(status.item()) == (lmt.LMT_STATUS_BAD_TOKEN if bad else 0)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("out", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("id_kind", ["i32", "i64"])
+def test_lookup_types(dtype, out, id_kind):
+    rng = np.random.default_rng(3)
+    check_embed(rng.integers(0, 50, 77), 50, 100, dtype, out, id_kind, 10.0)
+
+
+@pytest.mark.parametrize("n,vocab,width", [(1, 1, 1), (1, 300, 1024), (5, 3, 7), (64, 2, 8), (37, 100, 9), (65, 20, 257), (3, 5, 4099), (513, 11, 63), (2, 2, 511), (2, 2, 513)])
+def test_lookup_sizes_strides_and_starts(n, vocab, width):
+    rng = np.random.default_rng(n * 1000 + width)
+    tokens = rng.integers(0, vocab, n)
+    check_embed(tokens, vocab, width, "bf16", "bf16", "i64", 2.0, (5, 3), (1, 3, 1))
+    check_embed(tokens, vocab, width, "f32", "f16", "i32", 0.1, (1, 0), (3, 1, 1))
+    check_embed(tokens, vocab, width, "f32", "f32", "i64", 1.0, (0, 7), (0, 1, 0))
+
+
+def test_lookup_of_tokens_that_are_none():
+    check_embed([0, -1, 4, 5, 2 ** 31 - 1, -2 ** 31, 3], 5, 33, "bf16", "f32", "i32")
+    check_embed([0, -1, 4, 5, 2 ** 32, 2 ** 40 + 1, 2 ** 63 - 1, -2 ** 63, 3], 5, 33, "f32", "bf16", "i64")
+
+
+def test_lookup_passes_infinities_and_nan_on():
+    table = np.array([[np.inf, -np.inf, np.nan, 1.0], [0.0, -0.0, 65504.0, 1e-7]])
+    o = torch.empty(2, 4, dtype=torch.bfloat16, device="cuda")
+    lmt.embed(torch.tensor(table, dtype=torch.float32, device="cuda"), ids([0, 1], "i64"), o, -1.0)
+    want = (torch.tensor(table, dtype=torch.float32) * -1).bfloat16()
+    assert np.array_equal(o.float().cpu().numpy(), want.float().numpy(), equal_nan=True)
+
+
+def test_lookup_in_a_table_beyond_32_bit_offsets():
+    vocab, ld, width = 40000, 131072, 65          # 5.2e9 elements between the first and the last row
+    table = torch.empty(vocab * ld, dtype=torch.bfloat16, device="cuda").view(vocab, ld)[:, :width]
+    tokens = [0, 16384, 32767, 32768, 39999]
+    rows = torch.randn(5, width, device="cuda").bfloat16()
+    for i, t in enumerate(tokens):
+        table[t] = rows[i]
+    out = torch.empty(5, width, dtype=torch.bfloat16, device="cuda")
+    lmt.embed(table, ids(tokens, "i32"), out)
+    assert torch.equal(out, rows)
+    # and the gradient of such a table, row by row of a padded matrix
+    table.zero_()
+    ws = torch.empty(lmt.embed_grad_workspace(5, vocab, width), dtype=torch.uint8, device="cuda")
+    lmt.embed_grad(rows, ids(tokens, "i32"), table, ws, accumulate=True)
+    for i, t in enumerate(tokens):
+        assert torch.equal(table[t], rows[i])
+
+
+def check_grad(tokens, vocab, width, dtype, grad, id_kind="i64", scale=1.0, skip=-1, accumulate=False, gaps=(0, 0), offsets=(0, 0, 0), sigma=1.0, seed=0, stream=None):
+    rng = np.random.default_rng(seed)
+    n = len(tokens)
+    g = typed(rng.normal(0, sigma, (n, width)), dtype)
+    old = typed(rng.normal(0, sigma, (vocab, width)), grad)
+    gm, tm = Mat(n, width, dtype, gaps[0], offsets[0], g), Mat(vocab, width, grad, gaps[1], offsets[1], old)
+    ws = torch.full((max(16, lmt.embed_grad_workspace(n, vocab, width)) + 16,), 0xC3, dtype=torch.uint8, device="cuda")
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    used = ws[:lmt.embed_grad_workspace(n, vocab, width)]
+    tk = ids(tokens, id_kind, offsets[2])
+    torch.cuda.synchronize()
+    lmt.embed_grad(gm.view, tk, tm.view, used, scale, skip, accumulate, status, stream)
+    torch.cuda.synchronize()
+    want, bound = R.embed_grad(g, np.asarray(tokens), vocab, scale, skip, old if accumulate else None)
+    within(tm.numpy(), want, bound + R.rounded(want, grad) * 2)
+    assert tm.untouched_outside() and gm.untouched_outside() and bool((ws[len(used):] == 0xC3).all())
+    if accumulate:                                                 # rows that do not occur keep their bits
+        absent = np.setdiff1d(np.arange(vocab), [t for t in tokens if t != skip])
+        assert np.array_equal(tm.numpy()[absent], old[absent])
+    assert int(status.item()) == (lmt.LMT_STATUS_BAD_TOKEN if any(not 0 <= v < vocab and v != skip for v in tokens) else 0)
+    return tm.view
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("grad", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("accumulate", [False, True])
+def test_gradient_types(dtype, grad, accumulate):
+    rng = np.random.default_rng(4)
+    check_grad(zipf(rng, 300, 90), 90, 100, dtype, grad, "i32", 4.0, 0, accumulate)
+
+
+@pytest.mark.parametrize("n,vocab,width", [(1, 1, 1), (1, 1000, 33), (2, 1, 300), (15, 3, 8), (16, 16, 9), (17, 2, 64), (100, 5000, 12), (255, 7, 257), (1000, 40, 515),
+                                           (4095, 300, 20), (4096, 300, 20), (4097, 300, 20), (8193, 2000, 5), (16384, 1500, 6), (16385, 1500, 6), (20000, 70000, 4)])
+def test_gradient_sizes_strides_and_starts(n, vocab, width):
+    rng = np.random.default_rng(n)
+    tokens = zipf(rng, n, vocab)
+    check_grad(tokens, vocab, width, "bf16", "f32", "i64", 0.5, 0, False, (3, 5), (1, 1, 1), seed=n)
+    check_grad(tokens, vocab, width, "f32", "bf16", "i32", 1.0, -1, True, (1, 3), (1, 3, 1), seed=n)
+
+
+@pytest.mark.parametrize("n", [40, 5000, 20000])
+@pytest.mark.parametrize("accumulate", [False, True])
+def test_gradient_of_one_token_everywhere_of_all_different_ones_and_of_none(n, accumulate):
+    vocab = 20001
+    for tokens in (np.full(n, 7), np.full(n, vocab - 1), np.arange(n), np.arange(n)[::-1].copy(), np.full(n, 0), np.arange(n) % 2 * (vocab - 1)):
+        check_grad(tokens, vocab, 9, "f32", "f32", "i64", 1.0, 0, accumulate, seed=n)
+
+
+def test_gradient_leaves_out_tokens_that_are_none():
+    check_grad([3, -1, 3, 5, 2 ** 31 - 1, -2 ** 31, 0, 4], 5, 17, "f32", "f32", "i32")
+    check_grad([3, -1, 3, 5, 2 ** 32 + 3, 2 ** 63 - 1, -2 ** 63, 0, 4], 5, 17, "bf16", "f32", "i64", accumulate=True)
+    check_grad([3, -1, 3, -1, 0, 4], 5, 17, "f32", "f32", "i64", skip=-1)           # the padding is outside the vocabulary: nothing to report
+    check_grad([9, 9, 9], 9, 17, "f32", "f32", "i64")
+
+
+@pytest.mark.parametrize("vocab", [1, 2, 1023, 1024, 1025, 2 ** 20 - 1, 2 ** 20, 2 ** 20 + 1, 3_000_000])
+def test_gradient_vocabularies_around_the_sort_digits(vocab):
+    rng = np.random.default_rng(vocab)
+    n = 5000
+    tokens = np.concatenate([rng.integers(0, vocab, n - 4), [0, vocab - 1, vocab // 2, vocab - 1]])
+    g = typed(rng.normal(0, 1, (n, 3)), "f32")
+    grad = torch.full((vocab, 3), 5.0, device="cuda")
+    ws = torch.empty(lmt.embed_grad_workspace(n, vocab, 3), dtype=torch.uint8, device="cuda")
+    lmt.embed_grad(torch.tensor(g, dtype=torch.float32, device="cuda"), ids(tokens, "i32"), grad, ws)
+    got = grad.double().cpu().numpy()
+    want, size = np.zeros((vocab, 3)), np.zeros((vocab, 3))
+    np.add.at(want, tokens, g)
+    np.add.at(size, tokens, np.abs(g))
+    within(got, want, size * R.U32 * (np.bincount(tokens, minlength=vocab)[:, None] + 2))
+
+
+def test_gradient_without_tokens_is_zero_and_with_accumulation_nothing():
+    for kind in ("f32", "f16", "bf16"):
+        m = Mat(300, 21, kind, 3, 1, np.ones((300, 21)))
+        none, ws = torch.empty(0, 21, device="cuda"), torch.empty(0, dtype=torch.uint8, device="cuda")
+        lmt.embed_grad(none, ids([], "i64"), m.view, ws, accumulate=True)
+        assert (m.numpy() == 1).all()
+        lmt.embed_grad(none, ids([], "i64"), m.view, ws)
+        assert (m.numpy() == 0).all() and m.untouched_outside()
+
+
+def test_gradient_keeps_infinities_and_nan_in_their_rows():
+    g = torch.zeros(64, 40, device="cuda")
+    g[5, 3], g[9, 4], g[9, 5], g[11, 5] = float("nan"), float("inf"), float("inf"), float("-inf")
+    tokens = np.arange(64) % 4                                     # 5 and 9 with token 1, 11 with token 3
+    grad = torch.empty(5, 40, device="cuda")
+    ws = torch.empty(lmt.embed_grad_workspace(64, 5, 40), dtype=torch.uint8, device="cuda")
+    lmt.embed_grad(g, ids(tokens, "i64"), grad, ws)
+    got = grad.cpu().numpy()
+    assert np.isnan(got[1, 3]) and np.isposinf(got[1, 4]) and np.isposinf(got[1, 5]) and np.isneginf(got[3, 5])
+    got[1, 3:6] = got[3, 5] = 0
+    assert not got.any()
+
+
+def test_gradient_is_the_same_bits_every_time_and_on_any_stream():
+    rng = np.random.default_rng(8)
+    for n, width in ((3000, 70), (40000, 130)):
+        tokens = ids(zipf(rng, n, 1000), "i32")
+        g = torch.randn(n, width, device="cuda").bfloat16()
+        ws = torch.empty(lmt.embed_grad_workspace(n, 1000, width), dtype=torch.uint8, device="cuda")
+        first = torch.empty(1000, width, device="cuda")
+        lmt.embed_grad(g, tokens, first, ws, skip_token=0)
+        torch.cuda.synchronize()
+        side = torch.cuda.Stream()
+        for stream in (None, side, side):
+            again = torch.full((1000, width), 3.0, device="cuda")
+            ws.fill_(0xEE)
+            torch.cuda.synchronize()
+            lmt.embed_grad(g, tokens, again, ws, skip_token=0, stream=stream)
+            torch.cuda.synchronize()
+            assert torch.equal(first, again)
+
+
+def test_gradient_against_differences():
+    """sum of g * embed(table) is linear in the table: along a random direction d its derivative is sum of d * embed_grad(g)."""
+    rng = np.random.default_rng(9)
+    n, vocab, width = 500, 60, 48
+    tokens = ids(zipf(rng, n, vocab), "i64")
+    # multiples of 2^-6 below 8: all products and sums of the differences are exact in 64 bits
+    table, d, g = (torch.tensor(np.round(rng.normal(0, 1, s) * 64).clip(-511, 511) / 64, dtype=torch.float32, device="cuda") for s in ((vocab, width), (vocab, width), (n, width)))
+    out = [torch.empty(n, width, device="cuda") for _ in range(2)]
+    lmt.embed(table + d, tokens, out[0], 2.0)
+    lmt.embed(table - d, tokens, out[1], 2.0)
+    want = float(((out[0].double() - out[1].double()) * g.double()).sum()) / 2
+    grad = torch.empty(vocab, width, device="cuda")
+    lmt.embed_grad(g, tokens, grad, torch.empty(lmt.embed_grad_workspace(n, vocab, width), dtype=torch.uint8, device="cuda"), 2.0)
+    assert float((grad.double() * d.double()).sum()) == want
+
+
+@pytest.mark.parametrize("n", [700, 20000])
+def test_lookup_and_gradient_in_a_replayed_graph(n):
+    rng = np.random.default_rng(10)
+    vocab, width = 400, 96
+    tokens, table = ids(zipf(rng, n, vocab), "i32"), torch.randn(vocab, width, device="cuda")
+    out, grad = torch.empty(n, width, dtype=torch.bfloat16, device="cuda"), torch.empty(vocab, width, device="cuda")
+    ws = torch.empty(lmt.embed_grad_workspace(n, vocab, width), dtype=torch.uint8, device="cuda")
+    s, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=s):
+        lmt.embed(table, tokens, out, 3.0, stream=s)
+        lmt.embed_grad(out, tokens, grad, ws, 0.5, 0, stream=s)
+    for k in range(3):
+        tokens.copy_(ids(zipf(rng, n, vocab), "i32"))
+        table.normal_()
+        eager = torch.empty_like(out), torch.empty_like(grad)
+        lmt.embed(table, tokens, eager[0], 3.0)
+        lmt.embed_grad(eager[0], tokens, eager[1], torch.empty_like(ws), 0.5, 0)
+        grad.fill_(9.0)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, eager[0]) and torch.equal(grad, eager[1])
