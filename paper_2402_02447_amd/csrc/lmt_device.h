@@ -59,6 +59,13 @@ struct Vec {
     }
   }
 };
+// One element, for rows that are shorter than a vector.
+template <typename T>
+struct Vec<T, 1> {
+  T x;
+  __device__ __forceinline__ float get(int) const { return to_f32(x); }
+  __device__ __forceinline__ void set(const float (&f)[1]) { x = from_f32<T>(f[0]); }
+};
 template <int SIZE>
 struct At;  // words aligned to elements of SIZE bytes
 template <>
@@ -74,7 +81,7 @@ struct At<4> {
   typedef uint32_t x1;
 };
 template <bool NT, typename T, int N>
-__device__ __forceinline__ void load(Vec<T, N>& v, const T* p) {
+__device__ __forceinline__ void load_words(Vec<T, N>& v, const T* p) {
   constexpr int W = Vec<T, N>::kWords;
   static_assert(W == 1 || W == 2 || W % 4 == 0, "4, 8 or a multiple of 16 bytes");
   if constexpr (W == 1) {
@@ -99,7 +106,7 @@ __device__ __forceinline__ void load(Vec<T, N>& v, const T* p) {
   }
 }
 template <bool NT, typename T, int N>
-__device__ __forceinline__ void store(T* p, const Vec<T, N>& v) {
+__device__ __forceinline__ void store_words(T* p, const Vec<T, N>& v) {
   constexpr int W = Vec<T, N>::kWords;
   if constexpr (W == 1) {
     LMT_GLOBAL auto* g = (LMT_GLOBAL typename At<sizeof(T)>::x1*)p;
@@ -118,6 +125,22 @@ __device__ __forceinline__ void store(T* p, const Vec<T, N>& v) {
       if constexpr (NT) __builtin_nontemporal_store(x, g + i);
       else g[i] = x;
     }
+  }
+}
+template <bool NT, typename T, int N>
+__device__ __forceinline__ void load(Vec<T, N>& v, const T* p) {
+  if constexpr (N == 1) {
+    v.x = *(const LMT_GLOBAL T*)p;
+  } else {
+    load_words<NT>(v, p);
+  }
+}
+template <bool NT, typename T, int N>
+__device__ __forceinline__ void store(T* p, const Vec<T, N>& v) {
+  if constexpr (N == 1) {
+    *(LMT_GLOBAL T*)p = v.x;
+  } else {
+    store_words<NT>(p, v);
   }
 }
 template <typename T>

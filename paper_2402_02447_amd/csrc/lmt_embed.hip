@@ -5,10 +5,11 @@
 // short rows.
 //
 // Gradient: grad[v] = scale * sum of grad_out[t] over the t with token[t] = v.  The positions t are sorted by token (stable
-// radix sort, ten bits at a time at most), the sorted list is cut into chunks of equal length, and a wavefront sums the
-// rows of one chunk in list order, row after row in registers: rows whose tokens lie in one chunk are finished there; a
-// row that goes over a chunk's end is filed as partial sums (one in front, one behind per chunk) and joined in chunk order by a
-// last kernel.  Nothing is added atomically: the order of every sum depends on the sizes and the tokens alone.
+// radix sort, ten bits at a time at most; up to 16 384 tokens by one workgroup in LDS, while the others clear the table), the sorted
+// list is cut into chunks of equal length, and a wavefront sums the rows of one chunk in list order, row after row in
+// registers: rows whose tokens lie in one chunk are finished there; a row that goes over a chunk's end is filed as partial
+// sums (one in front, one behind per chunk) and joined in chunk order by a last kernel.  Nothing is added atomically: the
+// order of every sum depends on the sizes and the tokens alone.
 #include "lmt_device.h"
 #include "lmt_internal.h"
 
@@ -60,7 +61,6 @@ __global__ __launch_bounds__(kThreads) void k_embed(const Embed p, uint32_t lane
 // ---- sorting the tokens --------------------------------------------------------------
 
 constexpr uint32_t kMaxDigitBits = 10, kMaxBins = 1u << kMaxDigitBits;
-constexpr uint32_t kRounds = 16, kSortBlock = kThreads * kRounds;  // tokens a workgroup counts and moves
 
 // A token's sort key: itself, or `vocab`, behind all others, if it has no gradient.
 template <typename I>
@@ -70,31 +70,6 @@ __device__ __forceinline__ uint32_t key_of(const EmbedGrad& p, uint32_t t) {
   if ((uint64_t)token < p.vocab) return (uint32_t)token;
   if (p.status) atomicOr(p.status, LMT_STATUS_BAD_TOKEN);
   return p.vocab;
-}
-
-struct Sort {  // one pass of the radix sort: keys and positions from, keys and positions to (FIRST: from the tokens themselves)
-  const uint32_t *key, *at;
-  uint32_t *key_to, *at_to;
-  uint32_t* counts;  // [blocks][bins]
-  uint32_t shift, bits;
-};
-
-template <typename I, bool FIRST>
-__global__ __launch_bounds__(kThreads) void k_token_counts(const EmbedGrad p, const Sort s) {
-  __shared__ uint32_t bin[kMaxBins];
-  const uint32_t bins = 1u << s.bits;
-  for (uint32_t i = threadIdx.x; i < bins; i += kThreads) bin[i] = 0;
-  __syncthreads();
-#pragma unroll 4
-  for (uint32_t r = 0; r < kRounds; ++r) {
-    const uint32_t t = blockIdx.x * kSortBlock + r * kThreads + threadIdx.x;
-    if (t < p.n_tokens) {
-      const uint32_t key = FIRST ? key_of<I>(p, t) : s.key[t];
-      atomicAdd(&bin[key >> s.shift & (bins - 1u)], 1u);
-    }
-  }
-  __syncthreads();
-  for (uint32_t i = threadIdx.x; i < bins; i += kThreads) s.counts[(uint64_t)blockIdx.x * bins + i] = bin[i];
 }
 
 // Lanes of this wavefront that hold the same digit, among the lanes in `valid`.
@@ -108,244 +83,445 @@ __device__ __forceinline__ uint64_t same_digit(uint32_t digit, uint32_t bits, ui
   return same;
 }
 
-template <typename I, bool FIRST>
-__global__ __launch_bounds__(kThreads) void k_token_move(const EmbedGrad p, const Sort s, uint32_t n_blocks) {
-  __shared__ uint32_t seen[kWaves][kMaxBins];  // per wavefront: how many of a digit so far; then where its next one goes
-  __shared__ uint32_t wave_sum[kWaves];
-  const uint32_t bins = 1u << s.bits, wave = threadIdx.x >> 6, lane = lane_id();
-  for (uint32_t i = threadIdx.x; i < kWaves * kMaxBins; i += kThreads) seen[i / kMaxBins][i % kMaxBins] = 0;
-  __syncthreads();
-  // ranks among the wavefront's equal digits; a wavefront has 16 x 64 consecutive positions
-  uint32_t key[kRounds], at[kRounds], rank[kRounds];
-  volatile uint32_t* mine = seen[wave];
-  const uint32_t first = blockIdx.x * kSortBlock + wave * (kRounds * 64u);
+// Ranks of a wavefront's keys (R x 64 in a row, round by round) among its equal digits; seen[digit], cleared before, counts them.
+template <int R>
+__device__ __forceinline__ void rank_digits(const uint32_t (&key)[R], uint32_t shift, uint32_t bits, uint32_t n_valid, volatile uint16_t* seen, uint32_t (&rank)[R]) {
+  const uint32_t lane = lane_id();
 #pragma unroll
-  for (uint32_t r = 0; r < kRounds; ++r) {
+  for (int r = 0; r < R; ++r) {
+    const bool valid = r * 64u + lane < n_valid;
+    const uint32_t digit = key[r] >> shift & ((1u << bits) - 1u);
+    const uint64_t same = same_digit(digit, bits, __ballot(valid));
+    const uint32_t before = (uint32_t)__popcll(same & ((1ull << lane) - 1ull));
+    rank[r] = valid ? seen[digit] + before : 0u;
+    __builtin_amdgcn_wave_barrier();
+    if (valid && before == 0) seen[digit] = (uint16_t)(rank[r] + (uint32_t)__popcll(same));
+    __builtin_amdgcn_wave_barrier();
+  }
+}
+
+// Sum over the threads in front of this one.  sums: LDS, one word per wavefront.
+__device__ __forceinline__ uint32_t sum_in_front(uint32_t x, uint32_t* sums) {
+  const uint32_t lane = lane_id(), wave = threadIdx.x >> 6;
+  uint32_t up_to = x;
+#pragma unroll
+  for (uint32_t d = 1; d < 64; d *= 2) {
+    const uint32_t y = __shfl_up(up_to, d);
+    if (lane >= d) up_to += y;
+  }
+  if (lane == 63) sums[wave] = up_to;
+  __syncthreads();
+  uint32_t before = up_to - x;
+  for (uint32_t w = 0; w < wave; ++w) before += sums[w];
+  return before;
+}
+
+// Rows of bytes to be cleared, `bytes` of each; a table without gaps is one long row cut into pieces.
+struct Clear {
+  char* at;
+  uint64_t rows, stride, bytes, end;  // end: of the last row
+};
+__device__ __forceinline__ void clear_rows(const Clear& c, uint64_t first, uint64_t step) {
+  for (uint64_t r = first; r < c.rows; r += step) {
+    char* row = c.at + r * c.stride;
+    const uint64_t n = min(c.bytes, c.end - r * c.stride);
+    for (uint64_t b = (uint64_t)lane_id() * 16u; b < n; b += 1024u) {
+      if (b + 16u <= n) {
+        *(LMT_GLOBAL typename At<2>::x4*)(row + b) = u32x4{0, 0, 0, 0};
+      } else {
+        for (uint64_t e = b; e < n; e += 2u) *(LMT_GLOBAL uint16_t*)(row + e) = 0;
+      }
+    }
+  }
+}
+
+// A token's key and its position.
+__device__ __forceinline__ u32x2 pair_at(const u32x2* list, uint64_t i) { return *(const LMT_GLOBAL u32x2*)(list + i); }
+__device__ __forceinline__ uint32_t key_at(const u32x2* list, uint64_t i) { return *(const LMT_GLOBAL uint32_t*)(list + i); }
+
+constexpr uint32_t kSortThreads = 1024, kSortWaves = kSortThreads / 64;
+
+// The whole sort of up to 1024 R tokens by workgroup 0, digit after digit in LDS; the other workgroups clear the table
+// meanwhile (the rows that get a sum are written twice for that).
+template <typename I, int R>
+__global__ __launch_bounds__(kSortThreads) void k_token_sort(const EmbedGrad p, uint32_t passes, uint32_t bits, u32x2* list, const Clear clear) {
+  const uint32_t wave = threadIdx.x >> 6, lane = lane_id();
+  if (blockIdx.x > 0) {
+    clear_rows(clear, (uint64_t)(blockIdx.x - 1u) * kSortWaves + wave, (uint64_t)(gridDim.x - 1u) * kSortWaves);
+    return;
+  }
+  __shared__ uint32_t keys[kSortThreads * R];
+  __shared__ uint16_t ats[kSortThreads * R];
+  __shared__ uint16_t seen[kSortWaves][kMaxBins];
+  __shared__ uint32_t sums[kSortWaves];
+  const uint32_t first = wave * (R * 64u), bins = 1u << bits;
+  const uint32_t n_valid = p.n_tokens > first ? p.n_tokens - first : 0u;
+  uint32_t key[R], at[R], rank[R];
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    at[r] = first + r * 64u + lane;
+    key[r] = at[r] < p.n_tokens ? key_of<I>(p, at[r]) : 0u;
+  }
+  for (uint32_t pass = 0; pass < passes; ++pass) {
+    const uint32_t shift = pass * bits;
+    for (uint32_t i = threadIdx.x; i < kSortWaves * bins; i += kSortThreads) seen[i >> bits][i & (bins - 1u)] = 0;
+    __syncthreads();
+    rank_digits<R>(key, shift, bits, n_valid, seen[wave], rank);
+    __syncthreads();
+    uint32_t count = 0;
+    if (threadIdx.x < bins) {
+#pragma unroll
+      for (uint32_t w = 0; w < kSortWaves; ++w) count += seen[w][threadIdx.x];
+    }
+    uint32_t to = sum_in_front(count, sums);
+    if (threadIdx.x < bins) {
+#pragma unroll
+      for (uint32_t w = 0; w < kSortWaves; ++w) {
+        const uint32_t c = seen[w][threadIdx.x];
+        seen[w][threadIdx.x] = (uint16_t)to;
+        to += c;
+      }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      if (r * 64u + lane >= n_valid) continue;
+      to = seen[wave][key[r] >> shift & (bins - 1u)] + rank[r];
+      keys[to] = key[r], ats[to] = (uint16_t)at[r];
+    }
+    __syncthreads();
+    if (pass + 1u == passes) break;
+#pragma unroll
+    for (int r = 0; r < R; ++r) key[r] = keys[first + r * 64u + lane], at[r] = ats[first + r * 64u + lane];
+  }
+  for (uint32_t i = threadIdx.x; i < p.n_tokens; i += kSortThreads) *(LMT_GLOBAL u32x2*)(list + i) = u32x2{keys[i], ats[i]};
+}
+
+// One pass of the sort of more tokens than that: workgroups count their digits, then each adds up the counts and moves its
+// tokens.  1024 threads with R tokens each: 2 where that makes up to 256 workgroups, which all read all counts, and 8 above.
+struct Sort {  // FIRST: from the tokens themselves
+  const u32x2* from;
+  u32x2* to;
+  uint16_t* counts;  // [blocks][bins]
+  uint32_t shift, bits, blocks;
+};
+
+template <typename I, bool FIRST, int R>
+__global__ __launch_bounds__(kSortThreads) void k_token_counts(const EmbedGrad p, const Sort s) {
+  __shared__ uint32_t bin[kMaxBins];
+  const uint32_t bins = 1u << s.bits;
+  uint32_t key[R];
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    const uint32_t t = blockIdx.x * (R * kSortThreads) + r * kSortThreads + threadIdx.x;
+    key[r] = t < p.n_tokens ? (FIRST ? key_of<I>(p, t) : key_at(s.from, t)) : ~0u;
+  }
+  if (threadIdx.x < bins) bin[threadIdx.x] = 0;
+  __syncthreads();
+#pragma unroll
+  for (int r = 0; r < R; ++r)
+    if (key[r] != ~0u) atomicAdd(&bin[key[r] >> s.shift & (bins - 1u)], 1u);
+  __syncthreads();
+  if (threadIdx.x < bins) s.counts[(uint64_t)blockIdx.x * bins + threadIdx.x] = (uint16_t)bin[threadIdx.x];
+}
+
+template <typename I, bool FIRST, int R>
+__global__ __launch_bounds__(kSortThreads) void k_token_move(const EmbedGrad p, const Sort s) {
+  __shared__ uint16_t seen[kSortWaves][kMaxBins];  // of a wavefront's tokens so far
+  __shared__ uint32_t start[kMaxBins];             // where this workgroup's tokens of a digit go
+  __shared__ uint32_t all_part[8 * kSortThreads], front_part[8 * kSortThreads];
+  __shared__ uint32_t sums[kSortWaves];
+  const uint32_t bins = 1u << s.bits, wave = threadIdx.x >> 6, lane = lane_id();
+  const uint32_t first = blockIdx.x * (R * kSortThreads) + wave * (R * 64u);
+  const uint32_t n_valid = p.n_tokens > first ? p.n_tokens - first : 0u;
+  uint32_t key[R], at[R], rank[R];
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
     const uint32_t t = first + r * 64u + lane;
     key[r] = 0, at[r] = t;
     if (t < p.n_tokens) {
-      key[r] = FIRST ? key_of<I>(p, t) : s.key[t];
-      if (!FIRST) at[r] = s.at[t];
+      if (FIRST) {
+        key[r] = key_of<I>(p, t);
+      } else {
+        const u32x2 x = pair_at(s.from, t);
+        key[r] = x.x, at[r] = x.y;
+      }
     }
   }
+  for (uint32_t i = threadIdx.x; i < kSortWaves * bins; i += kSortThreads) seen[i >> s.bits][i & (bins - 1u)] = 0;
+  // the counts of all workgroups and of those in front: a thread has eight digits of every n-th workgroup
+  {
+    const uint32_t across = bins / 8u, groups = kSortThreads / across, group = threadIdx.x / across, d = threadIdx.x % across * 8u;
+    uint32_t all[8] = {}, front[8] = {};
+#pragma unroll 4
+    for (uint32_t b = group; b < s.blocks; b += groups) {
+      const u32x4 w = *(const LMT_GLOBAL u32x4*)(s.counts + (uint64_t)b * bins + d);
 #pragma unroll
-  for (uint32_t r = 0; r < kRounds; ++r) {
-    const bool valid = first + r * 64u + lane < p.n_tokens;
-    const uint32_t digit = key[r] >> s.shift & (bins - 1u);
-    const uint64_t same = same_digit(digit, s.bits, __ballot(valid));
-    const uint32_t before = (uint32_t)__popcll(same & ((1ull << lane) - 1ull));
-    rank[r] = 0;
-    if (valid) rank[r] = mine[digit] + before;
-    __builtin_amdgcn_wave_barrier();
-    if (valid && before == 0) mine[digit] = rank[r] + (uint32_t)__popcll(same);
-    __builtin_amdgcn_wave_barrier();
-  }
-  __syncthreads();
-  // where each digit of this workgroup starts: the smaller digits of all workgroups, this digit of the workgroups in front
-  uint32_t in_front[kMaxBins / kThreads], sum = 0;
-  const uint32_t per = (bins + kThreads - 1u) / kThreads;  // digits threadIdx.x * per ...
-#pragma unroll
-  for (uint32_t j = 0; j < kMaxBins / kThreads; ++j) {
-    const uint32_t d = threadIdx.x * per + j;
-    in_front[j] = 0;
-    if (j >= per || d >= bins) continue;
-    uint32_t all = 0;
-    for (uint32_t b = 0; b < n_blocks; ++b) {
-      const uint32_t c = s.counts[(uint64_t)b * bins + d];
-      if (b < blockIdx.x) in_front[j] += c;
-      all += c;
+      for (uint32_t i = 0; i < 8; ++i) {
+        const uint32_t c = w[i / 2] >> (16 * (i & 1)) & 0xffffu;
+        all[i] += c;
+        front[i] += b < blockIdx.x ? c : 0u;
+      }
     }
-    in_front[j] += sum;
-    sum += all;
-  }
-  uint32_t before = sum;  // exclusive sum over the threads
 #pragma unroll
-  for (uint32_t d = 1; d < 64; d *= 2) {
-    const uint32_t x = __shfl_up(before, d);
-    if (lane >= d) before += x;
+    for (uint32_t i = 0; i < 8; ++i) all_part[group * bins + d + i] = all[i], front_part[group * bins + d + i] = front[i];
   }
-  if (lane == 63) wave_sum[wave] = before;
-  before -= sum;
   __syncthreads();
-  for (uint32_t w = 0; w < wave; ++w) before += wave_sum[w];
+  rank_digits<R>(key, s.shift, s.bits, n_valid, seen[wave], rank);
+  // where this workgroup's tokens of a digit go: behind the smaller digits of all workgroups and this digit of those in front
+  uint32_t all = 0, front = 0;
+  if (threadIdx.x < bins)
+    for (uint32_t g = threadIdx.x; g < 8u * kSortThreads; g += bins) all += all_part[g], front += front_part[g];
+  const uint32_t before = sum_in_front(all, sums);  // a barrier for `seen` too
+  if (threadIdx.x < bins) {
+    start[threadIdx.x] = before + front;
+    uint32_t to = 0;
 #pragma unroll
-  for (uint32_t j = 0; j < kMaxBins / kThreads; ++j) {
-    const uint32_t d = threadIdx.x * per + j;
-    if (j >= per || d >= bins) continue;
-    uint32_t to = before + in_front[j];
-#pragma unroll
-    for (uint32_t w = 0; w < kWaves; ++w) {
-      const uint32_t c = seen[w][d];
-      seen[w][d] = to;
+    for (uint32_t w = 0; w < kSortWaves; ++w) {
+      const uint32_t c = seen[w][threadIdx.x];
+      seen[w][threadIdx.x] = (uint16_t)to;
       to += c;
     }
   }
   __syncthreads();
 #pragma unroll
-  for (uint32_t r = 0; r < kRounds; ++r) {
-    if (first + r * 64u + lane >= p.n_tokens) continue;
-    const uint32_t to = seen[wave][key[r] >> s.shift & (bins - 1u)] + rank[r];
-    s.key_to[to] = key[r];
-    s.at_to[to] = at[r];
+  for (int r = 0; r < R; ++r) {
+    if (r * 64u + lane >= n_valid) continue;
+    const uint32_t d = key[r] >> s.shift & (bins - 1u);
+    *(LMT_GLOBAL u32x2*)(s.to + start[d] + seen[wave][d] + rank[r]) = u32x2{key[r], at[r]};
   }
 }
 
 // ---- summing the rows ------------------------------------------------------------------
 
 struct Sums {
-  const uint32_t *key, *at;  // sorted: token and position
-  float *front, *behind;     // [chunks][width]: a chunk's share of the row that comes over its start, of the row that leaves over its end
-  uint32_t chunk, n_chunks;
+  const u32x2* list;  // sorted: token and position
+  float* partial;      // [2][chunks][pieces][V]: a chunk's share of the row that comes over its start; of the one that leaves over its end
+  uint32_t chunk, n_chunks, pieces;
 };
 
-// First index in [lo, hi) of the sorted keys that is not below `key`.
-__device__ __forceinline__ uint32_t lower_bound(const uint32_t* keys, uint32_t lo, uint32_t hi, uint32_t key) {
+// First index in [lo, hi) of the sorted list whose key is not below `key`.
+__device__ __forceinline__ uint32_t lower_bound(const u32x2* list, uint32_t lo, uint32_t hi, uint32_t key) {
   while (lo < hi) {
     const uint32_t mid = lo + (hi - lo) / 2u;
-    if (keys[mid] < key) lo = mid + 1u;
+    if (key_at(list, mid) < key) lo = mid + 1u;
     else hi = mid;
   }
   return lo;
 }
 
-// V elements of fp32 of a workspace row whose length may be odd.
+// Row `i` of a matrix with rows of ld elements, `offset` bytes (32 bits, a lane's) into it: for a uniform i the row's address stays in
+// scalar registers, where computing it costs the vector unit nothing.
+template <typename T>
+__device__ __forceinline__ T* in_row(const void* base, uint32_t i, uint64_t ld, uint32_t offset) {
+  return (T*)((LMT_GLOBAL char*)base + i * (ld * sizeof(T)) + offset);
+}
+
+// A lane's V columns of a row: V at a time, the last ones from the end (width >= V), so that every load is a whole vector; of those only
+// the ones from `own` on are the lane's to write (V: none).
 template <int V>
-__device__ __forceinline__ void put_partial(float* to, const float (&x)[V], uint32_t n) {
-#pragma unroll
-  for (int i = 0; i < V; ++i)
-    if ((uint32_t)i < n) store1(to + i, x[i]);
-}
-
-template <typename TO, int V>
-__device__ __forceinline__ void put_row(const EmbedGrad& p, uint32_t key, uint32_t col, uint32_t n, const float (&sum)[V]) {
-  TO* to = static_cast<TO*>(p.grad) + (uint64_t)key * p.grad_ld + col;
-  Vec<TO, V> y = {};
-  float f[V];
-  if (p.accumulate) {
-    if (n == V) load<false>(y, to);
-    else load_end(y, to, n, 0.f);
+struct Piece {
+  uint32_t index, col, own;
+  __device__ __forceinline__ Piece(uint32_t i, uint32_t width, uint32_t pieces) {
+    index = min(i, pieces - 1u);
+    col = min(index * V, width - V);
+    own = i < pieces ? index * V - col : (uint32_t)V;
   }
+};
+template <typename T, int V>
+__device__ __forceinline__ void store_own(T* to, const Vec<T, V>& y, uint32_t own) {
+  if (own == 0) {
+    store<true>(to, y);
+  } else {
 #pragma unroll
-  for (int i = 0; i < V; ++i) f[i] = p.accumulate ? __builtin_fmaf(sum[i], p.scale, y.get(i)) : sum[i] * p.scale;
+    for (int i = 0; i < V; ++i)
+      if ((uint32_t)i >= own) store1(to + i, from_f32<T>(y.get(i)));
+  }
+}
+template <typename TO, int V>
+__device__ __forceinline__ void put_row(const EmbedGrad& p, uint32_t key, const Piece<V>& piece, const float (&sum)[V], const Vec<TO, V>& old, bool add) {
+  float f[V];
+#pragma unroll
+  for (int i = 0; i < V; ++i) f[i] = add ? __builtin_fmaf(sum[i], p.scale, old.get(i)) : sum[i] * p.scale;
+  Vec<TO, V> y;
   y.set(f);
-  if (n == V) store<false>(to, y);
-  else store_end(to, y, n);
+  store_own(in_row<TO>(p.grad, key, p.grad_ld, piece.col * (uint32_t)sizeof(TO)), y, piece.own);
+}
+template <int V>
+__device__ __forceinline__ float* partial_at(const Sums& s, uint32_t c, const Piece<V>& piece) {  // c: of the chunk, plus n_chunks for its end
+  return s.partial + ((uint64_t)c * s.pieces + piece.index) * V;
 }
 
-constexpr uint32_t kBatch = 8;  // rows in flight per wavefront
-
-// Workgroups [0, sum_blocks): a wavefront per chunk and slab of 64 pieces.  Behind them, without LMT_ACCUMULATE: rows of tokens that
-// do not occur, 64 per wavefront, are cleared.
-template <typename TI, typename TO>
+// A wavefront loads rows in batches, one ahead of the one that it adds, and with them, when it accumulates (ADD), what the table
+// holds for the tokens that end there.
+// Workgroups [0, sum_blocks): a wavefront per chunk and slab of 64 pieces.  Behind them, where the table has not been cleared: rows
+// of tokens that do not occur, 64 per wavefront, are.
+template <typename TI, typename TO, int V, bool ADD>
 __global__ __launch_bounds__(kThreads) void k_token_sums(const EmbedGrad p, const Sums s, uint32_t slabs, uint32_t sum_blocks) {
-  constexpr int V = 16 / sizeof(TI);
+  constexpr uint32_t kBatch = ADD ? 4 : 8;
   const uint32_t lane = lane_id();
-  if (blockIdx.x >= sum_blocks) {
+  if (!ADD && blockIdx.x >= sum_blocks) {
     const uint64_t v0 = ((uint64_t)(blockIdx.x - sum_blocks) * kWaves + (threadIdx.x >> 6)) * 64u;
     bool absent = false;
     if (v0 + lane < p.vocab) {
-      const uint32_t i = lower_bound(s.key, 0, p.n_tokens, (uint32_t)v0 + lane);
-      absent = i == p.n_tokens || s.key[i] != (uint32_t)v0 + lane;
+      const uint32_t i = lower_bound(s.list, 0, p.n_tokens, (uint32_t)v0 + lane);
+      absent = i == p.n_tokens || key_at(s.list, i) != (uint32_t)v0 + lane;
     }
-    constexpr int Z = 16 / sizeof(TO);
     for (uint64_t rows = __ballot(absent); rows != 0; rows &= rows - 1ull) {
       TO* row = static_cast<TO*>(p.grad) + (v0 + (uint64_t)(__ffsll((unsigned long long)rows) - 1)) * p.grad_ld;
-      for (uint32_t col = lane * Z; col < p.width; col += 64u * Z) {
-        const Vec<TO, Z> zero = {};
-        const uint32_t n = min((uint32_t)Z, p.width - col);
-        if (n == Z) store<false>(row + col, zero);
-        else store_end(row + col, zero, n);
+      for (uint32_t q = lane; q < s.pieces; q += 64u) {
+        const Piece<V> piece(q, p.width, s.pieces);
+        Vec<TO, V> zero;
+        const float f[V] = {};
+        zero.set(f);
+        store_own(row + piece.col, zero, piece.own);
       }
     }
     return;
   }
-  const uint32_t unit = blockIdx.x * kWaves + (threadIdx.x >> 6);
+  const uint32_t unit = blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const uint32_t c = unit / slabs;
   if (c >= s.n_chunks) return;
-  const uint32_t col = (unit % slabs * 64u + lane) * V;
-  const uint32_t n = col < p.width ? min((uint32_t)V, p.width - col) : 0u;
+  const Piece<V> piece(unit % slabs * 64u + lane, p.width, s.pieces);
   const uint32_t lo = c * s.chunk, hi = min(p.n_tokens, lo + s.chunk);
-  const uint32_t before = lo > 0 ? s.key[lo - 1u] : ~0u, behind = hi < p.n_tokens ? s.key[hi] : ~0u;
-  float sum[V] = {};
-  uint32_t run = ~0u;      // the token whose rows are being summed
+  const uint32_t before = __builtin_amdgcn_readfirstlane(lo > 0 ? key_at(s.list, lo - 1u) : ~0u);
+  const uint32_t behind = __builtin_amdgcn_readfirstlane(hi < p.n_tokens ? key_at(s.list, hi) : ~0u);
+  float sum[V];
+  uint32_t run = ~0u;       // the token whose rows are being summed
   bool from_front = false;  // ... since the chunk in front
-  const auto finish = [&](bool leaves) {
-    float* to = from_front ? s.front : leaves ? s.behind : nullptr;
-    if (to) put_partial(to + (uint64_t)c * p.width + col, sum, n);
-    else if (n != 0) put_row<TO>(p, run, col, n, sum);
+  struct Batch {
+    Vec<TI, V> x[kBatch];
+    Vec<TO, V> old[ADD ? kBatch : 1];
   };
   for (uint32_t i0 = lo; i0 < hi; i0 += 64u) {
-    const uint32_t i = min(i0 + lane, p.n_tokens - 1u);
-    const uint32_t key = s.key[i], at = s.at[i];
-    const uint32_t count = (uint32_t)__popcll(__ballot(i0 + lane < hi && key < p.vocab));  // those without gradient are last
-    for (uint32_t j0 = 0; j0 < count; j0 += kBatch) {
-      Vec<TI, V> x[kBatch];
+    const uint32_t i = min(i0 + lane, hi - 1u);
+    const u32x2 pair = pair_at(s.list, i);
+    const uint32_t next = i + 1u < hi ? key_at(s.list, i + 1u) : ~0u;
+    const uint64_t valid = __ballot(i0 + lane < hi && pair.x < p.vocab);  // those without gradient are last
+    const uint64_t ends = __ballot(pair.x != next) & valid;
+    const uint32_t count = (uint32_t)__popcll(valid);
+    if (count == 0) break;
+    const auto fetch = [&](Batch& b, uint32_t j0) {
 #pragma unroll
       for (uint32_t j = 0; j < kBatch; ++j) {
-        x[j] = {};
-        if (j0 + j < count && n != 0) {
-          const uint32_t t = __builtin_amdgcn_readlane(at, j0 + j);
-          const TI* from = static_cast<const TI*>(p.grad_out) + (uint64_t)t * p.grad_out_ld + col;
-          if (n == V) load<false>(x[j], from);
-          else load_end(x[j], from, n, 0.f);
+        const uint32_t at = min(j0 + j, count - 1u);
+        load<true>(b.x[j], in_row<const TI>(p.grad_out, __builtin_amdgcn_readlane(pair.y, at), p.grad_out_ld, piece.col * (uint32_t)sizeof(TI)));
+        if constexpr (ADD) {
+          if (ends >> at & 1ull) load<true>(b.old[j], in_row<const TO>(p.grad, __builtin_amdgcn_readlane(pair.x, at), p.grad_ld, piece.col * (uint32_t)sizeof(TO)));
         }
       }
+    };
+    const auto add = [&](const Batch& b, uint32_t j0) {
 #pragma unroll
       for (uint32_t j = 0; j < kBatch; ++j) {
         if (j0 + j >= count) break;
-        const uint32_t k = __builtin_amdgcn_readlane(key, j0 + j);
+        const uint32_t k = __builtin_amdgcn_readlane(pair.x, j0 + j);
         if (k != run) {
-          if (run != ~0u) finish(false);
           run = k, from_front = i0 + j0 + j == lo && k == before;
 #pragma unroll
           for (int v = 0; v < V; ++v) sum[v] = 0.f;
         }
 #pragma unroll
-        for (int v = 0; v < V; ++v) sum[v] += x[j].get(v);
+        for (int v = 0; v < V; ++v) sum[v] += b.x[j].get(v);
+        if (ends >> (j0 + j) & 1ull) {
+          if (from_front || (i0 + j0 + j + 1u == hi && k == behind)) {
+            float* to = partial_at(s, from_front ? c : s.n_chunks + c, piece);
+#pragma unroll
+            for (int v = 0; v < V; ++v) *(LMT_GLOBAL float*)(to + v) = sum[v];
+          } else {
+            put_row<TO, V>(p, k, piece, sum, b.old[ADD ? j : 0], ADD);
+          }
+        }
       }
+    };
+    Batch a, b;
+    fetch(a, 0);
+    for (uint32_t j0 = 0; j0 < count; j0 += 2u * kBatch) {
+      fetch(b, j0 + kBatch);
+      add(a, j0);
+      fetch(a, j0 + 2u * kBatch);
+      add(b, j0 + kBatch);
     }
     if (count < 64u) break;
   }
-  if (run != ~0u) finish(run == behind);
 }
 
-// Rows that go over chunk ends: the workgroup of the chunk where such a row starts adds its partial sums, eight wavefronts
-// every eighth of them, then the eight sums in order.
-constexpr uint32_t kJoinWaves = 8;
-template <typename TO>
+// Rows that go over chunk ends.  A wavefront looks at one chunk and, if such a row starts there, adds its partial sums; a row of over
+// kLong chunks is left to all wavefronts of the workgroup, which add every sixteenth of its chunks, then the sixteen sums in order.
+constexpr uint32_t kJoinWaves = 16, kLong = 16;
+template <typename TO, int V>
 __global__ __launch_bounds__(64 * kJoinWaves) void k_token_joins(const EmbedGrad p, const Sums s) {
-  __shared__ float part[kJoinWaves][64][4];
-  const uint32_t c = blockIdx.x, lane = lane_id(), wave = threadIdx.x >> 6;
-  const uint32_t lo = c * s.chunk, hi = lo + s.chunk;
-  if (hi >= p.n_tokens) return;
-  const uint32_t key = s.key[hi - 1u];
-  if (key >= p.vocab || s.key[hi] != key) return;                       // no row leaves
-  if (s.key[lo] == key && lo > 0 && s.key[lo - 1u] == key) return;        // it started further in front
-  const uint32_t end = lower_bound(s.key, hi, p.n_tokens, key + 1u);      // the row's tokens are [.., end)
-  const uint32_t last = (end - 1u) / s.chunk;                             // its last chunk
-  const uint32_t col = (blockIdx.y * 64u + lane) * 4u;
-  const uint32_t n = col < p.width ? min(4u, p.width - col) : 0u;
-  float sum[4] = {};
-  if (wave == 0) {
+  __shared__ float part[kJoinWaves][V][64];
+  __shared__ uint32_t long_last[kJoinWaves];
+  const uint32_t lane = lane_id(), wave = threadIdx.x >> 6;
+  const Piece<V> piece(blockIdx.y * 64u + lane, p.width, s.pieces);
+  const auto get = [&](uint32_t c, float (&x)[V]) {
+    const float* from = partial_at(s, c, piece);
 #pragma unroll
-    for (uint32_t v = 0; v < 4; ++v)
-      if (v < n) sum[v] = load1(s.behind + (uint64_t)c * p.width + col + v);
+    for (int v = 0; v < V; ++v) x[v] = *(const LMT_GLOBAL float*)(from + v);
+  };
+  // adds chunks d, d + step, ... up to the last one, eight loads ahead
+  const auto add = [&](float (&sum)[V], uint32_t d, uint32_t last, uint32_t step) {
+    for (; d <= last; d += 8u * step) {
+      float x[8][V];
+#pragma unroll
+      for (uint32_t i = 0; i < 8; ++i) get(min(d + i * step, last), x[i]);
+#pragma unroll
+      for (uint32_t i = 0; i < 8; ++i)
+#pragma unroll
+        for (int v = 0; v < V; ++v) sum[v] += d + i * step <= last ? x[i][v] : 0.f;
+    }
+  };
+  const auto old_of = [&](uint32_t key, Vec<TO, V>& old) {
+    if (p.accumulate) load<true>(old, static_cast<const TO*>(p.grad) + (uint64_t)key * p.grad_ld + piece.col);
+  };
+  const uint32_t c = blockIdx.x * kJoinWaves + wave;
+  uint32_t last = 0, key = 0;
+  if (c + 1u < s.n_chunks) {
+    const uint32_t lo = c * s.chunk, hi = lo + s.chunk;
+    key = key_at(s.list, hi - 1u);
+    const uint32_t next = key_at(s.list, hi), start = key_at(s.list, lo), before = lo > 0 ? key_at(s.list, lo - 1u) : ~0u;
+    if (key < p.vocab && next == key && !(start == key && before == key)) {  // a row leaves that has not come over the start
+      last = c;
+      for (uint64_t more = ~0ull; more == ~0ull; last += more == ~0ull ? 64u : (uint32_t)__ffsll((unsigned long long)~more) - 1u)
+        more = __ballot((uint64_t)last + 1u + lane < s.n_chunks && key_at(s.list, (uint64_t)(last + 1u + lane) * s.chunk) == key);
+    }
   }
-#pragma unroll 4
-  for (uint32_t d = c + 1u + wave; d <= last; d += kJoinWaves) {
-#pragma unroll
-    for (uint32_t v = 0; v < 4; ++v)
-      if (v < n) sum[v] += load1(s.front + (uint64_t)d * p.width + col + v);
+  const bool is_long = last > c + kLong;
+  if (last != 0 && !is_long) {
+    float sum[V];
+    Vec<TO, V> old;
+    old_of(key, old);
+    get(s.n_chunks + c, sum);
+    add(sum, c + 1u, last, 1u);
+    put_row<TO, V>(p, key, piece, sum, old, p.accumulate);
   }
-#pragma unroll
-  for (uint32_t v = 0; v < 4; ++v) part[wave][lane][v] = sum[v];
+  if (lane == 0) long_last[wave] = is_long ? last : 0u;
   __syncthreads();
-  if (wave != 0 || n == 0) return;
+  for (uint32_t w = 0; w < kJoinWaves; ++w) {
+    last = long_last[w];
+    if (last == 0) continue;
+    const uint32_t cw = blockIdx.x * kJoinWaves + w;
+    float sum[V] = {};
+    Vec<TO, V> old;
+    if (wave == 0) {
+      key = key_at(s.list, (uint64_t)last * s.chunk);
+      old_of(key, old);
+      get(s.n_chunks + cw, sum);
+    }
+    add(sum, cw + 1u + wave, last, kJoinWaves);
 #pragma unroll
-  for (uint32_t w = 1; w < kJoinWaves; ++w)
+    for (int v = 0; v < V; ++v) part[wave][v][lane] = sum[v];
+    __syncthreads();
+    if (wave == 0) {
 #pragma unroll
-    for (uint32_t v = 0; v < 4; ++v) sum[v] += part[w][lane][v];
-  put_row<TO>(p, key, col, n, sum);
+      for (uint32_t x = 1; x < kJoinWaves; ++x)
+#pragma unroll
+        for (int v = 0; v < V; ++v) sum[v] += part[x][v][lane];
+      put_row<TO, V>(p, key, piece, sum, old, p.accumulate);
+    }
+    __syncthreads();
+  }
 }
 
 // A table without a token: zeros.
@@ -358,37 +534,44 @@ __global__ __launch_bounds__(kThreads) void k_token_none(const EmbedGrad p) {
 
 // ---- launches ------------------------------------------------------------------------
 
-uint32_t chunk_of(uint64_t n_tokens) {  // positions per chunk: 16, and about a thousand chunks where there are many
+uint32_t chunk_of(uint64_t n_tokens) {  // positions per chunk: 16, and about two thousand chunks where there are many
   uint64_t chunk = 16;
-  while (chunk * 1024u < n_tokens) chunk *= 2;
+  while (chunk * 2048u < n_tokens) chunk *= 2;
   return (uint32_t)chunk;
 }
 
+constexpr uint64_t kMostSorted = 16 * kSortThreads;  // tokens that one workgroup sorts
+
 struct Passes {
-  uint32_t n, bits, blocks;
+  uint32_t n, bits, rounds, blocks;
 };
 Passes passes_of(uint64_t n_tokens, uint64_t vocab) {
   uint32_t bits = 1;
   while (vocab >> bits) ++bits;  // keys 0 .. vocab
   const uint32_t n = (uint32_t)ceil_div(bits, kMaxDigitBits);
-  return {n, (uint32_t)ceil_div(bits, n), (uint32_t)ceil_div(n_tokens, kSortBlock)};
+  const uint32_t rounds = n_tokens <= 256u * 2u * kSortThreads ? 2u : 8u;
+  return {n, std::max(3u, (uint32_t)ceil_div(bits, n)), rounds, (uint32_t)ceil_div(n_tokens, rounds * kSortThreads)};
 }
 
 struct Parts {  // offsets in bytes
-  uint64_t key[2], at[2], counts, front, behind, total;
+  uint64_t list[2], counts, partial, total;
 };
 Parts parts_of(uint64_t n_tokens, uint64_t vocab, uint64_t width) {
   const Passes passes = passes_of(n_tokens, vocab);
-  const uint64_t ids = round_up(4 * n_tokens, 256), rows = round_up(4 * width * ceil_div(n_tokens, chunk_of(n_tokens)), 256);
+  const uint64_t list = round_up(8 * n_tokens, 256), rows = 4 * round_up(width, 8) * ceil_div(n_tokens, chunk_of(n_tokens));
+  const bool small = n_tokens <= kMostSorted;
   Parts w{};
-  for (int i = 0; i < 2; ++i) w.key[i] = 2 * i * ids, w.at[i] = (2 * i + 1) * ids;
-  w.counts = 4 * ids;
-  w.front = w.counts + round_up((uint64_t)passes.blocks * 4 << passes.bits, 256);
-  w.behind = w.front + rows;
-  w.total = w.behind + rows;
+  w.list[0] = 0, w.list[1] = list;
+  w.counts = 2 * list;
+  w.partial = small ? list : w.counts + round_up(2 * (uint64_t)passes.blocks << passes.bits, 256);
+  w.total = w.partial + 2 * rows;
   return w;
 }
 
+template <int N>
+struct Const {
+  static constexpr int value = N;
+};
 template <typename F>
 hipError_t with_float(int dtype, F f) {
   switch (dtype) {
@@ -437,39 +620,55 @@ hipError_t launch_embed_grad(const EmbedGrad& p, int grad_out_dtype, int token_d
   const Passes passes = passes_of(p.n_tokens, p.vocab);
   const Parts w = parts_of(p.n_tokens, p.vocab, p.width);
   char* base = static_cast<char*>(workspace);
-  uint32_t* key[2] = {(uint32_t*)(base + w.key[0]), (uint32_t*)(base + w.key[1])};
-  uint32_t* at[2] = {(uint32_t*)(base + w.at[0]), (uint32_t*)(base + w.at[1])};
-  hipError_t e = with_id(token_dtype, [&](auto id) {
-    typedef decltype(id) I;
-    for (uint32_t i = 0; i < passes.n; ++i) {
-      const Sort sort{key[(i + 1) & 1], at[(i + 1) & 1], key[i & 1], at[i & 1], (uint32_t*)(base + w.counts), i * passes.bits, passes.bits};
-      if (i == 0) {
-        hipLaunchKernelGGL((k_token_counts<I, true>), dim3(passes.blocks), dim3(kThreads), 0, s, p, sort);
-        hipLaunchKernelGGL((k_token_move<I, true>), dim3(passes.blocks), dim3(kThreads), 0, s, p, sort, passes.blocks);
-      } else {
-        hipLaunchKernelGGL((k_token_counts<I, false>), dim3(passes.blocks), dim3(kThreads), 0, s, p, sort);
-        hipLaunchKernelGGL((k_token_move<I, false>), dim3(passes.blocks), dim3(kThreads), 0, s, p, sort, passes.blocks);
-      }
-    }
-    return hipGetLastError();
-  });
-  if (e != hipSuccess) return e;
-  const uint32_t last = (passes.n - 1) & 1;
-  const uint32_t chunk = chunk_of(p.n_tokens), n_chunks = (uint32_t)ceil_div(p.n_tokens, chunk);
-  const Sums sums{key[last], at[last], (float*)(base + w.front), (float*)(base + w.behind), chunk, n_chunks};
-  return with_float(grad_dtype, [&](auto to) {
-    typedef decltype(to) TO;
-    e = with_float(grad_out_dtype, [&](auto ti) {
-      typedef decltype(ti) TI;
-      const uint32_t slabs = (uint32_t)ceil_div(p.width, 64u * (16u / sizeof(TI)));
-      const uint32_t sum_blocks = (uint32_t)ceil_div((uint64_t)n_chunks * slabs, kWaves);
-      const uint32_t clear_blocks = p.accumulate ? 0u : (uint32_t)ceil_div(p.vocab, 64u * kWaves);
-      hipLaunchKernelGGL((k_token_sums<TI, TO>), dim3(sum_blocks + clear_blocks), dim3(kThreads), 0, s, p, sums, slabs, sum_blocks);
+  u32x2* list[2] = {(u32x2*)(base + w.list[0]), (u32x2*)(base + w.list[1])};
+  const bool small = p.n_tokens <= kMostSorted, cleared = small && !p.accumulate;
+  uint32_t last = 0;
+  hipError_t e;
+  if (small) {
+    const uint64_t size = grad_dtype == LMT_F32 ? 4 : 2, bytes = p.width * size, stride = p.grad_ld * size, end = (p.vocab - 1) * stride + bytes;
+    const Clear clear = p.grad_ld == p.width ? Clear{static_cast<char*>(p.grad), ceil_div(end, 4096), 4096, 4096, end} : Clear{static_cast<char*>(p.grad), p.vocab, stride, bytes, end};
+    const uint32_t grid = 1u + (p.accumulate ? 0u : (uint32_t)std::min<uint64_t>(kCus - 1u, ceil_div(clear.rows, kSortWaves)));
+    e = with_id(token_dtype, [&](auto id) {
+      typedef decltype(id) I;
+      const auto kernel = p.n_tokens <= 2 * kSortThreads ? k_token_sort<I, 2> : p.n_tokens <= 4 * kSortThreads ? k_token_sort<I, 4> : p.n_tokens <= 8 * kSortThreads ? k_token_sort<I, 8> : k_token_sort<I, 16>;
+      hipLaunchKernelGGL(kernel, dim3(grid), dim3(kSortThreads), 0, s, p, passes.n, passes.bits, list[0], clear);
       return hipGetLastError();
     });
-    if (e != hipSuccess || n_chunks < 2u) return e;
-    hipLaunchKernelGGL((k_token_joins<TO>), dim3(n_chunks - 1u, (uint32_t)ceil_div(p.width, 256u)), dim3(64 * kJoinWaves), 0, s, p, sums);
-    return hipGetLastError();
+  } else {
+    last = (passes.n - 1) & 1;
+    e = with_id(token_dtype, [&](auto id) {
+      typedef decltype(id) I;
+      for (uint32_t i = 0; i < passes.n; ++i) {
+        const Sort sort{list[(i + 1) & 1], list[i & 1], (uint16_t*)(base + w.counts), i * passes.bits, passes.bits, passes.blocks};
+        const bool few = passes.rounds == 2;
+        hipLaunchKernelGGL((i == 0 ? few ? k_token_counts<I, true, 2> : k_token_counts<I, true, 8> : few ? k_token_counts<I, false, 2> : k_token_counts<I, false, 8>),
+                           dim3(passes.blocks), dim3(kSortThreads), 0, s, p, sort);
+        hipLaunchKernelGGL((i == 0 ? few ? k_token_move<I, true, 2> : k_token_move<I, true, 8> : few ? k_token_move<I, false, 2> : k_token_move<I, false, 8>),
+                           dim3(passes.blocks), dim3(kSortThreads), 0, s, p, sort);
+      }
+      return hipGetLastError();
+    });
+  }
+  if (e != hipSuccess) return e;
+  const uint32_t chunk = chunk_of(p.n_tokens), n_chunks = (uint32_t)ceil_div(p.n_tokens, chunk);
+  return with_float(grad_out_dtype, [&](auto ti) {
+    return with_float(grad_dtype, [&](auto to) {
+      typedef decltype(ti) TI;
+      typedef decltype(to) TO;
+      const auto go = [&](auto n) {
+        constexpr int V = decltype(n)::value;
+        const Sums sums{list[last], (float*)(base + w.partial), chunk, n_chunks, (uint32_t)ceil_div(p.width, V)};
+        const uint32_t slabs = (uint32_t)ceil_div(sums.pieces, 64);
+        const uint32_t sum_blocks = (uint32_t)ceil_div((uint64_t)n_chunks * slabs, kWaves);
+        const uint32_t clear_blocks = p.accumulate || cleared ? 0u : (uint32_t)ceil_div(p.vocab, 64u * kWaves);
+        hipLaunchKernelGGL((p.accumulate ? k_token_sums<TI, TO, V, true> : k_token_sums<TI, TO, V, false>), dim3(sum_blocks + clear_blocks), dim3(kThreads), 0, s, p, sums, slabs, sum_blocks);
+        if (n_chunks > 1)
+          hipLaunchKernelGGL((k_token_joins<TO, V>), dim3((uint32_t)ceil_div(n_chunks - 1u, kJoinWaves), slabs), dim3(64 * kJoinWaves), 0, s, p, sums);
+        return hipGetLastError();
+      };
+      constexpr int V = 4;
+      return p.width >= (uint32_t)V ? go(Const<V>{}) : go(Const<1>{});
+    });
   });
 }
 

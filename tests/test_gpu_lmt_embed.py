@@ -241,3 +241,18 @@ def test_lookup_and_gradient_in_a_replayed_graph(n):
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(out, eager[0]) and torch.equal(grad, eager[1])
+
+
+@pytest.mark.parametrize("n,vocab", [(262144, 5000), (262145, 5000), (300001, 1 << 21)])
+def test_gradient_of_many_tokens(n, vocab):
+    rng = np.random.default_rng(n)
+    tokens = zipf(rng, n, vocab)
+    g = typed(rng.normal(0, 1, (n, 3)), "bf16")
+    grad = torch.full((vocab, 3), 5.0, device="cuda")
+    ws = torch.empty(lmt.embed_grad_workspace(n, vocab, 3), dtype=torch.uint8, device="cuda")
+    lmt.embed_grad(torch.tensor(g, device="cuda").bfloat16(), ids(tokens, "i32"), grad, ws, skip_token=0)
+    want, size, count = np.zeros((vocab, 3)), np.zeros((vocab, 3)), np.bincount(tokens, minlength=vocab)[:, None]
+    kept = tokens != 0
+    np.add.at(want, tokens[kept], g[kept])
+    np.add.at(size, tokens[kept], np.abs(g[kept]))
+    within(grad.double().cpu().numpy(), want, size * R.U32 * (count + 2))
