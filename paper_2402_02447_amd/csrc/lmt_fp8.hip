@@ -171,142 +171,181 @@ __global__ __launch_bounds__(kThreads) void k_quantize(const Quantize p, uint32_
 // ---- product ---------------------------------------------------------------------------
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
-// A tile of c for WM x WN wavefronts, each with TM x TN squares of 32 x 32.  WIDE: operands are widened to bf16.
+// A tile of c for WM x WN wavefronts, each with TM x TN squares of 32 x 32.  k goes through LDS in blocks of 128 bytes a row, two at
+// a time: one that is being multiplied and one on its way.  With eight wavefronts, two on a SIMD, they go in two groups that
+// take turns: one multiplies 64 bytes of k while the other reads its next operands from LDS.
 template <int WM_, int WN_, int TM_, int TN_>
 struct Shape {
   static constexpr int WM = WM_, WN = WN_, TM = TM_, TN = TN_;
   static constexpr int waves = WM * WN, threads = 64 * waves;
   static constexpr int rows_m = 32 * TM * WM, rows_n = 32 * TN * WN;  // of c
-  static constexpr int rows = rows_m + rows_n;                        // staged for every block of 128: a's, then b's
-  static constexpr int loads = rows * 8 / threads;                    // of 16 bytes per thread
+  static constexpr int rows = rows_m + rows_n;                        // staged: a's, then b's
+  static constexpr int loads = rows * 8 / threads;                    // of 16 bytes per thread and block
+  static constexpr int lds = 2 * rows * 128;                          // stages; then results, 64 x 64 per wavefront
+  static constexpr bool turns = waves == 8;
   static_assert(rows_m % (8 * waves) == 0 && rows_n % (8 * waves) == 0, "a load of all wavefronts is a's or b's");
+  static_assert(TN == 2 && TM % 2 == 0 && lds >= waves * 64 * 64 * 4, "results go out by squares of 64 x 64");
 };
 
-// c's row i, columns j .. j + 3.
-template <typename TC>
-__device__ __forceinline__ void put4(const Matmul& p, uint32_t i, uint32_t j, const f32x4& d) {
-  if (i >= p.m || j >= p.n) return;
-  TC* to = static_cast<TC*>(p.c) + (uint64_t)i * p.ldc + j;
-  const uint32_t n = min(4u, p.n - j);
-  Vec<TC, 4> y = {};
-  if (p.accumulate) {
-    if (n == 4) load<false>(y, to);
-    else load_end(y, to, n, 0.f);
-  }
-  float f[4];
-#pragma unroll
-  for (int r = 0; r < 4; ++r) f[r] = p.accumulate ? d[r] + y.get(r) : d[r];
-  y.set(f);
-  if (n == 4) store<false>(to, y);
-  else store_end(to, y, n);
-}
-
-// Which tile a workgroup has.
+// Which tile a workgroup has: XCD x, which takes every eighth workgroup, has an eighth of the list of tiles, so that its L2 sees neighbours;
+// the list goes down kGroup tiles of m, then across n, so that both operands of the tiles in flight are few.
 struct Tiles {
   uint32_t across, down, splits, split_blocks;  // of c in n and m; parts of k, and blocks of 128 in each
 };
-__device__ __forceinline__ void tile_of(const Tiles& t, uint32_t id, uint32_t* tm, uint32_t* tn, uint32_t* split) {
-  const uint32_t n = t.across * t.down;
-  *split = id / n, id %= n;
-  *tm = id % t.down, *tn = id / t.down;
+constexpr uint32_t kXcds = 8, kGroup = 8;
+__device__ __forceinline__ void tile_of(const Tiles& t, uint32_t id, uint32_t* tm, uint32_t* tn) {
+  const uint32_t n = t.across * t.down, x = id % kXcds, share = n / kXcds, extra = n % kXcds;
+  id = x * share + min(x, extra) + id / kXcds;
+  const uint32_t group = id / (kGroup * t.across), tall = min(kGroup, t.down - group * kGroup), in_group = id - group * kGroup * t.across;
+  *tm = group * kGroup + in_group % tall, *tn = in_group / tall;
 }
 
 // The matrix instructions take X = b and Y = a: D[i][j] += sum over k of X[i][k] Y[j][k].  Lane l gives row l % 32 of both and has
 // D[8 g + 4 (l / 32) + r][l % 32] in element 4 g + r: four neighbours of a row of c.  Which k a lane gives is of no concern as long
 // as it is the same for X and Y.
-template <typename S, int AF, int BF, bool WIDE>
-__device__ __forceinline__ void step(f32x16 (&acc)[S::TM][S::TN], const uint8_t* a, const uint8_t* b, const uint32_t (&at)[2][2],
-                                     const uint32_t (&as)[S::TM], const uint32_t (&bs)[S::TN], int block) {
+// What has been added is added here: the compiler would put the instructions off, their operands in registers until then.
+template <typename S>
+__device__ __forceinline__ void settle(f32x16 (&acc)[S::TM][S::TN]) {
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    if constexpr (!WIDE) {
-      i32x8 x[S::TN], y[S::TM];
-      const auto get = [&](const uint8_t* from) {
-        const u32x4 lo = *reinterpret_cast<const u32x4*>(from + at[h][0]), hi = *reinterpret_cast<const u32x4*>(from + at[h][1]);
-        return i32x8{(int)lo.x, (int)lo.y, (int)lo.z, (int)lo.w, (int)hi.x, (int)hi.y, (int)hi.z, (int)hi.w};
-      };
+  for (int i = 0; i < S::TM; ++i)
 #pragma unroll
-      for (int f = 0; f < S::TN; ++f) x[f] = get(b + f * 4096);
+    for (int j = 0; j < S::TN; ++j) asm volatile("" : "+v"(acc[i][j]));
+  __builtin_amdgcn_sched_barrier(0);
+}
+// A lane's operands for 64 bytes of k: pieces at[0] and at[1] of its rows.
+template <typename S>
+struct Operands {
+  u32x4 x[S::TN][2], y[S::TM][2];
+  __device__ __forceinline__ void read(const uint8_t* a, const uint8_t* b, const uint32_t (&at)[2]) {
 #pragma unroll
-      for (int f = 0; f < S::TM; ++f) y[f] = get(a + f * 4096);
+    for (int f = 0; f < S::TN; ++f)
 #pragma unroll
-      for (int i = 0; i < S::TM; ++i)
+      for (int q = 0; q < 2; ++q) x[f][q] = *reinterpret_cast<const u32x4*>(b + f * 4096 + at[q]);
 #pragma unroll
-        for (int j = 0; j < S::TN; ++j) {
-          switch (block) {
-            case 0: acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(x[j], y[i], acc[i][j], BF, AF, 0, (int)bs[j], 0, (int)as[i]); break;
-            case 1: acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(x[j], y[i], acc[i][j], BF, AF, 1, (int)bs[j], 1, (int)as[i]); break;
-            case 2: acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(x[j], y[i], acc[i][j], BF, AF, 2, (int)bs[j], 2, (int)as[i]); break;
-            default: acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(x[j], y[i], acc[i][j], BF, AF, 3, (int)bs[j], 3, (int)as[i]); break;
-          }
-        }
-    } else {
+    for (int f = 0; f < S::TM; ++f)
 #pragma unroll
-      for (int q = 0; q < 2; ++q) {
-        bf16x8 x[S::TN][2], y[S::TM][2];
-        const auto get = [&](bf16x8 (&to)[2], const uint8_t* from, uint32_t scales, auto e5m2) {
-          const u32x4 w = *reinterpret_cast<const u32x4*>(from + at[h][q]);
-          const float s = __uint_as_float((scales >> (8 * block) & 255u) << 23);
-#pragma unroll
-          for (int v = 0; v < 4; ++v) {
-            bf16x2 lo, hi;
-            if constexpr (decltype(e5m2)::value) lo = __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8((int)w[v], s, false), hi = __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8((int)w[v], s, true);
-            else lo = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)w[v], s, false), hi = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)w[v], s, true);
-            to[v / 2][4 * (v % 2)] = lo.x, to[v / 2][4 * (v % 2) + 1] = lo.y;
-            to[v / 2][4 * (v % 2) + 2] = hi.x, to[v / 2][4 * (v % 2) + 3] = hi.y;
-          }
-        };
-#pragma unroll
-        for (int f = 0; f < S::TN; ++f) get(x[f], b + f * 4096, bs[f], Const<BF>{});
-#pragma unroll
-        for (int f = 0; f < S::TM; ++f) get(y[f], a + f * 4096, as[f], Const<AF>{});
-#pragma unroll
-        for (int v = 0; v < 2; ++v)
-#pragma unroll
-          for (int i = 0; i < S::TM; ++i)
-#pragma unroll
-            for (int j = 0; j < S::TN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[j][v], y[i][v], acc[i][j], 0, 0, 0);
-      }
-    }
+      for (int q = 0; q < 2; ++q) y[f][q] = *reinterpret_cast<const u32x4*>(a + f * 4096 + at[q]);
   }
+};
+// as, bs: the scales of the lane's rows, this block's in the lowest byte.
+// narrow: one instruction takes 64 bytes of k and the scales.
+template <typename S, int AF, int BF>
+__device__ __forceinline__ void multiply_narrow(f32x16 (&acc)[S::TM][S::TN], const Operands<S>& o, const uint32_t (&as)[S::TM], const uint32_t (&bs)[S::TN]) {
+  const auto whole = [](const u32x4 (&w)[2]) {
+    return i32x8{(int)w[0].x, (int)w[0].y, (int)w[0].z, (int)w[0].w, (int)w[1].x, (int)w[1].y, (int)w[1].z, (int)w[1].w};
+  };
+#pragma unroll
+  for (int i = 0; i < S::TM; ++i)
+#pragma unroll
+    for (int j = 0; j < S::TN; ++j)
+      acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(whole(o.x[j]), whole(o.y[i]), acc[i][j], BF, AF, 0, (int)bs[j], 0, (int)as[i]);
+}
+// Two 8-bit values, the lower or the upper ones of w, in bf16, times s.
+template <int E5M2, bool UPPER>
+__device__ __forceinline__ uint32_t widen(uint32_t w, float s) {
+  if constexpr (E5M2) return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8((int)w, s, UPPER));
+  else return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)w, s, UPPER));
+}
+// wide: operands go to bf16 with their scales, 16 bytes at a time; each instruction takes 16 of k.
+template <typename S, int AF, int BF>
+__device__ __forceinline__ void multiply_wide(f32x16 (&acc)[S::TM][S::TN], const Operands<S>& o, const uint32_t (&as)[S::TM], const uint32_t (&bs)[S::TN]) {
+  const auto wide = [](bf16x8 (&to)[2], const u32x4& w, uint32_t scales, auto e5m2) {
+    const float s = __uint_as_float((scales & 255u) << 23);
+#pragma unroll
+    for (int v = 0; v < 2; ++v)
+      to[v] = __builtin_bit_cast(bf16x8, u32x4{widen<e5m2.value, false>(w[2 * v], s), widen<e5m2.value, true>(w[2 * v], s),
+                                               widen<e5m2.value, false>(w[2 * v + 1], s), widen<e5m2.value, true>(w[2 * v + 1], s)});
+  };
+#pragma unroll
+  for (int q = 0; q < 2; ++q) {
+    bf16x8 x[S::TN][2];
+#pragma unroll
+    for (int f = 0; f < S::TN; ++f) wide(x[f], o.x[f][q], bs[f], Const<BF>{});
+#pragma unroll
+    for (int i = 0; i < S::TM; ++i) {
+      bf16x8 y[2];
+      wide(y, o.y[i][q], as[i], Const<AF>{});
+#pragma unroll
+      for (int v = 0; v < 2; ++v)
+#pragma unroll
+        for (int j = 0; j < S::TN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[j][v], y[v], acc[i][j], 0, 0, 0);
+    }
+    if (q == 0) settle<S>(acc);  // one piece's operands at a time fit the registers
+  }
+}
+
+// Buffer loads from `base` on: a 32-bit offset per lane and one per wavefront, without address arithmetic.
+__device__ __forceinline__ uint32_t load_word(const uint8_t* base, uint32_t offset, uint32_t wave_offset) {
+  return __builtin_amdgcn_raw_buffer_load_b32(__builtin_amdgcn_make_buffer_rsrc((void*)base, 0, -1, 0x27000), (int)offset, (int)wave_offset, 0);
+}
+// ... of 16 bytes per lane, which go to lds + 16 * lane.
+__device__ __forceinline__ void load_to_lds(const uint8_t* base, uint32_t offset, uint32_t wave_offset, uint8_t* lds) {
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(__builtin_amdgcn_make_buffer_rsrc((void*)base, 0, -1, 0x27000), (__attribute__((address_space(3))) void*)lds, 16, (int)offset, (int)wave_offset, 0, 0);
+}
+// At most N of this wavefront's loads are in flight and none of its LDS reads; then a barrier.  (A barrier alone does not order memory
+// operations for the compiler, a fence would wait for all loads.)
+template <int N>
+__device__ __forceinline__ void wait_and_meet() {
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
+}
+
+__device__ __forceinline__ void reads_done_and_meet() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+__device__ __forceinline__ void meet() { asm volatile("s_barrier" ::: "memory"); }
+
+// N neighbours of c's row i from column j on.
+template <typename TC, int N>
+__device__ __forceinline__ void put(const Matmul& p, uint32_t i, uint32_t j, float (&f)[N]) {
+  if (i >= p.m || j >= p.n) return;
+  TC* to = static_cast<TC*>(p.c) + (uint64_t)i * p.ldc + j;
+  const uint32_t n = min((uint32_t)N, p.n - j);
+  Vec<TC, N> y = {};
+  if (p.accumulate) {
+    if (n == N) load<false>(y, to);
+    else load_end(y, to, n, 0.f);
+#pragma unroll
+    for (int r = 0; r < N; ++r) f[r] += y.get(r);
+  }
+  y.set(f);
+  if (n == N) store<false>(to, y);
+  else store_end(to, y, n);
 }
 
 template <typename S, int AF, int BF, bool WIDE, typename TC>
 __global__ __launch_bounds__(S::threads, 2) void k_matmul(const Matmul p, const Tiles t) {
-  __shared__ __align__(16) uint8_t stage[2][S::rows * 128];
-  const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, wm = wave / S::WN, wn = wave % S::WN;
-  uint32_t tile_m, tile_n, split;
-  tile_of(t, blockIdx.x, &tile_m, &tile_n, &split);
+  __shared__ __align__(16) uint8_t stage[S::lds];
+  constexpr uint32_t kStage = S::rows * 128;
+  const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave / S::WN, wn = wave % S::WN;
+  const uint32_t n_tiles = t.across * t.down, split = blockIdx.x / n_tiles;
+  uint32_t tile_m, tile_n;
+  tile_of(t, blockIdx.x - split * n_tiles, &tile_m, &tile_n);
   const uint32_t m0 = tile_m * S::rows_m, n0 = tile_n * S::rows_n;
   const uint32_t blocks = (p.k + 127u) / 128u, s_row = (uint32_t)scale_row_bytes(p.k), row = blocks * 128u;
   const uint32_t first = split * t.split_blocks, end = min(blocks, first + t.split_blocks);
   // what this thread stages: rows behind the last one are the last one again.  The eight pieces of 16 bytes of a row's block change
-  // places by the row, so that the lanes of a read of one piece from many rows spread over the LDS banks.
+  // places by half the row's number: a read of one piece from 16 rows (LDS serves 16 lanes of 16 bytes at once) then meets every
+  // bank once.
   const uint8_t *a0 = p.a + (uint64_t)m0 * row, *b0 = p.b + (uint64_t)n0 * row;
   const uint32_t last_m = p.m - 1u - m0, last_n = p.n - 1u - n0;
   uint32_t from[S::loads];
 #pragma unroll
   for (int j = 0; j < S::loads; ++j) {
     const uint32_t r = (j * S::waves + wave) * 8u + lane / 8u;
-    const uint32_t piece = ((lane & 7u) ^ (lane / 8u)) * 16u;
+    const uint32_t piece = ((lane & 7u) ^ (r >> 1 & 7u)) * 16u;
     from[j] = (j * S::waves * 8 < S::rows_m ? min(r, last_m) : min(r - S::rows_m, last_n)) * row + piece;
   }
-  const auto fetch = [&](uint32_t block, int buffer) {
+  const auto fetch = [&](uint32_t block, uint32_t at) {
 #pragma unroll
-    for (int j = 0; j < S::loads; ++j) {
-      const uint8_t* base = (j * S::waves * 8 < S::rows_m ? a0 : b0) + (uint64_t)block * 128u;
-      __builtin_amdgcn_global_load_lds((const LMT_GLOBAL void*)(base + from[j]), (__attribute__((address_space(3))) void*)(&stage[buffer][(j * S::waves + wave) * 1024]), 16, 0, 0);
-    }
+    for (int j = 0; j < S::loads; ++j)
+      load_to_lds(j * S::waves * 8 < S::rows_m ? a0 : b0, from[j], block * 128u, stage + at + (j * S::waves + wave) * 1024u);
   };
-  // what this lane reads: pieces 4 h + 2 (l / 32) + q
+  // what this lane reads: pieces 4 h + 2 (l / 32) + q of rows l % 32
   uint32_t at[2][2];
 #pragma unroll
   for (uint32_t h = 0; h < 2; ++h)
 #pragma unroll
-    for (uint32_t q = 0; q < 2; ++q) at[h][q] = (lane & 31u) * 128u + ((4u * h + 2u * (lane >> 5) + q) ^ (lane & 7u)) * 16u;
+    for (uint32_t q = 0; q < 2; ++q) at[h][q] = (lane & 31u) * 128u + ((4u * h + 2u * (lane >> 5) + q) ^ (lane >> 1 & 7u)) * 16u;
   const uint32_t a_at = wm * S::TM * 4096u, b_at = S::rows_m * 128u + wn * S::TN * 4096u;
   // scales of the lane's rows, four blocks at a time
   const uint8_t *as0 = p.a_scales + (uint64_t)m0 * s_row, *bs0 = p.b_scales + (uint64_t)n0 * s_row;
@@ -318,58 +357,184 @@ __global__ __launch_bounds__(S::threads, 2) void k_matmul(const Matmul p, const 
   uint32_t as[S::TM], bs[S::TN], as_next[S::TM], bs_next[S::TN];
   const auto scales = [&](uint32_t block) {
 #pragma unroll
-    for (int i = 0; i < S::TM; ++i) as_next[i] = *(const LMT_GLOBAL uint32_t*)(as0 + block + as_from[i]);
+    for (int i = 0; i < S::TM; ++i) as_next[i] = load_word(as0, as_from[i], block);
 #pragma unroll
-    for (int j = 0; j < S::TN; ++j) bs_next[j] = *(const LMT_GLOBAL uint32_t*)(bs0 + block + bs_from[j]);
+    for (int j = 0; j < S::TN; ++j) bs_next[j] = load_word(bs0, bs_from[j], block);
   };
   f32x16 acc[S::TM][S::TN] = {};
+  uint32_t now = 0;  // the stage that is multiplied
   if (first < end) {
     scales(first);
     fetch(first, 0);
+  }
+  Operands<S> o;
+  if constexpr (S::turns) {
+    wait_and_meet<0>();            // the first block has arrived
+    if (wave >= S::waves / 2) meet();  // the second group is one turn behind
   }
   for (uint32_t g = first; g < end; g += 4u) {
 #pragma unroll
     for (int i = 0; i < S::TM; ++i) as[i] = as_next[i];
 #pragma unroll
     for (int j = 0; j < S::TN; ++j) bs[j] = bs_next[j];
-    if (g + 4u < end) scales(g + 4u);
+    const uint32_t stop = min(g + 4u, end);
+    for (uint32_t block = g; block < stop; ++block) {
+      if constexpr (!S::turns) wait_and_meet<0>();  // the block has arrived, everybody's part of it, and nobody reads the other stage any more
+      if (block == g && stop < end) scales(stop);
+      // With turns: nobody reads the other stage, as everybody's reads of the block in front ended before a barrier that this group has
+      // passed, and the second half's turn below ends with what is fetched here in place, one turn before anyone reads it
+      if (block + 1u < end) fetch(block + 1u, kStage - now);
 #pragma unroll
-    for (int s = 0; s < 4; ++s) {
-      if (g + s >= end) break;
-      __syncthreads();  // block g + s is staged, and nobody reads the other buffer any more
-      if (g + s + 1u < end) fetch(g + s + 1u, (s + 1) & 1);
-      step<S, AF, BF, WIDE>(acc, &stage[s & 1][a_at], &stage[s & 1][b_at], at, as, bs, s);
-    }
-  }
-  float* part = t.splits > 1u ? p.workspace + ((uint64_t)blockIdx.x * S::threads + threadIdx.x) * 4u : nullptr;
-#pragma unroll
-  for (int i = 0; i < S::TM; ++i)
-#pragma unroll
-    for (int j = 0; j < S::TN; ++j)
-#pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        const f32x4 d = {acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]};
-        if (t.splits > 1u) {
-          *(LMT_GLOBAL f32x4*)(part + (uint64_t)((i * S::TN + j) * 4 + g) * gridDim.x * S::threads * 4u) = d;
-        } else {
-          put4<TC>(p, m0 + (wm * S::TM + i) * 32u + (lane & 31u), n0 + (wn * S::TN + j) * 32u + g * 8u + (lane >> 5) * 4u, d);
+      for (int h = 0; h < 2; ++h) {
+        o.read(stage + now + a_at, stage + now + b_at, at[h]);
+        if constexpr (S::turns) {
+          if (h == 0) reads_done_and_meet();
+          else wait_and_meet<0>();
+          __builtin_amdgcn_s_setprio(1);
+        }
+        if constexpr (WIDE) multiply_wide<S, AF, BF>(acc, o, as, bs);
+        else multiply_narrow<S, AF, BF>(acc, o, as, bs);
+        settle<S>(acc);
+        if constexpr (S::turns) {
+          __builtin_amdgcn_s_setprio(0);
+          meet();
         }
       }
+      now = kStage - now;
+#pragma unroll
+      for (int i = 0; i < S::TM; ++i) as[i] >>= 8;
+#pragma unroll
+      for (int j = 0; j < S::TN; ++j) bs[j] >>= 8;
+    }
+  }
+  if constexpr (S::turns) {
+    if (wave < S::waves / 2) meet();
+  }
+  if (t.splits > 1u) {  // this part's sums, in the order of the threads
+    float* part = p.workspace + ((uint64_t)blockIdx.x * S::threads + threadIdx.x) * 4u;
+#pragma unroll
+    for (int i = 0; i < S::TM; ++i)
+#pragma unroll
+      for (int j = 0; j < S::TN; ++j)
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+          *(LMT_GLOBAL f32x4*)(part + (uint64_t)((i * S::TN + j) * 4 + g) * gridDim.x * S::threads * 4u) =
+              f32x4{acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]};
+    return;
+  }
+  // 64 rows of 64 at a time through LDS, a wavefront in its own part of it, so that rows of c are written 128 bytes and more at a time
+  wait_and_meet<0>();
+  float* mine = reinterpret_cast<float*>(stage) + wave * (64 * 64);
+  constexpr int N = 16 / sizeof(TC);  // elements a lane writes
+#pragma unroll
+  for (int half = 0; half < S::TM / 2; ++half) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int j = 0; j < S::TN; ++j)
+#pragma unroll
+        for (uint32_t g = 0; g < 4; ++g) {
+          const f32x16& d = acc[2 * half + i][j];
+          const uint32_t r = i * 32u + (lane & 31u), piece = j * 8u + g * 2u + (lane >> 5);
+          *reinterpret_cast<f32x4*>(mine + r * 64u + (piece ^ (r & 15u)) * 4u) = f32x4{d[4 * g], d[4 * g + 1], d[4 * g + 2], d[4 * g + 3]};
+        }
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (uint32_t it = 0; it < 64u * 64u / (64u * N); ++it) {
+      const uint32_t e = it * 64u + lane, r = e / (64u / N), col = e % (64u / N) * N;
+      float f[N];
+#pragma unroll
+      for (uint32_t v = 0; v < N; v += 4) {
+        const f32x4 d = *reinterpret_cast<const f32x4*>(mine + r * 64u + ((col / 4u + v / 4u) ^ (r & 15u)) * 4u);
+        f[v] = d.x, f[v + 1] = d.y, f[v + 2] = d.z, f[v + 3] = d.w;
+      }
+      put<TC, N>(p, m0 + (wm * S::TM + 2 * half) * 32u + r, n0 + wn * 64u + col, f);
+    }
+    __builtin_amdgcn_wave_barrier();
+  }
 }
 
-// Adds the parts of k in order, one workgroup per tile and 4 x 64 x waves elements of it, in the layout of k_matmul's threads.
+// Adds the parts of k in order, one workgroup per tile and 4 x threads elements of it, in the layout of k_matmul's threads.
 template <typename S, typename TC>
 __global__ __launch_bounds__(S::threads) void k_matmul_join(const Matmul p, const Tiles t) {
   const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, wm = wave / S::WN, wn = wave % S::WN;
   const uint32_t n_tiles = t.across * t.down, piece = blockIdx.x / n_tiles, id = blockIdx.x % n_tiles;
-  uint32_t tile_m, tile_n, split;
-  tile_of(t, id, &tile_m, &tile_n, &split);
+  uint32_t tile_m, tile_n;
+  tile_of(t, id, &tile_m, &tile_n);
   const uint32_t i = piece / (S::TN * 4), j = piece / 4 % S::TN, g = piece % 4;
   const uint64_t split_size = (uint64_t)n_tiles * S::threads * 4u;
   const float* part = p.workspace + (uint64_t)piece * t.splits * split_size + ((uint64_t)id * S::threads + threadIdx.x) * 4u;
   f32x4 sum = *(const LMT_GLOBAL f32x4*)part;
+#pragma unroll 4
   for (uint32_t s = 1; s < t.splits; ++s) sum += *(const LMT_GLOBAL f32x4*)(part + s * split_size);
-  put4<TC>(p, tile_m * S::rows_m + (wm * S::TM + i) * 32u + (lane & 31u), tile_n * S::rows_n + (wn * S::TN + j) * 32u + g * 8u + (lane >> 5) * 4u, sum);
+  float f[4] = {sum.x, sum.y, sum.z, sum.w};
+  put<TC, 4>(p, tile_m * S::rows_m + (wm * S::TM + i) * 32u + (lane & 31u), tile_n * S::rows_n + (wn * S::TN + j) * 32u + g * 8u + (lane >> 5) * 4u, f);
+}
+
+// Few rows of a (up to 64) and a short k: what counts is how soon the last byte has arrived.  A workgroup has 16 rows of b, its eight
+// wavefronts every eighth block of k, operands straight from memory to registers (16 rows of 128 bytes to an instruction, whole
+// lines), all in flight at once; the eight sums meet in LDS.  37 x 1 024 x 1 024: 5.2 us, by tiles of 128 x 128 7.4.
+constexpr uint32_t kFewRows = 64, kFewWaves = 8;
+struct Lane {  // 32 bytes of a row's block, the lane's share of it
+  u32x4 w[2];
+  uint32_t scale;
+  __device__ __forceinline__ void read(const uint8_t* from, const uint8_t* scales, uint32_t block) {
+    const LMT_GLOBAL u32x4* g = (const LMT_GLOBAL u32x4*)(from + (uint64_t)block * 128u);
+    w[0] = g[0], w[1] = g[1];
+    scale = *(const LMT_GLOBAL uint8_t*)(scales + block);
+  }
+  __device__ __forceinline__ i32x8 whole() const {
+    return i32x8{(int)w[0].x, (int)w[0].y, (int)w[0].z, (int)w[0].w, (int)w[1].x, (int)w[1].y, (int)w[1].z, (int)w[1].w};
+  }
+  template <int E5M2>
+  __device__ __forceinline__ bf16x8 wide(int q) const {  // bytes 8 q .. 8 q + 7
+    const float s = __uint_as_float(scale << 23);
+    const uint32_t lo = w[q / 2][2 * (q % 2)], hi = w[q / 2][2 * (q % 2) + 1];
+    return __builtin_bit_cast(bf16x8, u32x4{widen<E5M2, false>(lo, s), widen<E5M2, true>(lo, s), widen<E5M2, false>(hi, s), widen<E5M2, true>(hi, s)});
+  }
+};
+template <int AF, int BF, typename TC>
+__global__ __launch_bounds__(64 * kFewWaves) void k_matmul_few(const Matmul p) {
+  constexpr bool WIDE = sizeof(TC) == 4;
+  __shared__ f32x4 part[kFewWaves][4][64];
+  const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15u;
+  const uint32_t n0 = blockIdx.x * 16u, blocks = (p.k + 127u) / 128u, s_row = (uint32_t)scale_row_bytes(p.k);
+  const uint64_t row = (uint64_t)blocks * 128u;
+  const uint8_t *a[4], *as[4];
+#pragma unroll
+  for (uint32_t f = 0; f < 4; ++f) {
+    const uint32_t i = min(f * 16u + r, p.m - 1u);
+    a[f] = p.a + i * row + (lane >> 4) * 32u, as[f] = p.a_scales + (uint64_t)i * s_row;
+  }
+  const uint32_t of_b = min(n0 + r, p.n - 1u);
+  const uint8_t *b = p.b + of_b * row + (lane >> 4) * 32u, *bs = p.b_scales + (uint64_t)of_b * s_row;
+  f32x4 acc[4] = {};
+  for (uint32_t block = wave; block < blocks; block += kFewWaves) {
+    Lane x, y[4];
+    x.read(b, bs, block);
+#pragma unroll
+    for (uint32_t f = 0; f < 4; ++f)
+      if (f * 16u < p.m) y[f].read(a[f], as[f], block);
+#pragma unroll
+    for (uint32_t f = 0; f < 4; ++f) {
+      if (f * 16u >= p.m) continue;
+      if constexpr (WIDE) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) acc[f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x.template wide<BF>(q), y[f].template wide<AF>(q), acc[f], 0, 0, 0);
+      } else {
+        acc[f] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x.whole(), y[f].whole(), acc[f], BF, AF, 0, (int)x.scale, 0, (int)y[f].scale);
+      }
+    }
+  }
+#pragma unroll
+  for (int f = 0; f < 4; ++f) part[wave][f][lane] = acc[f];
+  __syncthreads();
+  if (wave >= 4u) return;  // a wavefront per square of 16 x 16
+  f32x4 sum = part[0][wave][lane];
+#pragma unroll
+  for (uint32_t w = 1; w < kFewWaves; ++w) sum += part[w][wave][lane];
+  float f[4] = {sum.x, sum.y, sum.z, sum.w};
+  put<TC, 4>(p, wave * 16u + r, n0 + (lane >> 4) * 4u, f);  // lane l has rows l % 16 of a and four neighbours, from 4 (l / 16) on, of b
 }
 
 template <typename F>
@@ -407,22 +572,29 @@ typedef Shape<2, 4, 4, 2> Large;   // 256 x 256
 typedef Shape<2, 2, 2, 2> Medium;  // 128 x 128
 
 struct Choice {
-  bool large;
+  enum { kFew, kMedium, kLarge } form;
   Tiles tiles;
 };
 template <typename S>
-Tiles tiles_of(uint64_t m, uint64_t n, uint64_t k, uint32_t splits) {
-  const uint64_t blocks = ceil_div(k, 128);
-  const uint64_t per = std::max<uint64_t>(4, round_up(ceil_div(blocks, splits), 4));
+Tiles tiles_of(uint64_t m, uint64_t n, uint64_t k, uint64_t splits) {
+  const uint64_t blocks = ceil_div(k, 128), per = std::max<uint64_t>(4, round_up(ceil_div(blocks, splits), 4));  // scales come four at a time
   return {(uint32_t)ceil_div(n, S::rows_n), (uint32_t)ceil_div(m, S::rows_m), (uint32_t)std::max<uint64_t>(1, ceil_div(blocks, per)), (uint32_t)per};
 }
+// us with bf16 results, the chosen form first.
+//   Few rows: while a workgroup's wavefronts have few loads each.  37 x 1 024 x 1 024: 5.2 (medium 7.4), 1 x 1 024 x 4 096: 5.5 (9.3);
+//   beyond, 37 x 1 024 x 4 096: medium 9.7 (11.2), 64 x 30 522 x 1 024: 9.4 (16.7).
+//   Large tiles, one workgroup per compute unit, take 5/3 of the time of a round of medium ones, of which there are two per unit:
+//   4 096 x 4 096 x 4 096: large 62 (73), 6 144 x 4 096 x 1 024: medium 34 (39), 2 048 x 4 096 x 1 024: medium 14 (19).
+//   Too few tiles: parts of k, of 1 024 at least, up to a workgroup per unit.  1 024 x 1 024 x 4 096: 17 (in one part 24).  With a long k
+//   large tiles are worth the more parts: 4 096 x 1 024 x 32 768 in fp32 226 (medium 252); at 8 192 medium 68 (79).
 Choice choose(uint64_t m, uint64_t n, uint64_t k) {
+  const uint64_t blocks = ceil_div(k, 128);
+  if (m <= kFewRows && n <= 4096 && ceil_div(m, 16) * blocks <= 32) return {Choice::kFew, {}};
   const uint64_t large = ceil_div(m, Large::rows_m) * ceil_div(n, Large::rows_n);
   const uint64_t medium = ceil_div(m, Medium::rows_m) * ceil_div(n, Medium::rows_n);
-  if (large >= kCus) return {true, tiles_of<Large>(m, n, k, 1)};
-  const uint64_t splits = std::min<uint64_t>(std::max<uint64_t>(1, kCus / large), std::max<uint64_t>(1, k / 2048));
-  if (large * splits >= 128) return {true, tiles_of<Large>(m, n, k, (uint32_t)splits)};
-  return {false, tiles_of<Medium>(m, n, k, (uint32_t)std::min<uint64_t>(std::max<uint64_t>(1, kCus / medium), std::max<uint64_t>(1, k / 1024)))};
+  if (medium > 2 * kCus && 5 * ceil_div(large, kCus) <= 3 * ceil_div(medium, 2 * kCus)) return {Choice::kLarge, tiles_of<Large>(m, n, k, 1)};
+  if (large <= kCus && k >= 16384 && large * (k / 4096) >= kCus) return {Choice::kLarge, tiles_of<Large>(m, n, k, kCus / large)};
+  return {Choice::kMedium, tiles_of<Medium>(m, n, k, std::max<uint64_t>(1, std::min<uint64_t>(kCus / medium, k / 1024)))};
 }
 
 }  // namespace
@@ -430,13 +602,13 @@ Choice choose(uint64_t m, uint64_t n, uint64_t k) {
 uint64_t matmul_workspace(uint64_t m, uint64_t n, uint64_t k) {
   if (m == 0 || n == 0) return 0;
   const Choice c = choose(m, n, k);
-  const uint64_t tile = c.large ? Large::rows_m * Large::rows_n : Medium::rows_m * Medium::rows_n;
+  const uint64_t tile = c.form == Choice::kLarge ? Large::rows_m * Large::rows_n : Medium::rows_m * Medium::rows_n;
   return c.tiles.splits > 1 ? 4 * tile * c.tiles.splits * c.tiles.across * c.tiles.down : 0;
 }
 
 hipError_t launch_matmul(const Matmul& p, int a_fp8, int b_fp8, int c_dtype, hipStream_t s) {
   const Choice c = choose(p.m, p.n, p.k);
-  const auto go = [&](auto shape, auto af, auto bf, auto tc) {
+  const auto tiled = [&](auto shape, auto af, auto bf, auto tc) {
     typedef decltype(shape) S;
     typedef decltype(tc) TC;
     const uint32_t n_tiles = c.tiles.across * c.tiles.down;
@@ -447,7 +619,15 @@ hipError_t launch_matmul(const Matmul& p, int a_fp8, int b_fp8, int c_dtype, hip
   };
   return with_fp8(a_fp8, [&](auto af) {
     return with_fp8(b_fp8, [&](auto bf) {
-      return with_float(c_dtype, [&](auto tc) { return c.large ? go(Large{}, af, bf, tc) : go(Medium{}, af, bf, tc); });
+      return with_float(c_dtype, [&](auto tc) {
+        switch (c.form) {
+          case Choice::kFew:
+            hipLaunchKernelGGL((k_matmul_few<decltype(af)::value, decltype(bf)::value, decltype(tc)>), dim3((uint32_t)ceil_div(p.n, 16)), dim3(64 * kFewWaves), 0, s, p);
+            return hipGetLastError();
+          case Choice::kMedium: return tiled(Medium{}, af, bf, tc);
+          default: return tiled(Large{}, af, bf, tc);
+        }
+      });
     });
   });
 }
