@@ -9,12 +9,19 @@
 namespace lmt {
 namespace {
 
-constexpr uint32_t kThreads = 256;
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 template <int N>
 struct Const {
   static constexpr int value = N;
 };
+
+// Of a list of n items: the one for workgroup `id`.  XCD x, which takes every eighth workgroup, gets an eighth of the list, so that its
+// L2 sees neighbours.
+__device__ __forceinline__ uint64_t neighbours(uint64_t id, uint64_t n) {
+  constexpr uint32_t kXcds = 8;
+  const uint64_t x = id % kXcds, share = n / kXcds, extra = n % kXcds;
+  return x * share + min(x, extra) + id / kXcds;
+}
 
 // ---- quantisation ---------------------------------------------------------------------
 
@@ -58,74 +65,75 @@ __device__ __forceinline__ uint32_t max16(uint32_t x) {
   return x;
 }
 
-// A workgroup takes squares of 128 x 128; a thread 8 rows of 8 columns, which it reads once for both results.
+// A workgroup takes squares of 128 x 128; a thread 4 rows of 8 columns, which it reads once for both results.  Bound by memory: 30 522 x
+// 1 024 in fp32, both sides, 38 us (4.9 TB/s); 8 192 x 1 024 in bf16 11.6 (8 rows to a thread of half as many 12.5: two workgroups
+// a compute unit, with less in flight).
+constexpr uint32_t kQuantizeThreads = 512;
 template <typename T, bool E5M2, bool TILE>
-__global__ __launch_bounds__(kThreads) void k_quantize(const Quantize p, uint32_t tiles_across, uint32_t tiles_down) {
-  __shared__ uint32_t col_max[4][128];
+__global__ __launch_bounds__(kQuantizeThreads, 4) void k_quantize(const Quantize p, uint32_t tiles_across, uint32_t tiles_down) {
+  __shared__ __align__(16) uint32_t col_max[128];  // TILE: the first is the square's
   __shared__ __align__(16) uint8_t turned[128 * 128];
-  const uint32_t cg = threadIdx.x & 15u, rg = threadIdx.x >> 4, wave = threadIdx.x >> 6;
+  const uint32_t cg = threadIdx.x & 15u, rg = threadIdx.x >> 4;
   const uint64_t q_row = round_up(p.cols, 128), s_row = 4 * ceil_div(p.cols, 512), qt_row = round_up(p.rows, 128), st_row = 4 * ceil_div(p.rows, 512);
   const uint64_t n_tiles = (uint64_t)tiles_across * tiles_down;
-  for (uint64_t tile = blockIdx.x; tile < n_tiles; tile += gridDim.x) {
+  for (uint64_t at = blockIdx.x; at < n_tiles; at += gridDim.x) {
+    const uint64_t tile = neighbours(at, n_tiles);  // a line of scales holds several squares': one L2 puts it together
     const uint32_t tr = (uint32_t)(tile / tiles_across), tc = (uint32_t)(tile % tiles_across);
-    const uint32_t r0 = tr * 128u + rg * 8u, c0 = tc * 128u + cg * 8u;
+    const uint32_t r0 = tr * 128u + rg * 4u, c0 = tc * 128u + cg * 8u;
     const uint32_t n = c0 < p.cols ? min(8u, p.cols - c0) : 0u;
-    Vec<T, 8> x[8];
+    Vec<T, 8> x[4];
 #pragma unroll
-    for (uint32_t j = 0; j < 8; ++j) {
+    for (uint32_t j = 0; j < 4; ++j) {
       x[j] = {};
-      if (r0 + j < p.rows && n != 0) {
-        const T* from = static_cast<const T*>(p.x) + (uint64_t)(r0 + j) * p.ld + c0;
-        if (n == 8) load<false>(x[j], from);
-        else load_end(x[j], from, n, 0.f);
-      }
+      if (r0 + j < p.rows && n == 8) load<true>(x[j], static_cast<const T*>(p.x) + (uint64_t)(r0 + j) * p.ld + c0);
     }
-    uint32_t row_max[8], cm[8] = {};
+    if (n != 0 && n != 8) {  // the end of a row
 #pragma unroll
-    for (uint32_t j = 0; j < 8; ++j) {
-      row_max[j] = 0;
+      for (uint32_t j = 0; j < 4; ++j)
+        if (r0 + j < p.rows) load_end(x[j], static_cast<const T*>(p.x) + (uint64_t)(r0 + j) * p.ld + c0, n, 0.f);
+    }
+    if (threadIdx.x < 128u) col_max[threadIdx.x] = 0;
+    __syncthreads();
+    uint32_t row_max[4] = {}, cm[8] = {};
+#pragma unroll
+    for (uint32_t j = 0; j < 4; ++j)
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const uint32_t m = magnitude(x[j].get(i));
         row_max[j] = max(row_max[j], m);
         cm[i] = max(cm[i], m);
       }
-    }
-    uint32_t row_scale[8], col_scale[8];
+    uint32_t row_scale[4], col_scale[8];
     if constexpr (TILE) {
-      uint32_t m = 0;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) m = max(m, cm[i]);
+      uint32_t m = max(max(row_max[0], row_max[1]), max(row_max[2], row_max[3]));
       m = max16(m);
       m = max(m, (uint32_t)__shfl_xor((int)m, 16));
       m = max(m, (uint32_t)__shfl_xor((int)m, 32));
-      if ((threadIdx.x & 63u) == 0) col_max[wave][0] = m;
+      if ((threadIdx.x & 63u) == 0) atomicMax(&col_max[0], m);
       __syncthreads();
-      m = max(max(col_max[0][0], col_max[1][0]), max(col_max[2][0], col_max[3][0]));
-      const uint32_t s = scale_of<E5M2>(m);
+      const uint32_t s = scale_of<E5M2>(col_max[0]);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) row_scale[i] = col_scale[i] = s;
+      for (int i = 0; i < 4; ++i) row_scale[i] = s;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) col_scale[i] = s;
     } else {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) row_scale[j] = scale_of<E5M2>(max16(row_max[j]));
+      for (int j = 0; j < 4; ++j) row_scale[j] = scale_of<E5M2>(max16(row_max[j]));
       if (p.qt) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           uint32_t m = max(cm[i], (uint32_t)__shfl_xor((int)cm[i], 16));
           m = max(m, (uint32_t)__shfl_xor((int)m, 32));
-          if ((threadIdx.x & 48u) == 0) col_max[wave][cg * 8u + i] = m;
+          if ((threadIdx.x & 48u) == 0) atomicMax(&col_max[cg * 8u + i], m);
         }
         __syncthreads();
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const uint32_t c = cg * 8u + i;
-          col_scale[i] = scale_of<E5M2>(max(max(col_max[0][c], col_max[1][c]), max(col_max[2][c], col_max[3][c])));
-        }
+        for (int i = 0; i < 8; ++i) col_scale[i] = scale_of<E5M2>(col_max[cg * 8u + i]);
       }
     }
     if (p.q) {
 #pragma unroll
-      for (uint32_t j = 0; j < 8; ++j) {
+      for (uint32_t j = 0; j < 4; ++j) {
         if (r0 + j >= p.rows) break;
         const float by = inverse_of(row_scale[j]);
         const float lo[4] = {x[j].get(0), x[j].get(1), x[j].get(2), x[j].get(3)}, hi[4] = {x[j].get(4), x[j].get(5), x[j].get(6), x[j].get(7)};
@@ -142,11 +150,9 @@ __global__ __launch_bounds__(kThreads) void k_quantize(const Quantize p, uint32_
     if (p.qt) {
 #pragma unroll
       for (uint32_t i = 0; i < 8; ++i) {
-        const float by = inverse_of(col_scale[i]);
-        const float lo[4] = {x[0].get(i), x[1].get(i), x[2].get(i), x[3].get(i)}, hi[4] = {x[4].get(i), x[5].get(i), x[6].get(i), x[7].get(i)};
-        const u32x2 w = {pack4<E5M2>(lo, by), pack4<E5M2>(hi, by)};
+        const float col[4] = {x[0].get(i), x[1].get(i), x[2].get(i), x[3].get(i)};
         // 16-byte pieces of a column's 128 bytes change places by the column's eight, so that they spread over the LDS banks
-        *reinterpret_cast<u32x2*>(&turned[(cg * 8u + i) * 128u + ((rg / 2u) ^ (cg & 7u)) * 16u + (rg & 1u) * 8u]) = w;
+        *reinterpret_cast<uint32_t*>(&turned[(cg * 8u + i) * 128u + ((rg / 4u) ^ (cg & 7u)) * 16u + (rg & 3u) * 4u]) = pack4<E5M2>(col, inverse_of(col_scale[i]));
         const uint32_t c = c0 + i;
         if (rg == 0 && c < p.cols) {
           uint8_t* s = p.scales_t + (uint64_t)c * st_row;
@@ -157,8 +163,8 @@ __global__ __launch_bounds__(kThreads) void k_quantize(const Quantize p, uint32_
       }
       __syncthreads();
 #pragma unroll
-      for (uint32_t k = 0; k < 4; ++k) {
-        const uint32_t c = k * 32u + threadIdx.x / 8u, piece = threadIdx.x & 7u;
+      for (uint32_t k = 0; k < 2; ++k) {
+        const uint32_t c = k * 64u + threadIdx.x / 8u, piece = threadIdx.x & 7u;
         if (tc * 128u + c < p.cols)
           *(LMT_GLOBAL u32x4*)(p.qt + (uint64_t)(tc * 128u + c) * qt_row + (uint64_t)tr * 128u + piece * 16u) =
               *reinterpret_cast<const u32x4*>(&turned[c * 128u + (piece ^ (c / 8u & 7u)) * 16u]);
@@ -189,15 +195,14 @@ struct Shape {
   static_assert(TN == 2 && TM % 2 == 0 && lds >= waves * 64 * 64 * 4, "results go out by squares of 64 x 64");
 };
 
-// Which tile a workgroup has: XCD x, which takes every eighth workgroup, has an eighth of the list of tiles, so that its L2 sees neighbours;
-// the list goes down kGroup tiles of m, then across n, so that both operands of the tiles in flight are few.
+// Which tile a workgroup has: a list of tiles that goes down kGroup tiles of m, then across n, so that both operands of the tiles in
+// flight on an XCD are few.
 struct Tiles {
   uint32_t across, down, splits, split_blocks;  // of c in n and m; parts of k, and blocks of 128 in each
 };
-constexpr uint32_t kXcds = 8, kGroup = 8;
+constexpr uint32_t kGroup = 8;
 __device__ __forceinline__ void tile_of(const Tiles& t, uint32_t id, uint32_t* tm, uint32_t* tn) {
-  const uint32_t n = t.across * t.down, x = id % kXcds, share = n / kXcds, extra = n % kXcds;
-  id = x * share + min(x, extra) + id / kXcds;
+  id = (uint32_t)neighbours(id, t.across * t.down);
   const uint32_t group = id / (kGroup * t.across), tall = min(kGroup, t.down - group * kGroup), in_group = id - group * kGroup * t.across;
   *tm = group * kGroup + in_group % tall, *tn = in_group / tall;
 }
@@ -559,8 +564,8 @@ hipError_t launch_quantize(const Quantize& p, int dtype, int fp8, bool tile, hip
     return with_fp8(fp8, [&](auto f) {
       typedef decltype(t) T;
       constexpr bool E5M2 = decltype(f)::value == 1;
-      if (tile) hipLaunchKernelGGL((k_quantize<T, E5M2, true>), dim3(grid), dim3(kThreads), 0, s, p, across, down);
-      else hipLaunchKernelGGL((k_quantize<T, E5M2, false>), dim3(grid), dim3(kThreads), 0, s, p, across, down);
+      if (tile) hipLaunchKernelGGL((k_quantize<T, E5M2, true>), dim3(grid), dim3(kQuantizeThreads), 0, s, p, across, down);
+      else hipLaunchKernelGGL((k_quantize<T, E5M2, false>), dim3(grid), dim3(kQuantizeThreads), 0, s, p, across, down);
       return hipGetLastError();
     });
   });
@@ -589,6 +594,7 @@ Tiles tiles_of(uint64_t m, uint64_t n, uint64_t k, uint64_t splits) {
 //   large tiles are worth the more parts: 4 096 x 1 024 x 32 768 in fp32 226 (medium 252); at 8 192 medium 68 (79).
 Choice choose(uint64_t m, uint64_t n, uint64_t k) {
   const uint64_t blocks = ceil_div(k, 128);
+  k = 128 * blocks;  // what the operands hold: the same form, and workspace, for any k of so many blocks
   if (m <= kFewRows && n <= 4096 && ceil_div(m, 16) * blocks <= 32) return {Choice::kFew, {}};
   const uint64_t large = ceil_div(m, Large::rows_m) * ceil_div(n, Large::rows_n);
   const uint64_t medium = ceil_div(m, Medium::rows_m) * ceil_div(n, Medium::rows_n);

@@ -98,6 +98,13 @@ def test_calls_with_nothing_to_do_succeed():
     assert lmt.fp8_shapes(3, 0) == ((3, 0), (3, 0)) and lmt.fp8_shapes(3, 1) == ((3, 128), (3, 4)) and lmt.fp8_shapes(2, 513) == ((2, 640), (2, 8))
 
 
+def test_the_workspace_of_a_product_is_that_of_its_operands_blocks():
+    """Operands do not say how much of their last block is padding."""
+    for m, n in ((1, 64), (37, 1024), (65, 300), (300, 1000), (2432, 30522), (4096, 1024)):
+        for k in (1, 100, 128, 129, 1000, 1023, 1025, 4000, 4095, 5000, 16380, 32700):
+            assert lmt.matmul_workspace(m, n, k) == lmt.matmul_workspace(m, n, -(-k // 128) * 128), (m, n, k)
+
+
 # ---- the extension module ---------------------------------------------------------------
 
 
