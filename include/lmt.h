@@ -57,7 +57,7 @@ extern "C" {
 #define LMT_ACCUMULATE 1u  /* add to what the output holds                                           */
 #define LMT_TILE_SCALES 2u /* lmt_quantize: one scale for a square of 128 x 128 instead of 128 x 1     */
 
-#define LMT_MAX_ROWS 0x7fffffffu  /* tokens, vocabulary, rows, classes, m, n                     */
+#define LMT_MAX_ROWS 0x7fffff00u  /* tokens, vocabulary, rows, classes, m, n                     */
 #define LMT_MAX_WIDTH 0x7fffffu   /* row length of tables and of 8-bit matrices, k                 */
 
 /* out[t][j] = scale * table[token[t]][j] for t < n_tokens, j < width, rounded once to out's type.
@@ -89,7 +89,7 @@ uint64_t lmt_scale_row_bytes(uint64_t cols);
 
 /* x (fp32, fp16 or bf16, [rows][ld]) in 8 bits: q and scales, and / or its transpose, qt and scales_t (a matrix of `cols`
  * rows of `rows` elements, with blocks along its own rows).  Either pair may be NULL.  A block's scale is the smallest
- * power of two, at least 2^-126, that brings its largest finite magnitude to fp8's largest value or below (1 block of
+ * power of two, at least 2^-126, that brings its largest finite magnitude to fp8's largest value or below (a block of
  * zeros: 2^-126); with LMT_TILE_SCALES the block is the square of 128 x 128 that the element lies in, so that the
  * transpose holds the same values.  Elements are rounded to the nearest value, ties to even; infinities and NaN become NaN
  * and take no part in the scale.  fp8: LMT_E4M3 or LMT_E5M2. */
@@ -98,9 +98,12 @@ int lmt_quantize(const void* x /*DEVICE*/, int dtype, uint64_t rows, uint64_t co
                  void* stream);
 
 /* c[i][j] = (old c[i][j], with LMT_ACCUMULATE) + sum over l < k of a[i][l] * b[j][l], for i < m, j < n, both operands in the
- * 8-bit form above with rows of k elements (each LMT_E4M3 or LMT_E5M2); c: fp32, fp16 or bf16, [m][ldc].  Products
- * are exact, sums in fp32 on the matrix cores, rounded once.  scales are 4-byte aligned.  workspace: as above, at
- * least lmt_matmul_workspace bytes; may be NULL where that is 0.
+ * 8-bit form above with rows of k elements (each LMT_E4M3 or LMT_E5M2); c: fp32, fp16 or bf16, [m][ldc].  Products and sums are
+ * made by the matrix cores in fp32 and rounded once to c's type.  A 16-bit c takes the 8-bit instructions, which line up the products of a
+ * few neighbours before they add them: of terms that are much smaller than their neighbours the last bits are lost (about 1.5e-5
+ * of the 2-norm of a result of random numbers, a hundredth of bf16's rounding); an fp32 c takes bf16 ones, at a third to half of the rate, and
+ * keeps 1e-7.  a_scales and b_scales are 4-byte aligned and between 1 and 254.  workspace: as above, at least
+ * lmt_matmul_workspace bytes; may be NULL where that is 0.
  * With x [T][H] and a weight w [V][H]: logits = x w^T are matmul(q(x), q(w)); the input's gradient dy w is
  * matmul(q(dy), qt(w)); the weight's dy^T x is matmul(qt(dy), qt(x)). */
 uint64_t lmt_matmul_workspace(uint64_t m, uint64_t n, uint64_t k);

@@ -124,7 +124,7 @@ int lmt_cross_entropy(const void* logits, int dtype, uint64_t rows, uint64_t cla
   if (!logits || !targets) return fail(LMT_ERR_NULL, "logits or targets is NULL");
   if (off(logits, size_of(dtype)) || off(grad, size_of(dtype)) || off(targets, size_of(target_dtype)) || off(weights, 4) || off(loss, 4) || off(lse, 4) || off(status, 4))
     return fail(LMT_ERR_ALIGN, "a pointer is not aligned to its element size");
-  const lmt::CrossEntropy p{logits, targets, weights, loss, lse, grad, ld, grad_ld, (uint32_t)rows, (uint32_t)classes, ignore, status};
+  const lmt::CrossEntropy p{logits, targets, weights, loss, lse, grad, ld, grad_ld, (uint32_t)rows, (uint32_t)classes, 0, ignore, status};
   return launched("launching the loss", lmt::launch_cross_entropy(p, dtype, target_dtype, (hipStream_t)stream));
 }
 

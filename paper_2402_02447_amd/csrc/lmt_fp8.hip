@@ -559,7 +559,7 @@ hipError_t with_fp8(int fp8, F f) {
 
 hipError_t launch_quantize(const Quantize& p, int dtype, int fp8, bool tile, hipStream_t s) {
   const uint32_t across = (uint32_t)ceil_div(p.cols, 128), down = (uint32_t)ceil_div(p.rows, 128);
-  const uint32_t grid = (uint32_t)std::min<uint64_t>((uint64_t)across * down, 1u << 23);
+  const uint32_t grid = (uint32_t)std::min<uint64_t>((uint64_t)across * down, 1u << 22);
   return with_float(dtype, [&](auto t) {
     return with_fp8(fp8, [&](auto f) {
       typedef decltype(t) T;

@@ -67,7 +67,7 @@ struct CrossEntropy {
   float *loss, *lse;
   void* grad;
   uint64_t ld, grad_ld;
-  uint32_t rows, classes;
+  uint32_t rows, classes, first;  // first: the launch's first row
   int64_t ignore;
   int32_t* status;
 };

@@ -2,8 +2,8 @@
 //
 // lse = top + log(sum of exp(x - top)), loss = w (lse - x[target]), grad = w (exp(x - top) / sum - [j = target]).  Bound by memory: a row
 // is read once, kept in registers while its maximum and then its sum are found, and the gradient is written from there
-// (3 sweeps over memory, the last two from cache, took 1.6 times as long at 16 384 x 30 522 in bf16).  Rows longer than
-// the registers of a workgroup are read twice, with a running maximum and sum the first time.
+// (3 sweeps over memory, the last two from cache: 562 us at 16 384 x 30 522 in bf16, this 330 to 370, 5.5 to 6.1 TB/s).  Rows longer
+// than the registers of a workgroup are read twice, with a running maximum and sum the first time.
 #include "lmt_device.h"
 #include "lmt_internal.h"
 
@@ -61,7 +61,7 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void k_cross_entropy
   constexpr uint32_t kLowest = sizeof(T) == 4 ? 0xff800000u : __is_same(T, _Float16) ? 0xfc00fc00u : 0xff80ff80u;  // -Inf
   __shared__ float red[2][kRowWaves], goal;
   const uint32_t me = threadIdx.x % THREADS, wave = me >> 6;
-  const uint64_t row = THREADS < 256 ? (uint64_t)blockIdx.x * (256 / THREADS) + threadIdx.x / THREADS : blockIdx.x;
+  const uint64_t row = p.first + (THREADS < 256 ? (uint64_t)blockIdx.x * (256 / THREADS) + threadIdx.x / THREADS : blockIdx.x);
   if (row >= p.rows) return;
   const Row r = row_of<I>(p, row, me == 0);
   const bool read = r.there || p.lse;  // else nothing of the row counts
@@ -139,7 +139,7 @@ __global__ __launch_bounds__(kLongThreads) void k_cross_entropy_long(const Cross
   constexpr int V = 16 / sizeof(T);
   __shared__ float red[2][kLongWaves], goal;
   const uint32_t me = threadIdx.x;
-  const uint64_t row = blockIdx.x;
+  const uint64_t row = (uint64_t)p.first + blockIdx.x;
   const Row r = row_of<I>(p, row, me == 0);
   const T* x = static_cast<const T*>(p.logits) + row * p.ld;
   const uint32_t whole = p.classes / V, left = p.classes - whole * V;
@@ -213,19 +213,25 @@ hipError_t launch_cross_entropy(const CrossEntropy& p, int dtype, int target_dty
     typedef decltype(t) T;
     typedef decltype(id) I;
     const uint32_t whole = p.classes / (16 / sizeof(T));  // vectors of a row
-    const auto launch = [&](void (*kernel)(const CrossEntropy), uint64_t grid, int threads) {
-      hipLaunchKernelGGL(kernel, dim3((uint32_t)grid), dim3(threads), 0, s, p);
-      return hipGetLastError();
+    const auto launch = [&](void (*kernel)(const CrossEntropy), uint32_t rows_each, int threads) {
+      constexpr uint64_t kMost = 1u << 21;  // workgroups to a launch: 32 bits count the threads of one
+      CrossEntropy part = p;
+      for (uint64_t first = 0; first < p.rows; first += kMost * rows_each) {
+        part.first = (uint32_t)first;
+        hipLaunchKernelGGL(kernel, dim3((uint32_t)std::min(kMost, ceil_div(p.rows - first, rows_each))), dim3(threads), 0, s, part);
+        if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+      }
+      return hipSuccess;
     };
     // the fewest threads that hold a row in a few vectors each
-    if (whole <= 64 * 2) return launch(k_cross_entropy<T, I, 64, 2>, ceil_div(p.rows, 4), 256);
-    if (whole <= 256 * 2) return launch(k_cross_entropy<T, I, 256, 2>, p.rows, 256);
-    if (whole <= 256 * 4) return launch(k_cross_entropy<T, I, 256, 4>, p.rows, 256);
-    if (whole <= 512 * 4) return launch(k_cross_entropy<T, I, 512, 4>, p.rows, 512);
-    if (whole <= 512 * 8) return launch(k_cross_entropy<T, I, 512, 8>, p.rows, 512);
-    if (whole <= 1024 * 8) return launch(k_cross_entropy<T, I, 1024, 8>, p.rows, 1024);
-    if (whole <= 1024 * 16) return launch(k_cross_entropy<T, I, 1024, 16>, p.rows, 1024);
-    return launch(k_cross_entropy_long<T, I>, p.rows, kLongThreads);
+    if (whole <= 64 * 2) return launch(k_cross_entropy<T, I, 64, 2>, 4, 256);
+    if (whole <= 256 * 2) return launch(k_cross_entropy<T, I, 256, 2>, 1, 256);
+    if (whole <= 256 * 4) return launch(k_cross_entropy<T, I, 256, 4>, 1, 256);
+    if (whole <= 512 * 4) return launch(k_cross_entropy<T, I, 512, 4>, 1, 512);
+    if (whole <= 512 * 8) return launch(k_cross_entropy<T, I, 512, 8>, 1, 512);
+    if (whole <= 1024 * 8) return launch(k_cross_entropy<T, I, 1024, 8>, 1, 1024);
+    if (whole <= 1024 * 16) return launch(k_cross_entropy<T, I, 1024, 16>, 1, 1024);
+    return launch(k_cross_entropy_long<T, I>, 1, kLongThreads);
   };
   const auto with = [&](auto id) { return dtype == LMT_F32 ? go(float{}, id) : dtype == LMT_F16 ? go(_Float16{}, id) : go(bf16_t{}, id); };
   return target_dtype == LMT_I64 ? with(int64_t{}) : with(int32_t{});

@@ -15,7 +15,7 @@ from .binding import load_library
 LMT_F32, LMT_F16, LMT_BF16, LMT_E4M3, LMT_E5M2, LMT_I32, LMT_I64 = range(7)
 LMT_STATUS_BAD_TOKEN, LMT_STATUS_BAD_TARGET = 1, 2
 LMT_ACCUMULATE, LMT_TILE_SCALES = 1, 2
-LMT_MAX_ROWS, LMT_MAX_WIDTH = 0x7FFFFFFF, 0x7FFFFF
+LMT_MAX_ROWS, LMT_MAX_WIDTH = 0x7FFFFF00, 0x7FFFFF
 _ERR = {-1: "LMT_ERR_NULL", -2: "LMT_ERR_ARG", -3: "LMT_ERR_LIMIT", -4: "LMT_ERR_HIP", -5: "LMT_ERR_ALIGN", -6: "LMT_ERR_WORKSPACE"}
 _BYTES = 7                          # uint8: scales and workspaces
 
