@@ -72,15 +72,16 @@ __device__ __forceinline__ uint32_t key_of(const EmbedGrad& p, uint32_t t) {
   return p.vocab;
 }
 
-// Lanes of this wavefront that hold the same digit, among the lanes in `valid`.
+// Lanes of this wavefront that hold the same digit, among the lanes in `valid`: those that agree bit by bit, four instructions for each.
 __device__ __forceinline__ uint64_t same_digit(uint32_t digit, uint32_t bits, uint64_t valid) {
-  uint64_t same = valid;
+  uint32_t lo = (uint32_t)valid, hi = (uint32_t)(valid >> 32);
+#pragma unroll 2
   for (uint32_t b = 0; b < bits; ++b) {
-    const bool one = digit >> b & 1u;
-    const uint64_t ones = __ballot(one);
-    same &= one ? ones : ~ones;
+    const uint32_t mine = (uint32_t)__builtin_amdgcn_sbfe((int)digit, b, 1);  // all ones or zeros
+    const uint64_t ones = __ballot(mine != 0);
+    lo &= ~((uint32_t)ones ^ mine), hi &= ~((uint32_t)(ones >> 32) ^ mine);
   }
-  return same;
+  return (uint64_t)hi << 32 | lo;
 }
 
 // Ranks of a wavefront's keys (R x 64 in a row, round by round) among its equal digits; seen[digit], cleared before, counts them.
@@ -92,7 +93,7 @@ __device__ __forceinline__ void rank_digits(const uint32_t (&key)[R], uint32_t s
     const bool valid = r * 64u + lane < n_valid;
     const uint32_t digit = key[r] >> shift & ((1u << bits) - 1u);
     const uint64_t same = same_digit(digit, bits, __ballot(valid));
-    const uint32_t before = (uint32_t)__popcll(same & ((1ull << lane) - 1ull));
+    const uint32_t before = __builtin_amdgcn_mbcnt_hi((uint32_t)(same >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)same, 0));
     rank[r] = valid ? seen[digit] + before : 0u;
     __builtin_amdgcn_wave_barrier();
     if (valid && before == 0) seen[digit] = (uint16_t)(rank[r] + (uint32_t)__popcll(same));
@@ -127,7 +128,7 @@ __device__ __forceinline__ void clear_rows(const Clear& c, uint64_t first, uint6
     const uint64_t n = min(c.bytes, c.end - r * c.stride);
     for (uint64_t b = (uint64_t)lane_id() * 16u; b < n; b += 1024u) {
       if (b + 16u <= n) {
-        *(LMT_GLOBAL typename At<2>::x4*)(row + b) = u32x4{0, 0, 0, 0};
+        __builtin_nontemporal_store(u32x4{0, 0, 0, 0}, (LMT_GLOBAL typename At<2>::x4*)(row + b));
       } else {
         for (uint64_t e = b; e < n; e += 2u) *(LMT_GLOBAL uint16_t*)(row + e) = 0;
       }
@@ -627,7 +628,7 @@ hipError_t launch_embed_grad(const EmbedGrad& p, int grad_out_dtype, int token_d
   if (small) {
     const uint64_t size = grad_dtype == LMT_F32 ? 4 : 2, bytes = p.width * size, stride = p.grad_ld * size, end = (p.vocab - 1) * stride + bytes;
     const Clear clear = p.grad_ld == p.width ? Clear{static_cast<char*>(p.grad), ceil_div(end, 4096), 4096, 4096, end} : Clear{static_cast<char*>(p.grad), p.vocab, stride, bytes, end};
-    const uint32_t grid = 1u + (p.accumulate ? 0u : (uint32_t)std::min<uint64_t>(kCus - 1u, ceil_div(clear.rows, kSortWaves)));
+    const uint32_t grid = 1u + (p.accumulate ? 0u : (uint32_t)std::min<uint64_t>(8 * kCus - 1u, ceil_div(clear.rows, kSortWaves)));
     e = with_id(token_dtype, [&](auto id) {
       typedef decltype(id) I;
       const auto kernel = p.n_tokens <= 2 * kSortThreads ? k_token_sort<I, 2> : p.n_tokens <= 4 * kSortThreads ? k_token_sort<I, 4> : p.n_tokens <= 8 * kSortThreads ? k_token_sort<I, 8> : k_token_sort<I, 16>;
