@@ -22,17 +22,18 @@ __device__ __forceinline__ uint32_t lane_id() { return threadIdx.x & 63u; }
 
 // ---- lookup ----------------------------------------------------------------------
 
-// Lanes per row: a power of two; rows longer than 64 pieces go in slabs of 64.  Bound by memory: 32 768 rows of 1 024 from fp32 to bf16 in
-// 19.2 us (94 MB to and from HBM, 4.8 TB/s, where a row is read once; 201 MB with what the caches repeat); 37 rows of 256 in 2.7.
+// Lanes per row: a power of two; rows longer than 64 pieces go in slabs of 64.  Bound by memory: 32 768 rows of 1 024, of 30 522 at random with a
+// quarter padding, from fp32 to bf16 in 26 us (29.7 with stores that stay in the L2; bf16 to bf16 18 and 27); 37 rows of 256 in 4.5, a launch.
 template <typename TI, typename TO, typename I>
 __global__ __launch_bounds__(kThreads) void k_embed(const Embed p, uint32_t lanes_log2, uint32_t slabs, uint64_t n_units) {
   constexpr int V = 16 / (sizeof(TI) > sizeof(TO) ? sizeof(TO) : sizeof(TI));
   const uint32_t lanes = 1u << lanes_log2, per_wave = 64u >> lanes_log2;
   const uint32_t sub = lane_id() >> lanes_log2, at = lane_id() & (lanes - 1u);
-  const uint64_t step = (uint64_t)gridDim.x * kWaves;
-  for (uint64_t u = (uint64_t)blockIdx.x * kWaves + (threadIdx.x >> 6); u < n_units; u += step) {
-    const uint64_t row = u / slabs * per_wave + sub;
-    const uint32_t col = ((uint32_t)(u % slabs) * 64u + at) * V;
+  const uint32_t step = gridDim.x * kWaves;
+  for (uint64_t unit = blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); unit < n_units; unit += step) {
+    const uint32_t u = (uint32_t)unit, of_row = u / slabs;  // the output is in memory, so there are fewer than 2^32
+    const uint64_t row = (uint64_t)of_row * per_wave + sub;
+    const uint32_t col = ((u - of_row * slabs) * 64u + at) * V;
     if (row >= p.n_tokens || col >= p.width) continue;
     const int64_t token = id_at<I>(p.tokens, row);
     const bool there = (uint64_t)token < p.vocab;
@@ -54,7 +55,7 @@ __global__ __launch_bounds__(kThreads) void k_embed(const Embed p, uint32_t lane
     }
     y.set(f);
     TO* to = static_cast<TO*>(p.out) + row * p.out_ld + col;
-    if (n == V) store<false>(to, y);
+    if (n == V) store<true>(to, y);
     else store_end(to, y, n);
   }
 }
@@ -76,7 +77,6 @@ __device__ __forceinline__ uint32_t key_of(const EmbedGrad& p, uint32_t t) {
 // Lanes of this wavefront that hold the same digit, among the lanes in `valid`: those that agree bit by bit, four instructions for each.
 __device__ __forceinline__ uint64_t same_digit(uint32_t digit, uint32_t bits, uint64_t valid) {
   uint32_t lo = (uint32_t)valid, hi = (uint32_t)(valid >> 32);
-#pragma unroll 2
   for (uint32_t b = 0; b < bits; ++b) {
     const uint32_t mine = (uint32_t)__builtin_amdgcn_sbfe((int)digit, b, 1);  // all ones or zeros
     const uint64_t ones = __ballot(mine != 0);

@@ -2,7 +2,7 @@
 //
 // lse = top + log(sum of exp(x - top)), loss = w (lse - x[target]), grad = w (exp(x - top) / sum - [j = target]).  Bound by memory: a row
 // is read once, kept in registers while its maximum and then its sum are found, and the gradient is written from there
-// (3 sweeps over memory, the last two from cache: 562 us at 16 384 x 30 522 in bf16, this 330 to 370, 5.4 to 6.1 TB/s).  Rows longer
+// (3 sweeps over memory, the last two from cache: 562 us at 16 384 x 30 522 in bf16, this 328, 6.1 TB/s).  Rows longer
 // than the registers of a workgroup are read twice, with a running maximum and sum the first time.
 #include "lmt_device.h"
 #include "lmt_internal.h"
@@ -54,8 +54,8 @@ __device__ __forceinline__ void put_loss(const CrossEntropy& p, uint64_t row, co
 }
 
 // One row per workgroup of THREADS threads (64: per wavefront), N vectors of 16 bytes per thread; what is left behind the last whole vector
-// goes one element to a thread.  16 384 x 30 522 in bf16 (512 threads of 8 vectors) 340 to 370 us, 2.0 GB; 19 rows in fp32 (1 024 of 8) 7.0,
-// the latency of one row.
+// goes one element to a thread.  16 384 x 30 522 in bf16 (512 threads of 8 vectors) 328 us, 2.0 GB, 6.1 TB/s (streaming stores of the gradient
+// 353); 19 rows in fp32 (1 024 threads of 8) 6.4, the latency of one row.
 template <typename T, typename I, int THREADS, int N>
 __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void k_cross_entropy(const CrossEntropy p) {
   constexpr int V = 16 / sizeof(T), kRowWaves = THREADS / 64;
@@ -134,6 +134,7 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void k_cross_entropy
 }
 
 // Rows of any length: a running maximum and sum per thread, joined at the end; then the gradient from a second reading.
+// 512 x 262 144 in bf16: 149 us (805 MB, 5.4 TB/s).
 constexpr int kLongThreads = 1024, kLongWaves = kLongThreads / 64;
 template <typename T, typename I>
 __global__ __launch_bounds__(kLongThreads) void k_cross_entropy_long(const CrossEntropy p) {
