@@ -2,6 +2,8 @@
 
 Thin ctypes binding over libbca.so (include/bca.h).  Every step of the path
 runs in the library's HIP kernels; Python only marshals pointers and sizes.
+The operators of a language model's step are in `lmt` (include/lmt.h), the
+load-balancing simulation in `lbs` (include/lbs.h).
 """
 from .binding import (  # noqa: F401
     BCA_CLIP_WHOLE_GRADIENT, BCA_GRAD_BF16, BCA_GRAD_F16, BCA_GRAD_F32, BCA_SKIP_STEP_ON_NONFINITE, BCA_STATUS_BAD_THRESHOLD, BCA_STATUS_NONFINITE,

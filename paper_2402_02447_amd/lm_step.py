@@ -27,17 +27,13 @@ IGNORE = -100
 
 
 class _Fp8:
-    """A matrix in 8 bits and / or its transpose, with the scales of both."""
+    """A matrix in 8 bits and its transpose, with the scales of both."""
 
-    def __init__(self, rows: int, cols: int, dtype, sides: str = "both", tile: bool = False):
-        self.q = self.scales = self.qt = self.scales_t = None
-        self.tile = tile
-        if sides != "cols":
-            q, s = lmt.fp8_shapes(rows, cols)
-            self.q, self.scales = torch.empty(q, dtype=dtype, device="cuda"), torch.empty(s, dtype=torch.uint8, device="cuda")
-        if sides != "rows":
-            q, s = lmt.fp8_shapes(cols, rows)
-            self.qt, self.scales_t = torch.empty(q, dtype=dtype, device="cuda"), torch.empty(s, dtype=torch.uint8, device="cuda")
+    def __init__(self, rows: int, cols: int, dtype, tile: bool = False):
+        def pair(r, c):
+            q, s = lmt.fp8_shapes(r, c)
+            return torch.empty(q, dtype=dtype, device="cuda"), torch.empty(s, dtype=torch.uint8, device="cuda")
+        (self.q, self.scales), (self.qt, self.scales_t), self.tile = pair(rows, cols), pair(cols, rows), tile
 
     def take(self, x, stream) -> None:
         lmt.quantize(x, self.q, self.scales, self.qt, self.scales_t, tile=self.tile, stream=stream)
