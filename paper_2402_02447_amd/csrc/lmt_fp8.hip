@@ -69,9 +69,10 @@ __device__ __forceinline__ uint32_t max16(uint32_t x) {
   return x;
 }
 
-// A workgroup takes squares of 128 x 128; a thread 4 rows of 8 columns, which it reads once for both results.  Bound by memory: 30 522 x
-// 1 024 in fp32, both sides, 38 us (4.9 TB/s); 8 192 x 1 024 in bf16 11.6 (8 rows to a thread of half as many 12.5: two workgroups
-// a compute unit, with less in flight).
+// A workgroup takes squares of 128 x 128; a thread 4 rows of 8 columns, which it reads once for both results.  Bound by memory, both sides:
+// 30 522 x 1 024 in fp32 38 us (4.9 TB/s), 16 384 x 4 096 in bf16 62 (4.3), 8 192 x 1 024 in bf16 8.6.  Results leave streaming, whole
+// lines at a time (kept in the L2: 38, 68, 11.2; only the transpose streaming: 38, 60, 9.5).  8 rows to a thread of half as many: two
+// workgroups a compute unit, less in flight, a tenth slower.
 constexpr uint32_t kQuantizeThreads = 512;
 template <typename T, bool E5M2, bool TILE>
 __global__ __launch_bounds__(kQuantizeThreads, 4) void k_quantize(const Quantize p, uint32_t tiles_across, uint32_t tiles_down) {
@@ -142,7 +143,7 @@ __global__ __launch_bounds__(kQuantizeThreads, 4) void k_quantize(const Quantize
         const float by = inverse_of(row_scale[j]);
         const float lo[4] = {x[j].get(0), x[j].get(1), x[j].get(2), x[j].get(3)}, hi[4] = {x[j].get(4), x[j].get(5), x[j].get(6), x[j].get(7)};
         const u32x2 w = {pack4<E5M2>(lo, by), pack4<E5M2>(hi, by)};
-        *(LMT_GLOBAL u32x2*)(p.q + (uint64_t)(r0 + j) * q_row + c0) = w;
+        __builtin_nontemporal_store(w, (LMT_GLOBAL u32x2*)(p.q + (uint64_t)(r0 + j) * q_row + c0));
         if (cg == 0) {
           uint8_t* s = p.scales + (uint64_t)(r0 + j) * s_row;
           s[tc] = (uint8_t)row_scale[j];
@@ -170,8 +171,7 @@ __global__ __launch_bounds__(kQuantizeThreads, 4) void k_quantize(const Quantize
       for (uint32_t k = 0; k < 2; ++k) {
         const uint32_t c = k * 64u + threadIdx.x / 8u, piece = threadIdx.x & 7u;
         if (tc * 128u + c < p.cols)
-          *(LMT_GLOBAL u32x4*)(p.qt + (uint64_t)(tc * 128u + c) * qt_row + (uint64_t)tr * 128u + piece * 16u) =
-              *reinterpret_cast<const u32x4*>(&turned[c * 128u + (piece ^ (c / 8u & 7u)) * 16u]);
+          __builtin_nontemporal_store(*reinterpret_cast<const u32x4*>(&turned[c * 128u + (piece ^ (c / 8u & 7u)) * 16u]), (LMT_GLOBAL u32x4*)(p.qt + (uint64_t)(tc * 128u + c) * qt_row + (uint64_t)tr * 128u + piece * 16u));
       }
     }
     __syncthreads();
