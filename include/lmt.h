@@ -22,7 +22,8 @@
  *     length.  Floating-point matrices need only be aligned to their element size; the
  *     8-bit ones start on 16 bytes and have the fixed strides below.
  *   - Outputs may not overlap inputs or each other except where it is said.
- *   - Sums are in fp32 in an order that depends on the sizes alone: the same call gives the same bits.
+ *   - Sums are in fp32 (but see lmt_matmul on 16-bit results) in an order that depends on the sizes, and for lmt_embed_grad
+ *     the tokens, alone: the same call gives the same bits.
  *   - `status` (DEVICE int32, or NULL) has LMT_STATUS_* bits ORed in; the caller clears it,
  *     so that one word can watch many calls.
  */
@@ -56,6 +57,7 @@ extern "C" {
 
 #define LMT_ACCUMULATE 1u  /* add to what the output holds                                           */
 #define LMT_TILE_SCALES 2u /* lmt_quantize: one scale for a square of 128 x 128 instead of 128 x 1     */
+#define LMT_FP32_SUMS 4u   /* lmt_matmul: a 16-bit c from sums as exact as an fp32 one's                */
 
 #define LMT_MAX_ROWS 0x7fffff00u  /* tokens, vocabulary, rows, classes, m, n                     */
 #define LMT_MAX_WIDTH 0x7fffffu   /* row length of tables and of 8-bit matrices, k                 */
@@ -99,11 +101,13 @@ int lmt_quantize(const void* x /*DEVICE*/, int dtype, uint64_t rows, uint64_t co
 
 /* c[i][j] = (old c[i][j], with LMT_ACCUMULATE) + sum over l < k of a[i][l] * b[j][l], for i < m, j < n, both operands in the
  * 8-bit form above with rows of k elements (each LMT_E4M3 or LMT_E5M2); c: fp32, fp16 or bf16, [m][ldc].  Products and sums are
- * made by the matrix cores in fp32 and rounded once to c's type.  A 16-bit c takes the 8-bit instructions, which line up the products of a
- * few neighbours before they add them: of terms that are much smaller than their neighbours the last bits are lost (about 1.5e-5
- * of the 2-norm of a result of random numbers, a hundredth of bf16's rounding); an fp32 c takes bf16 ones, at a third to half of the rate, and
- * keeps 1e-7.  a_scales and b_scales are 4-byte aligned and between 1 and 254.  workspace: as above, at least
- * lmt_matmul_workspace bytes; may be NULL where that is 0.
+ * made by the matrix cores and rounded once to c's type.  A 16-bit c takes the 8-bit instructions, which line up the products of
+ * eight neighbours before they add them in fp32: of terms that are much smaller than their neighbours the last bits are lost, about 1.5e-5 of the
+ * 2-norm of a result of normal numbers and up to 4e-5 where their magnitudes spread over e^2, at any k (a hundredth and a fortieth
+ * of bf16's rounding, a fourteenth and a fifth of fp16's).  With LMT_FP32_SUMS it takes the bf16 instructions that an fp32 c always takes: exact products, sums
+ * in fp32, at a third to half of the rate.  Those see an operand's elements as bf16 numbers: from 2^128 on infinite, below
+ * 2^-130 exact to 2^-133 only.  a_scales and b_scales are 4-byte aligned and between 1 and 254.  workspace: as above, at
+ * least lmt_matmul_workspace bytes; may be NULL where that is 0.
  * With x [T][H] and a weight w [V][H]: logits = x w^T are matmul(q(x), q(w)); the input's gradient dy w is
  * matmul(q(dy), qt(w)); the weight's dy^T x is matmul(qt(dy), qt(x)). */
 uint64_t lmt_matmul_workspace(uint64_t m, uint64_t n, uint64_t k);

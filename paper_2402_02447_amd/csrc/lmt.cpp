@@ -98,7 +98,7 @@ int lmt_matmul(const void* a, int a_fp8, const uint8_t* a_scales, const void* b,
                uint64_t k, void* c, int c_dtype, uint64_t ldc, uint32_t flags, void* workspace, uint64_t workspace_bytes, void* stream) {
   if (!is_fp8(a_fp8) || !is_fp8(b_fp8)) return fail(LMT_ERR_ARG, "a and b must be LMT_E4M3 or LMT_E5M2");
   if (!is_float(c_dtype)) return fail(LMT_ERR_ARG, "c must be fp32, fp16 or bf16");
-  if (flags & ~LMT_ACCUMULATE) return fail(LMT_ERR_ARG, "unknown flags");
+  if (flags & ~(LMT_ACCUMULATE | LMT_FP32_SUMS)) return fail(LMT_ERR_ARG, "unknown flags");
   if (m > LMT_MAX_ROWS || n > LMT_MAX_ROWS || k > LMT_MAX_WIDTH) return fail(LMT_ERR_LIMIT, "sizes exceed LMT_MAX_ROWS or LMT_MAX_WIDTH");
   if (ldc < n) return fail(LMT_ERR_ARG, "ldc is below n");
   const bool accumulate = (flags & LMT_ACCUMULATE) != 0;
@@ -108,7 +108,7 @@ int lmt_matmul(const void* a, int a_fp8, const uint8_t* a_scales, const void* b,
     return fail(LMT_ERR_ALIGN, "operands must start on 16 bytes, scales on 4, c on its element size");
   if (const int rc = workspace_error(workspace, workspace_bytes, lmt::matmul_workspace(m, n, k))) return rc;
   const lmt::Matmul p{static_cast<const uint8_t*>(a), a_scales, static_cast<const uint8_t*>(b), b_scales, c, ldc, (uint32_t)m, (uint32_t)n, (uint32_t)k, accumulate,
-                      static_cast<float*>(workspace)};
+                      (flags & LMT_FP32_SUMS) != 0, static_cast<float*>(workspace)};
   return launched("launching the product", lmt::launch_matmul(p, a_fp8, b_fp8, c_dtype, (hipStream_t)stream));
 }
 

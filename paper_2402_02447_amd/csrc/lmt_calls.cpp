@@ -234,16 +234,17 @@ PyObject* call_quantize(PyObject*, PyObject* const* args, Py_ssize_t n) {
   });
 }
 
-// lmt_matmul(functions, a, a_scales, b, b_scales, c, workspace, accumulate, stream)
+// lmt_matmul(functions, a, a_scales, b, b_scales, c, workspace, accumulate, stream[, fp32_sums])
 PyObject* call_matmul(PyObject*, PyObject* const* args, Py_ssize_t n) {
-  Args a(args, n, 9);
+  Args a(args, n, n == 10 ? 10 : 9);
   Tensor x, xs, y, ys, c;
   uint64_t bytes;
   a.fp8("a", "a_scales", &x, &xs, false), a.fp8("b", "b_scales", &y, &ys, false);
   a.matrix("c", &c);
   void* workspace = a.workspace(&bytes);
-  const uint32_t flags = a.truth() ? LMT_ACCUMULATE : 0u;
+  uint32_t flags = a.truth() ? LMT_ACCUMULATE : 0u;
   void* s = a.stream();
+  if (n == 10 && a.truth()) flags |= LMT_FP32_SUMS;
   a.need(x.cols() == y.cols(), "b", "rows as long as a's are wanted");
   a.need(c.rows() == x.rows() && c.cols() == y.rows(), "c", "a's rows times b's rows are wanted");
   return a.call([&] {

@@ -4,9 +4,12 @@
 // instructions of gfx950 take one for every 32 elements of an operand's row along with the operand
 // (v_mfma_scale_f32_32x32x64_f8f6f4): with a block of 128 all four are the same byte, and scaled blocks add up in the accumulators
 // with no work beside it.
-// Those instructions line up the products of eight neighbours before they add them, which costs 1.5e-5 of a result's 2-norm on random
-// numbers whatever k: nothing beside the rounding of a 16-bit c, but too much for an fp32 one, whose operands are widened to bf16 (exactly:
-// 3 bits of mantissa and a power of two) and go through the bf16 instructions (7e-8), at 1.3 PFLOP/s from registers instead of 4.7.
+// Those instructions line up the products of eight neighbours before they add them, on a grid that the largest of them sets; what lies below it is cut off.
+// Measured, of a result's 2-norm and whatever k: 1.5e-5 on normal numbers in e4m3 (e5m2 9e-6), up to 4e-5 where magnitudes spread over
+// e^2, a drift of 3e-6 towards zero where all terms have one sign.  A 16-bit c takes them by choice, as its own rounding is larger (2-norm
+// of it: bf16 1.7e-3, fp16 2.1e-4; one element in a hundred, or one in fifteen of an fp16 c, goes to the other neighbour) and they are two to three
+// times as fast; with LMT_FP32_SUMS it does not.  For those and for an fp32 c operands are widened to bf16 (exactly: 3 bits of
+// mantissa and a power of two) and go through the bf16 instructions (4e-8 at k of 1 024), at 1.3 PFLOP/s from registers instead of 4.7.
 #include "lmt_device.h"
 #include "lmt_internal.h"
 
@@ -508,9 +511,8 @@ struct Lane {  // 32 bytes of a row's block, the lane's share of it
     return __builtin_bit_cast(bf16x8, u32x4{widen<E5M2, false>(lo, s), widen<E5M2, true>(lo, s), widen<E5M2, false>(hi, s), widen<E5M2, true>(hi, s)});
   }
 };
-template <int AF, int BF, typename TC>
+template <int AF, int BF, bool WIDE, typename TC>
 __global__ __launch_bounds__(64 * kFewWaves) void k_matmul_few(const Matmul p) {
-  constexpr bool WIDE = sizeof(TC) == 4;
   __shared__ f32x4 part[kFewWaves][4][64];
   const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15u;
   const uint32_t n0 = blockIdx.x * 16u, blocks = (p.k + 127u) / 128u, s_row = (uint32_t)scale_row_bytes(p.k);
@@ -624,11 +626,11 @@ uint64_t matmul_workspace(uint64_t m, uint64_t n, uint64_t k) {
 
 hipError_t launch_matmul(const Matmul& p, int a_fp8, int b_fp8, int c_dtype, hipStream_t s) {
   const Choice c = choose(p.m, p.n, p.k);
-  const auto tiled = [&](auto shape, auto af, auto bf, auto tc) {
+  const auto tiled = [&](auto shape, auto af, auto bf, auto wide, auto tc) {
     typedef decltype(shape) S;
     typedef decltype(tc) TC;
     const uint32_t n_tiles = c.tiles.across * c.tiles.down;
-    hipLaunchKernelGGL((k_matmul<S, decltype(af)::value, decltype(bf)::value, sizeof(TC) == 4, TC>), dim3(n_tiles * c.tiles.splits), dim3(S::threads), 0, s, p, c.tiles);
+    hipLaunchKernelGGL((k_matmul<S, decltype(af)::value, decltype(bf)::value, decltype(wide)::value != 0, TC>), dim3(n_tiles * c.tiles.splits), dim3(S::threads), 0, s, p, c.tiles);
     if (c.tiles.splits > 1)
       hipLaunchKernelGGL((k_matmul_join<S, TC>), dim3(n_tiles * S::TM * S::TN * 4), dim3(S::threads), 0, s, p, c.tiles);
     return hipGetLastError();
@@ -636,13 +638,17 @@ hipError_t launch_matmul(const Matmul& p, int a_fp8, int b_fp8, int c_dtype, hip
   return with_fp8(a_fp8, [&](auto af) {
     return with_fp8(b_fp8, [&](auto bf) {
       return with_float(c_dtype, [&](auto tc) {
-        switch (c.form) {
-          case Choice::kFew:
-            hipLaunchKernelGGL((k_matmul_few<decltype(af)::value, decltype(bf)::value, decltype(tc)>), dim3((uint32_t)ceil_div(p.n, 16)), dim3(64 * kFewWaves), 0, s, p);
-            return hipGetLastError();
-          case Choice::kMedium: return tiled(Medium{}, af, bf, tc);
-          default: return tiled(Large{}, af, bf, tc);
-        }
+        const auto go = [&](auto wide) {
+          switch (c.form) {
+            case Choice::kFew:
+              hipLaunchKernelGGL((k_matmul_few<decltype(af)::value, decltype(bf)::value, decltype(wide)::value != 0, decltype(tc)>), dim3((uint32_t)ceil_div(p.n, 16)), dim3(64 * kFewWaves), 0, s, p);
+              return hipGetLastError();
+            case Choice::kMedium: return tiled(Medium{}, af, bf, wide, tc);
+            default: return tiled(Large{}, af, bf, wide, tc);
+          }
+        };
+        if constexpr (sizeof(tc) == 4) return go(Const<1>{});
+        else return p.fp32_sums ? go(Const<1>{}) : go(Const<0>{});
       });
     });
   });

@@ -55,7 +55,7 @@ struct Matmul {
   void* c;
   uint64_t ldc;
   uint32_t m, n, k;
-  bool accumulate;
+  bool accumulate, fp32_sums;
   float* workspace;
 };
 uint64_t matmul_workspace(uint64_t m, uint64_t n, uint64_t k);

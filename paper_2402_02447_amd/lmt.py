@@ -14,7 +14,7 @@ from .binding import load_library
 
 LMT_F32, LMT_F16, LMT_BF16, LMT_E4M3, LMT_E5M2, LMT_I32, LMT_I64 = range(7)
 LMT_STATUS_BAD_TOKEN, LMT_STATUS_BAD_TARGET = 1, 2
-LMT_ACCUMULATE, LMT_TILE_SCALES = 1, 2
+LMT_ACCUMULATE, LMT_TILE_SCALES, LMT_FP32_SUMS = 1, 2, 4
 LMT_MAX_ROWS, LMT_MAX_WIDTH = 0x7FFFFF00, 0x7FFFFF
 _ERR = {-1: "LMT_ERR_NULL", -2: "LMT_ERR_ARG", -3: "LMT_ERR_LIMIT", -4: "LMT_ERR_HIP", -5: "LMT_ERR_ALIGN", -6: "LMT_ERR_WORKSPACE"}
 _BYTES = 7                          # uint8: scales and workspaces
@@ -113,11 +113,12 @@ def matmul_workspace(m: int, n: int, k: int) -> int:
     return int(_lib().lmt_matmul_workspace(m, n, k))
 
 
-def matmul(a, a_scales, b, b_scales, c, workspace=None, accumulate: bool = False, stream=None) -> None:
-    """c [m, n] = (c if accumulate) + a b^T for operands as quantize leaves them, of m and n rows."""
+def matmul(a, a_scales, b, b_scales, c, workspace=None, accumulate: bool = False, stream=None, fp32_sums: bool = False) -> None:
+    """c [m, n] = (c if accumulate) + a b^T for operands as quantize leaves them, of m and n rows.  fp32_sums: a 16-bit c from sums as exact as an fp32
+    one's, at a third to half of the rate (lmt.h says what the others lose)."""
     if _table is None:
         _connect()
-    _check(_calls.lmt_matmul(_table, a, a_scales, b, b_scales, c, workspace, accumulate, stream))
+    _check(_calls.lmt_matmul(_table, a, a_scales, b, b_scales, c, workspace, accumulate, stream, fp32_sums))
 
 
 def cross_entropy(logits, targets, loss=None, lse=None, grad=None, weights=None, ignore: int = -100, status=None, stream=None) -> None:
