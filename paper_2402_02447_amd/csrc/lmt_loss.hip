@@ -46,11 +46,12 @@ __device__ __forceinline__ Row row_of(const CrossEntropy& p, uint64_t row, bool 
   r.w = !r.there ? 0.f : p.weights ? load1(p.weights + row) : 1.f;
   return r;
 }
-// Sum 0: nothing but -Inf (the largest logit adds 1, NaN makes the sum NaN).
+// Sum 0: nothing but -Inf (the largest logit adds 1, NaN makes the sum NaN).  The loss is not made of lse, which is rounded to the size of the logits: a small
+// loss would be the difference of two large numbers.
 __device__ __forceinline__ void put_loss(const CrossEntropy& p, uint64_t row, const Row& r, float top, float sum, float at_target) {
-  const float lse = sum == 0.f ? -INFINITY : top + __logf(sum);
-  if (p.lse) p.lse[row] = lse;
-  if (p.loss) p.loss[row] = !r.there ? 0.f : sum == 0.f ? INFINITY : r.w * (lse - at_target);
+  const float log_sum = __logf(sum);
+  if (p.lse) p.lse[row] = sum == 0.f ? -INFINITY : top + log_sum;
+  if (p.loss) p.loss[row] = !r.there ? 0.f : sum == 0.f ? INFINITY : r.w * ((top - at_target) + log_sum);
 }
 
 // One row per workgroup of THREADS threads (64: per wavefront), N vectors of 16 bytes per thread; what is left behind the last whole vector

@@ -1,0 +1,81 @@
+"""How exact losses and their gradients are (GPU): bounds from the roundings that a subtraction of the maximum, exp2 and a sum over lanes take, with no part that grows
+with the logits' common offset."""
+import numpy as np
+import pytest
+import torch
+
+from lmt_gpu import DT, typed, within
+from lmt_reference import U32 as U
+from paper_2402_02447_amd import lmt
+
+pytestmark = pytest.mark.gpu
+
+
+def formulas(x, t, w):
+    """loss, probabilities, x - max and log of the sum of exp(x - max), in 64 bits.  x, t, w: numpy, every row counted and finite."""
+    x, at = x.astype(np.float64), np.arange(len(x))
+    d = x - x.max(1, keepdims=True)
+    e = np.exp(d)
+    # the target's term apart, so that a loss of a probability near 1 keeps its digits
+    others = e.copy()
+    others[at, t] = 0
+    others = others.sum(1)
+    loss = w * np.where(d[at, t] == 0, np.log1p(others), np.log(others + e[at, t]) - d[at, t])
+    return loss, e / e.sum(1, keepdims=True), d, np.log(e.sum(1))
+
+
+def sum_roundings(V):
+    """Additions a term goes through: up to 128 of a lane's own, or its share of a longer row; 6 over a wavefront, 16 over a workgroup."""
+    return max(128, -(-V // 1024) + 8) + 22
+
+
+def sum_bound(p, d, V):
+    """Relative error of a row's sum: of each term 3 |d| u (the difference, log2(e) and their product, each rounded) and 3 u of exp2; the additions."""
+    return (p * (3 * np.abs(d) + 3)).sum(1) * U + sum_roundings(V) * U
+
+
+def loss_bound(loss, p, d, log_sum, t, w, V):
+    """The difference to the target, the sum, its logarithm (2 u of itself and 2 u near 0), their sum, the weight."""
+    to_target = np.abs(d[np.arange(len(t)), t])
+    return w * (U * to_target + sum_bound(p, d, V) + 2 * U * log_sum + 2 * U) + 2 * U * np.abs(loss)
+
+
+def call(x, t, w, dtype, grad=False, lse=False):
+    X = torch.as_tensor(x).to(DT[dtype]).cuda()
+    loss = torch.empty(len(x), device="cuda")
+    g = torch.empty_like(X) if grad else None
+    s = torch.empty_like(loss) if lse else None
+    lmt.cross_entropy(X, torch.as_tensor(t).cuda(), loss, s, g, torch.as_tensor(w, dtype=torch.float32).cuda())
+    return [None if o is None else o.double().cpu().numpy() for o in (loss, s, g)]
+
+
+def confident(rng, n, V, gap, offset):
+    """The target is the largest logit, `gap` above a field of N(0, 1): losses of about V exp(1/2 - gap)."""
+    x = rng.normal(0, 1, (n, V))
+    t = rng.integers(0, V, n)
+    x[np.arange(n), t] = gap
+    return x + offset, t, np.float32(rng.uniform(0.5, 2, n)).astype(np.float64)
+
+
+@pytest.mark.parametrize("V,gap", [(100, 12), (100, 18), (1000, 14), (30522, 18), (30522, 24), (200000, 20)])
+@pytest.mark.parametrize("offset", [0, 20, 60, -300, 3000])
+def test_a_small_loss_does_not_lose_to_the_logits_offset(V, gap, offset):
+    x, t, w = confident(np.random.default_rng(V + gap), 40 if V < 1e5 else 6, V, gap, offset)
+    x = typed(x, "f32")
+    loss, p, d, log_sum = formulas(x, t, w)
+    assert 1e-7 < loss.max() < 1e-1
+    within(call(x, t, w, "f32")[0], loss, loss_bound(loss, p, d, log_sum, t, w, V))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("V", [100, 3000, 30522, 200000])
+def test_an_offset_of_every_logit_leaves_the_same_loss(dtype, V):
+    """Logits of whole numbers and offsets that keep them so: x - max is the same bits, and so is all that follows."""
+    rng = np.random.default_rng(V)
+    x, t, w = rng.integers(-8, 9, (10, V)).astype(np.float64), rng.integers(0, V, 10), rng.uniform(0.5, 1, 10)
+    t[:5] = x[:5].argmax(1)
+    first = call(x, t, w, dtype, True)
+    for offset in (-100, 64, 200) if dtype == "bf16" else (-1000, 64, 2000):
+        near = call(x + offset, t, w, dtype, True)
+        assert np.array_equal(typed(x + offset, dtype), x + offset)
+        assert np.array_equal(first[0], near[0]) and np.array_equal(first[2], near[2])
