@@ -26,9 +26,11 @@ __device__ __forceinline__ float wave_sum(float x) {
 // exp(x - top) for x <= top.  The difference comes first: top * log2(e) alone would overflow where a row is masked with the
 // type's lowest value.
 __device__ __forceinline__ float term(float x, float top) { return __builtin_amdgcn_exp2f((x - top) * kLog2e); }
-// ... times c, with results below 2^-126 too, which the instruction cuts to 0.
+// ... times c, with results below 2^-126 too, which the instruction cuts to 0: as the square of the root, whose argument has the same bits (an offset to
+// the exponent instead, taken off again behind, would hold an argument of 16 to 32 to 2^-20).
 __device__ __forceinline__ float scaled_term(float x, float top, float c) {
-  return __builtin_amdgcn_ldexpf(__builtin_amdgcn_exp2f((x - top) * kLog2e + 32.f) * c, -32);
+  const float root = __builtin_amdgcn_exp2f((x - top) * (0.5f * kLog2e));
+  return root * c * root;
 }
 
 // What a row has beside its logits.

@@ -79,3 +79,35 @@ def test_an_offset_of_every_logit_leaves_the_same_loss(dtype, V):
         near = call(x + offset, t, w, dtype, True)
         assert np.array_equal(typed(x + offset, dtype), x + offset)
         assert np.array_equal(first[0], near[0]) and np.array_equal(first[2], near[2])
+
+
+@pytest.mark.parametrize("V", [200, 3000, 30522, 200000])
+@pytest.mark.parametrize("width", [2, 4, 12])
+def test_gradients_keep_the_low_bits_of_the_exponent(V, width):
+    """y = (x - max) log2(e) by two fp32 operations, which numpy repeats; what remains of a gradient is 2^y times a factor of its row: an ulp, 2 u, for 2^y,
+    u for the product, and as much for the median that stands for the factor.  (With an argument of 16 to 32 instead of y, errors reach 11 u more.)"""
+    rng = np.random.default_rng(V)
+    n = 12 if V < 1e5 else 4
+    x = rng.uniform(-width, 0, (n, V)).astype(np.float32)
+    grad = call(x, np.zeros(n, np.int64), np.ones(n), "f32", True)[2][:, 1:]      # the target has another formula
+    y = ((x - x.max(1, keepdims=True)) * np.float32(1.44269504088896340736))[:, 1:]
+    assert y.dtype == np.float32
+    ratio = grad / np.exp2(y.astype(np.float64))
+    assert (np.abs(ratio / np.median(ratio, 1, keepdims=True) - 1) <= 2 * (2 + 1) * U).all()
+
+
+@pytest.mark.parametrize("V", [40, 3000, 200000])
+def test_gradients_far_below_the_largest_are_not_cut_off(V):
+    """Probabilities from 1 down to fp32's smallest, below which 0 is right."""
+    rng = np.random.default_rng(V)
+    x = typed(rng.uniform(-110, 0, (8 if V < 1e5 else 2, V)), "f32")
+    x[:, 0] = 0
+    t, w = np.ones(len(x), np.int64), np.ones(len(x))
+    loss, p, d, log_sum = formulas(x, t, w)
+    for scale in (1.0, 2.0 ** -20, 2.0 ** 20):
+        grad = call(x, t, w * scale, "f32", True)[2]
+        want = scale * p
+        want[:, 1] -= scale
+        bound = scale * p * (3 * np.abs(d) + 6 + sum_bound(p, d, V)[:, None] / U) * U + 2.0 ** -149
+        bound[:, 1] += 2 * U * scale
+        within(grad, want, bound)
