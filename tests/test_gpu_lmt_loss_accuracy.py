@@ -4,8 +4,8 @@ import numpy as np
 import pytest
 import torch
 
-from lmt_gpu import DT, typed, within
-from lmt_reference import U32 as U
+from lmt_gpu import DT, Mat, typed, within
+from lmt_reference import U32 as U, rounded
 from paper_2402_02447_amd import lmt
 
 pytestmark = pytest.mark.gpu
@@ -111,3 +111,39 @@ def test_gradients_far_below_the_largest_are_not_cut_off(V):
         bound = scale * p * (3 * np.abs(d) + 6 + sum_bound(p, d, V)[:, None] / U) * U + 2.0 ** -149
         bound[:, 1] += 2 * U * scale
         within(grad, want, bound)
+
+
+SIZES = [(5, 1), (5, 2), (5, 7), (9, 8), (40, 255), (40, 257), (20, 1023), (10, 2049), (10, 4097), (6, 8193), (6, 16385), (4, 30522), (3, 32769), (3, 65537), (2, 131073), (2, 300001)]
+
+
+@pytest.mark.parametrize("n,V", SIZES)
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("sigma,offset", [(2.0, 0.0), (0.01, 9.0), (20.0, -40.0)])
+def test_every_output_within_the_roundings_of_sums_over_lanes(n, V, dtype, sigma, offset):
+    """A relative 2e-5 at most at the usual sizes; what a gradient's own type rounds comes on top."""
+    rng = np.random.default_rng(V)
+    x = typed(rng.normal(offset, sigma, (n, V)), dtype)
+    x[:, 1::7] = np.where(rng.random((n, 1)) < 0.5, -np.inf, x[:, 1::7])            # classes that cannot occur, in half of the rows
+    x[n - 1, 0] = x[n - 1].max()                                                     # a tie, for the first place too
+    t = np.where(rng.random(n) < 0.5, x.argmax(1), 0)
+    w = np.float32(rng.uniform(0.1, 2, n)).astype(np.float64)
+    loss, p, d, log_sum = formulas(x, t, w)
+    d = np.where(p > 0, d, 0)
+    rel = sum_bound(p, d, V)
+    assert V > 1e5 or sigma > 2 or rel.max() < 2e-5
+    at = np.arange(n)
+    grad = w[:, None] * p
+    # a gradient: what a term has, but 6 u of exp2 (its root twice, and their products), the quotient and its product 2; of the target's, the difference
+    bound = grad * (3 * np.abs(d) + 8 + rel[:, None] / U) * U
+    grad[at, t] = np.where(V > 1, w * (p[at, t] - 1), 0)
+    bound[at, t] += 2 * U * w
+    lse = x.max(1) + log_sum
+    for in_place in (False, True):
+        m = Mat(n, V, dtype, 3, 1, x)
+        g = m if in_place else Mat(n, V, dtype, 2, 0)
+        out, s = torch.empty(n, device="cuda"), torch.empty(n, device="cuda")
+        lmt.cross_entropy(m.view, torch.as_tensor(t).cuda(), out, s, g.view, torch.as_tensor(w, dtype=torch.float32).cuda())
+        within(out.cpu().numpy(), loss, loss_bound(loss, p, d, log_sum, t, w, V))
+        within(s.cpu().numpy(), lse, rel + 2 * U * log_sum + 2 * U + U * np.abs(lse))
+        within(g.numpy(), grad, bound + rounded(np.abs(grad) + bound, dtype))
+        assert g.untouched_outside() and m.untouched_outside()
