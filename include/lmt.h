@@ -105,7 +105,7 @@ int lmt_quantize(const void* x /*DEVICE*/, int dtype, uint64_t rows, uint64_t co
  * eight neighbours before they add them in fp32: of terms that are much smaller than their neighbours the last bits are lost, about 1.5e-5 of the
  * 2-norm of a result of normal numbers and up to 4e-5 where their magnitudes spread over e^2, at any k (a hundredth and a fortieth
  * of bf16's rounding, a fourteenth and a fifth of fp16's).  With LMT_FP32_SUMS it takes the bf16 instructions that an fp32 c always takes: exact products, sums
- * in fp32, at a third to half of the rate.  Those see an operand's elements as bf16 numbers: from 2^128 on infinite, below
+ * in fp32, at three to four fifths of the rate.  Those see an operand's elements as bf16 numbers: from 2^128 on infinite, below
  * 2^-130 exact to 2^-133 only.  a_scales and b_scales are 4-byte aligned and between 1 and 254.  workspace: as above, at
  * least lmt_matmul_workspace bytes; may be NULL where that is 0.
  * With x [T][H] and a weight w [V][H]: logits = x w^T are matmul(q(x), q(w)); the input's gradient dy w is

@@ -1,8 +1,8 @@
 // Embedding lookup and the gradient of its table (lmt.h).
 //
 // Lookup: out[t] = scale * table[token[t]].  Every element is read and written once; a row is taken by as many lanes of a
-// wavefront as it has pieces of 16 bytes (of the wider type's elements), so a wavefront has one piece of a long row or several
-// short rows.
+// wavefront as it has pieces, of as many elements as 16 bytes hold of the narrower of the two types, so a wavefront has 64 pieces of a
+// long row or several short rows.
 //
 // Gradient: grad[v] = scale * sum of grad_out[t] over the t with token[t] = v.  The positions t are sorted by token (stable
 // radix sort, ten bits at a time at most; up to 16 384 tokens by one workgroup in LDS, while the others clear the table), the sorted
@@ -204,7 +204,9 @@ __global__ __launch_bounds__(kSortThreads) void k_token_sort(const EmbedGrad p, 
 // One pass of the sort of more tokens than that: workgroups count their digits, then each adds up the counts and moves its
 // tokens.  1024 threads with R tokens each: 2 where that makes up to 256 workgroups, which all read all counts, and 8 above (calls with rows of
 // 64, us, 2 and 8: 262 144 tokens 73 and 86, 524 288 110 and 122, 1 048 576 203 and 188).  Bound by latency: 262 144 tokens in two passes of
-// 4.7 + 9.6 us (10 MB in and out).
+// 4.7 + 9.6 us (10 MB in and out).  Every workgroup reads the counts of all, so the reading grows with the square of the tokens: nothing beside the rest up to
+// a million, 51 us a pass of 4 194 304 tokens (30 522 of them different), 340 of 16 777 216, 8.6 GB; beyond, the form still gives the right order, but a
+// sum of the counts in a launch of its own would be the better one.
 struct Sort {  // FIRST: from the tokens themselves
   const u32x2* from;
   u32x2* to;
@@ -543,8 +545,10 @@ __global__ __launch_bounds__(kThreads) void k_token_none(const EmbedGrad p) {
 // ---- launches ------------------------------------------------------------------------
 
 // Positions per chunk.  Few tokens: short ones, so that more wavefronts load (us with 4, 8, 16: 600 tokens 14.2, 14.6, 16.1; 2 048 into a
-// table of 30 522 x 768 with 8, 16: 26.1, 27.1; 8 192: 31.4, 30.1, the joins cost more).  Many: about a thousand chunks (262 144 tokens
-// 139 us, with two thousand 141, with four 145).
+// table of 30 522 x 768 with 8, 16: 26.1, 27.1; 8 192: 31.4, 30.1, the joins cost more).  Many: about a thousand chunks (262 144 tokens with rows of 1 024
+// 139 us, with two thousand 141, with four 145).  Drawn for rows of 1 024, four wavefronts a chunk; rows of up to 256 have one, and 1 024 wavefronts do not fill the
+// card: 262 144 tokens with rows of 64, 128 and 256 in bf16 all take 74 to 80 us where 1 024 take 191, and 16 777 216 with rows of 64 spend 2 000 of
+// 2 750 in the sums, 1.1 TB/s.  Shorter chunks for narrow rows have not been measured.
 uint32_t chunk_of(uint64_t n_tokens) {
   uint64_t chunk = n_tokens <= 1024 ? 4 : n_tokens <= 4096 ? 8 : 16;
   while (chunk * 1024u < n_tokens) chunk *= 2;
@@ -552,7 +556,8 @@ uint32_t chunk_of(uint64_t n_tokens) {
 }
 
 // Tokens that one workgroup sorts.  A whole call into 30 522 x 768, with more than 2 048 tokens sorted by many workgroups instead: 4 096 tokens
-// 28 us (56), 8 192 30 (56), 16 384 47 (64); adding to the table, where nothing has to be cleared meanwhile, 23 (33), 32 (37), 51 (46).
+// 28 us (56), 8 192 30 (56), 16 384 47 (64); adding to the table, where nothing has to be cleared meanwhile, 23 (33), 32 (37), 51 (46).  One border for both,
+// since the workspace is asked for without the flag: it costs the upper end of what is added a tenth.
 constexpr uint64_t kMostSorted = 16 * kSortThreads;
 
 struct Passes {

@@ -2,7 +2,7 @@
 //
 // lse = top + log(sum of exp(x - top)), loss = w (lse - x[target]), grad = w (exp(x - top) / sum - [j = target]).  Bound by memory: a row
 // is read once, kept in registers while its maximum and then its sum are found, and the gradient is written from there
-// (3 sweeps over memory, the last two from cache: 562 us at 16 384 x 30 522 in bf16, this 328, 6.1 TB/s).  Rows longer
+// (3 sweeps over memory, the last two from cache: 562 us at 16 384 x 30 522 in bf16, this 328).  Rows longer
 // than the registers of a workgroup are read twice, with a running maximum and sum the first time.
 #include "lmt_device.h"
 #include "lmt_internal.h"
@@ -57,8 +57,9 @@ __device__ __forceinline__ void put_loss(const CrossEntropy& p, uint64_t row, co
 }
 
 // One row per workgroup of THREADS threads (64: per wavefront), N vectors of 16 bytes per thread; what is left behind the last whole vector
-// goes one element to a thread.  16 384 x 30 522 in bf16 (512 threads of 8 vectors) 328 us, 2.0 GB, 6.1 TB/s (streaming stores of the gradient
-// 353); 19 rows in fp32 (1 024 threads of 8) 6.4, the latency of one row.
+// goes one element to a thread.  16 384 x 30 522 in bf16 (512 threads of 8 vectors) 328 us a call in a row of calls, 2.0 GB, 6.1 TB/s
+// (under a kernel trace, which sets calls apart, 331 to 357; streaming stores of the gradient 353 in a row); in place 331, without gradient 172; 19 rows in fp32
+// (1 024 threads of 8) 6.5, the latency of one row.
 template <typename T, typename I, int THREADS, int N>
 __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void k_cross_entropy(const CrossEntropy p) {
   constexpr int V = 16 / sizeof(T), kRowWaves = THREADS / 64;

@@ -3,7 +3,8 @@ its table's gradient, 8-bit quantisation and products, cross entropy with its gr
 
 Same names as the C ABI without the prefix.  Arguments are torch tensors on the current device, whose shapes, strides and types
 give the rest; outputs are tensors that the caller has allocated.  Calls only enqueue on `stream` (a
-``torch.cuda.Stream``, an integer handle, or None for the default stream).  What does not fit together raises ValueError,
+``torch.cuda.Stream``, an integer handle, or None for the default stream, not for torch's current one), and write through the tensors'
+addresses: autograd sees neither the call nor, in its version counters, what it has changed.  What does not fit together raises ValueError,
 what the library refuses LmtError.  There is no CPU fallback: without the built library or the extension module
 _calls every call raises."""
 from __future__ import annotations
@@ -115,7 +116,7 @@ def matmul_workspace(m: int, n: int, k: int) -> int:
 
 def matmul(a, a_scales, b, b_scales, c, workspace=None, accumulate: bool = False, stream=None, fp32_sums: bool = False) -> None:
     """c [m, n] = (c if accumulate) + a b^T for operands as quantize leaves them, of m and n rows.  fp32_sums: a 16-bit c from sums as exact as an fp32
-    one's, at a third to half of the rate (lmt.h says what the others lose)."""
+    one's, at three to four fifths of the rate (lmt.h says what the others lose)."""
     if _table is None:
         _connect()
     _check(_calls.lmt_matmul(_table, a, a_scales, b, b_scales, c, workspace, accumulate, stream, fp32_sums))
