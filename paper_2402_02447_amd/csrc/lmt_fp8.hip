@@ -8,8 +8,9 @@
 // Measured, of a result's 2-norm and whatever k: 1.5e-5 on normal numbers in e4m3 (e5m2 9e-6), up to 4e-5 where magnitudes spread over
 // e^2, a drift of 3e-6 towards zero where all terms have one sign.  A 16-bit c takes them by choice, as its own rounding is larger (2-norm
 // of it: bf16 1.7e-3, fp16 2.1e-4; one element in a hundred, or one in fifteen of an fp16 c, goes to the other neighbour) and they are up to 1.6 times
-// as fast (8 192 x 8 192 x 8 192 480 and 760 us; few rows gain 0.1 to 0.4 us, but what an element loses shall not depend on how many rows there are); with LMT_FP32_SUMS it does not.  For those and for an fp32 c operands are widened to bf16 (exactly: 3 bits of
-// mantissa and a power of two) and go through the bf16 instructions (4e-8 at k of 1 024), at 1.3 PFLOP/s from registers instead of 4.7.
+// as fast (8 192 x 8 192 x 8 192 480 and 760 us; few rows gain 0.1 to 0.4 us, but what an element loses shall not depend on how
+// many rows there are); with LMT_FP32_SUMS it does not.  For those and for an fp32 c operands are widened to bf16 (exactly, within bf16's
+// range: 3 bits of mantissa and a power of two) and go through the bf16 instructions (4e-8 at k of 1 024), at 1.3 PFLOP/s from registers instead of 4.7.
 #include "lmt_device.h"
 #include "lmt_internal.h"
 
