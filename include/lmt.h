@@ -1,5 +1,5 @@
-/* lmt.h -- operators at the two ends of a language model's training step, on one
- * MI355X (gfx950).  Part of libbca.so.
+/* lmt.h -- operators at the two ends of a language model's training step and of the
+ * attention between them, on one MI355X (gfx950).  Part of libbca.so.
  *
  * bca.h takes gradients; these make the ones of the largest tensor a BERT-shaped
  * model has, the table of word pieces that is both the input's embedding and the
@@ -11,6 +11,12 @@
  *   lmt_matmul          products of two such matrices: logits, gradients of inputs
  *                       and of weights
  *   lmt_cross_entropy   the loss of every row of logits and its gradient
+ *   lmt_linear_cross_entropy  the same from the rows and the table, with the gradients of
+ *                       both, the logits never kept as a whole
+ * and these mix the rows of sequences of unlike lengths:
+ *   lmt_rotary          queries and keys turned by their positions; its gradient
+ *   lmt_attention       attention within each sequence of a packed or padded batch
+ *   lmt_attention_grad  gradients of its queries, keys and values
  *
  * Conventions
  *   - 0 on success, negative LMT_ERR_* otherwise (nothing enqueued);
@@ -47,18 +53,24 @@ extern "C" {
 
 #define LMT_ERR_NULL (-1)      /* a required pointer is NULL                                     */
 #define LMT_ERR_ARG (-2)       /* unknown type or flag, a stride below the row's length, no classes, scale not finite */
-#define LMT_ERR_LIMIT (-3)     /* sizes beyond LMT_MAX_*                                         */
+#define LMT_ERR_LIMIT (-3)     /* sizes beyond LMT_MAX_*, or more than a launch can have         */
 #define LMT_ERR_HIP (-4)       /* a HIP runtime call failed                                      */
 #define LMT_ERR_ALIGN (-5)     /* a pointer is not aligned as it must be                         */
 #define LMT_ERR_WORKSPACE (-6) /* the workspace is smaller than the call needs                   */
 
 #define LMT_STATUS_BAD_TOKEN 1  /* a token outside [0, vocab): looked up as zeros, no gradient    */
 #define LMT_STATUS_BAD_TARGET 2 /* a target outside [0, classes) that is not the ignored one: the row counts as ignored */
+#define LMT_STATUS_BAD_SEQUENCE 4 /* starts that fall or leave the rows, or a length that reaches into the next sequence: cut to what is there */
 
 #define LMT_ACCUMULATE 1u  /* add to what the output holds                                           */
 #define LMT_TILE_SCALES 2u /* lmt_quantize: one scale for a square of 128 x 128 instead of 128 x 1     */
 #define LMT_FP32_SUMS 4u   /* lmt_matmul: a 16-bit c from sums as exact as an fp32 one's                */
+#define LMT_NEIGHBOURS 8u  /* lmt_rotary: pairs of neighbours instead of elements `pairs` apart        */
+#define LMT_INVERSE 16u    /* lmt_rotary: turns back (the gradient)                                    */
+#define LMT_CAUSAL 32u     /* attention: no position sees a later one, but for prefixes                */
 
+#define LMT_MAX_HEAD 128u         /* elements of a head                                          */
+#define LMT_MAX_HEADS 65535u
 #define LMT_MAX_ROWS 0x7fffff00u  /* tokens, vocabulary, rows, classes, m, n                     */
 #define LMT_MAX_WIDTH 0x7fffffu   /* row length of tables and of 8-bit matrices, k                 */
 
@@ -126,6 +138,76 @@ int lmt_cross_entropy(const void* logits /*DEVICE*/, int dtype, uint64_t rows, u
                       const void* targets /*DEVICE*/, int target_dtype, int64_t ignore,
                       const float* weights /*DEVICE or NULL*/, float* loss, float* lse, void* grad, uint64_t grad_ld,
                       int32_t* status, void* stream);
+
+/* lmt_cross_entropy of the logits x table^T, which are made in pieces and never kept as a whole:
+ *   l[i][j] = sum over m of x[i][m] table[j][m];  lse, loss as above;  g[i][j] = w (exp(l[i][j] - lse[i]) - [j == t])
+ *   grad_x = g table;  grad_table = (old grad_table, with LMT_ACCUMULATE) + g^T x
+ * x: [rows][x_ld], table: [classes][table_ld], both of `dtype`, LMT_F16 or LMT_BF16; rows, classes and width are up to LMT_MAX_WIDTH.  Logits, losses and
+ * sums are in fp32; elements of g are rounded to `dtype` (fp16: scaled by powers of two, so that none gets lost below its range) before
+ * they are multiplied.  loss, lse (DEVICE [rows], fp32), grad_x (of `dtype`, [rows][grad_x_ld]) and grad_table (of grad_table_dtype,
+ * `dtype` or LMT_F32, [classes][grad_table_ld]) may each be NULL.  Ignored rows take no part, whatever they hold.
+ * Infinities and NaN in a row of x or in its weight are in that row's results and in grad_table; those in a row of the table are in everything.
+ * workspace: DEVICE, 16-byte aligned, lmt_linear_cross_entropy_workspace bytes (with gradients != 0 if grad_x or grad_table is given),
+ * contents of no concern; not shared by calls that overlap in time.  Without rows a grad_table that is not added to is refused. */
+uint64_t lmt_linear_cross_entropy_workspace(uint64_t rows, uint64_t classes, uint64_t width, int gradients);
+int lmt_linear_cross_entropy(const void* x /*DEVICE*/, uint64_t x_ld, const void* table /*DEVICE*/, uint64_t table_ld, int dtype,
+                             uint64_t rows, uint64_t classes, uint64_t width, const void* targets /*DEVICE*/, int target_dtype,
+                             int64_t ignore, const float* weights /*DEVICE or NULL*/, float* loss, float* lse, void* grad_x,
+                             uint64_t grad_x_ld, void* grad_table, int grad_table_dtype, uint64_t grad_table_ld, uint32_t flags,
+                             int32_t* status, void* workspace /*DEVICE*/, uint64_t workspace_bytes, void* stream);
+
+/* Rows (tokens) of heads: element j of head h of row i is at[i * row + h * head + j], strides in elements, so that the parts
+ * of one projection's output, and heads in front of rows, are taken as they lie.  Inputs may repeat rows or heads (strides of
+ * 0); elements of outputs may not coincide.  `at` is DEVICE and aligned to an element; nothing is written through that of an input. */
+typedef struct lmt_heads {
+  void* at;
+  uint64_t row, head;
+} lmt_heads;
+
+/* The first 2 * pairs elements of every head (size elements, at most LMT_MAX_HEAD) in pairs (a, b), pair f being elements f and
+ * f + pairs, or with LMT_NEIGHBOURS 2 f and 2 f + 1:
+ *   a' = m (a cos z - b sin z),  b' = m (a sin z + b cos z),  z = positions[i] * frequencies[f], or - z with LMT_INVERSE
+ * The rest of a head is copied.  The gradient of a call is the call with the same m and the other direction.  x, out: `dtype`
+ * (LMT_F32, LMT_F16, LMT_BF16), rows x heads; out may be x itself.  positions: [rows] of LMT_I32 or LMT_I64; frequencies:
+ * [pairs], fp32, radians.  The angle is made in 64 bits, so that far positions keep theirs. */
+int lmt_rotary(const lmt_heads* x, int dtype, uint64_t rows, uint64_t heads, uint64_t size, const void* positions /*DEVICE*/,
+               int position_dtype, const float* frequencies /*DEVICE*/, uint64_t pairs, double magnitude, uint32_t flags,
+               const lmt_heads* out, void* stream);
+
+/* What attention goes by.  Sequence s has the rows from starts[s] on, lengths[s] of them or (lengths NULL) those up to starts[s + 1];
+ * starts rise from 0 or above to `rows` or below, a sequence ends before the next one begins, and both are read on the device. */
+typedef struct lmt_attend {
+  int32_t dtype;                          /* of all elements: LMT_F16 or LMT_BF16                                          */
+  uint32_t flags;                         /* LMT_CAUSAL                                                                    */
+  uint64_t rows, heads, kv_heads, size;   /* query heads h use key head h / (heads / kv_heads); size <= LMT_MAX_HEAD        */
+  uint64_t sequences;
+  const int32_t *starts /*DEVICE [sequences + 1]*/, *lengths /*DEVICE [sequences] or NULL*/;
+  const int32_t* prefixes;                /* DEVICE [sequences] or NULL, with LMT_CAUSAL: all of a sequence sees its first prefixes[s] positions */
+  const float* slopes;                    /* DEVICE [heads] or NULL                                                        */
+  double scale, cap;                      /* cap: 0 for none                                                               */
+  int32_t* status;                        /* DEVICE or NULL                                                                */
+} lmt_attend;
+
+/* For every row i and head h, over the rows j of i's sequence that it sees (all, or with LMT_CAUSAL j <= i and the prefix):
+ *   s[j] = scale * (q[i] . k[j]), then cap * tanh(s / cap) if there is a cap, then - slopes[h] * |i - j|
+ *   out[i] = sum over j of exp(s[j] - lse) v[j];  lse[h][i] = log(sum over j of exp(s[j]))
+ * q, out: rows x heads; k, v: rows x kv_heads; lse: DEVICE [heads][rows], fp32, or NULL.  Rows of no sequence, and rows all of whose
+ * scores are -Inf, get zeros and an lse of -Inf.  What a row does not see has no part in its results, whatever it holds (rows that
+ * infinities or NaN reach are computed once more, slowly).  Scores, weights' sums and outputs' sums are in fp32, the weights that multiply v
+ * are rounded to `dtype`. */
+int lmt_attention(const lmt_attend* a, const lmt_heads* q, const lmt_heads* k, const lmt_heads* v, const lmt_heads* out,
+                  float* lse, void* stream);
+
+/* Gradients of lmt_attention with respect to q, k and v from that of out.  out and lse are what lmt_attention left for the same `a`.
+ *   d[j] = p[j] (grad_out[i] . v[j] - grad_out[i] . out[i]),  p[j] = exp(s[j] - lse),  times 1 - (s / cap)^2 behind a cap
+ *   grad_q[i] = scale * sum over j of d[j] k[j];  grad_k[j] = scale * sum over i of d[j] q[i];  grad_v[j] = sum over i of p[j] grad_out[i]
+ * A key head's gradients are sums over the query heads that use it.  Rows of no sequence get zeros.  p and d are rounded to `dtype`
+ * before they are multiplied (fp16: d scaled by a power of two that follows its size).  workspace: DEVICE, 16-byte aligned, at least
+ * lmt_attention_grad_workspace bytes, contents of no concern; not shared by calls that overlap in time. */
+uint64_t lmt_attention_grad_workspace(uint64_t rows, uint64_t heads, uint64_t kv_heads, uint64_t size);
+int lmt_attention_grad(const lmt_attend* a, const lmt_heads* grad_out, const lmt_heads* q, const lmt_heads* k, const lmt_heads* v,
+                       const lmt_heads* out, const float* lse, const lmt_heads* grad_q, const lmt_heads* grad_k,
+                       const lmt_heads* grad_v, void* workspace /*DEVICE*/, uint64_t workspace_bytes, void* stream);
 
 /* Message of the calling thread's last error; valid until its next call. */
 const char* lmt_last_error(void);

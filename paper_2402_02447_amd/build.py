@@ -1,5 +1,5 @@
 """Compile libbca.so (host side + HIP kernels of the clip + optimizer path, the load-balancing simulation, and the
-operators at the two ends of a training step) for gfx950, and the extension module _calls that Python makes its compute
+operators of a language model's training step) for gfx950, and the extension module _calls that Python makes its compute
 calls through, in-tree."""
 from __future__ import annotations
 
@@ -12,7 +12,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libbca.so")
 CALLS = os.path.join(HERE, "_calls" + sysconfig.get_config_var("EXT_SUFFIX"))
-SOURCES = [os.path.join(CSRC, f) for f in ("bca_host.cpp", "bca_kernels.hip", "lbs.hip", "lmt.cpp", "lmt_embed.hip", "lmt_fp8.hip", "lmt_loss.hip")]
+SOURCES = [os.path.join(CSRC, f) for f in ("bca_host.cpp", "bca_kernels.hip", "lbs.hip", "lmt.cpp", "lmt_embed.hip", "lmt_fp8.hip", "lmt_loss.hip", "lmt_rotary.hip", "lmt_attention.hip", "lmt_linear_loss.hip")]
 
 # Packed fp32 instructions are switched off for all device code.
 HIPCC_FLAGS = [

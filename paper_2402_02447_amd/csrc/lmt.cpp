@@ -33,6 +33,44 @@ int workspace_error(const void* workspace, uint64_t given, uint64_t needed) {
   return 0;
 }
 
+// Rows of heads, as an input or as what is written: then no two elements may have one place.
+int heads_error(const char* name, const lmt_heads* x, int dtype, uint64_t rows, uint64_t heads, uint64_t size, bool written, lmt::Heads* to) {
+  if (!x || !x->at) return fail(LMT_ERR_NULL, "%s is NULL", name);
+  if (off(x->at, size_of(dtype))) return fail(LMT_ERR_ALIGN, "%s is not aligned to its element size", name);
+  const uint64_t row = rows > 1 ? x->row : 0, head = heads > 1 ? x->head : 0;  // the strides of one row, or of one head, say nothing
+  if (row > lmt::kMaxStride || head > (1ull << 46)) return fail(LMT_ERR_LIMIT, "%s: a stride is too large", name);
+  if (written) {
+    const bool rows_inside = heads <= 1 || (rows > 1 && row < head);
+    const uint64_t small = rows_inside ? row : head, count = rows_inside ? rows : heads, large = rows_inside ? head : row, of_large = rows_inside ? heads : rows;
+    if ((count > 1 && small < size) || (of_large > 1 && large < (count - 1) * small + size)) return fail(LMT_ERR_ARG, "%s: elements have one place", name);
+  }
+  *to = {x->at, row, head};
+  return 0;
+}
+
+int attend_error(const lmt_attend* a) {
+  if (!a) return fail(LMT_ERR_NULL, "what attention goes by is NULL");
+  if (a->dtype != LMT_F16 && a->dtype != LMT_BF16) return fail(LMT_ERR_ARG, "attention takes fp16 or bf16");
+  if (a->flags & ~LMT_CAUSAL) return fail(LMT_ERR_ARG, "unknown flags");
+  if (a->prefixes && !(a->flags & LMT_CAUSAL)) return fail(LMT_ERR_ARG, "prefixes without LMT_CAUSAL");
+  if (!std::isfinite((float)a->scale)) return fail(LMT_ERR_ARG, "scale is not a finite fp32 number");
+  if (!std::isfinite((float)a->cap) || a->cap < 0 || (a->cap != 0 && (float)a->cap < 1e-30f)) return fail(LMT_ERR_ARG, "cap is neither 0 nor a positive fp32 number");
+  if (a->rows > LMT_MAX_ROWS || a->sequences > LMT_MAX_ROWS || a->heads > LMT_MAX_HEADS || a->kv_heads > LMT_MAX_HEADS || a->size > LMT_MAX_HEAD)
+    return fail(LMT_ERR_LIMIT, "sizes exceed LMT_MAX_ROWS, LMT_MAX_HEADS or LMT_MAX_HEAD");
+  if (a->kv_heads == 0 ? a->heads != 0 : a->heads % a->kv_heads != 0) return fail(LMT_ERR_ARG, "the query heads are no multiple of the key heads");
+  if (lmt::attention_launches(a->rows, a->heads) > lmt::kMaxWorkgroups) return fail(LMT_ERR_LIMIT, "rows times heads are more than a launch can have");
+  if (a->sequences != 0 && !a->starts) return fail(LMT_ERR_NULL, "starts is NULL");
+  if (off(a->starts, 4) || off(a->lengths, 4) || off(a->prefixes, 4) || off(a->slopes, 4) || off(a->status, 4)) return fail(LMT_ERR_ALIGN, "a pointer is not aligned to its element size");
+  return 0;
+}
+lmt::Attention attention_of(const lmt_attend& a) {
+  lmt::Attention p = {};
+  p.starts = a.starts, p.lengths = a.lengths, p.prefixes = a.prefixes, p.slopes = a.slopes, p.status = a.status;
+  p.rows = (uint32_t)a.rows, p.heads = (uint32_t)a.heads, p.kv_heads = (uint32_t)a.kv_heads, p.group = (uint32_t)(a.heads / a.kv_heads), p.size = (uint32_t)a.size;
+  p.sequences = (uint32_t)a.sequences, p.scale = (float)a.scale, p.cap = (float)a.cap, p.causal = (a.flags & LMT_CAUSAL) != 0;
+  return p;
+}
+
 }  // namespace
 
 extern "C" {
@@ -126,6 +164,99 @@ int lmt_cross_entropy(const void* logits, int dtype, uint64_t rows, uint64_t cla
     return fail(LMT_ERR_ALIGN, "a pointer is not aligned to its element size");
   const lmt::CrossEntropy p{logits, targets, weights, loss, lse, grad, ld, grad_ld, (uint32_t)rows, (uint32_t)classes, 0, ignore, status};
   return launched("launching the loss", lmt::launch_cross_entropy(p, dtype, target_dtype, (hipStream_t)stream));
+}
+
+uint64_t lmt_linear_cross_entropy_workspace(uint64_t rows, uint64_t classes, uint64_t width, int gradients) {
+  return rows > LMT_MAX_WIDTH || classes > LMT_MAX_WIDTH || width > LMT_MAX_WIDTH ? 0 : lmt::linear_loss_workspace(rows, classes, width, gradients != 0);
+}
+
+int lmt_linear_cross_entropy(const void* x, uint64_t x_ld, const void* table, uint64_t table_ld, int dtype, uint64_t rows, uint64_t classes,
+                             uint64_t width, const void* targets, int target_dtype, int64_t ignore, const float* weights, float* loss, float* lse,
+                             void* grad_x, uint64_t grad_x_ld, void* grad_table, int grad_table_dtype, uint64_t grad_table_ld, uint32_t flags,
+                             int32_t* status, void* workspace, uint64_t workspace_bytes, void* stream) {
+  if (dtype != LMT_F16 && dtype != LMT_BF16) return fail(LMT_ERR_ARG, "x and table must be fp16 or bf16");
+  if (!is_id(target_dtype)) return fail(LMT_ERR_ARG, "targets must be LMT_I32 or LMT_I64");
+  if (grad_table && grad_table_dtype != dtype && grad_table_dtype != LMT_F32) return fail(LMT_ERR_ARG, "grad_table must be of the table's type or fp32");
+  if (flags & ~LMT_ACCUMULATE) return fail(LMT_ERR_ARG, "unknown flags");
+  if (rows > LMT_MAX_WIDTH || classes > LMT_MAX_WIDTH || width > LMT_MAX_WIDTH) return fail(LMT_ERR_LIMIT, "sizes exceed LMT_MAX_WIDTH");
+  const auto tiles = [](uint64_t a, uint64_t b) { return lmt::ceil_div(a, 64) * lmt::ceil_div(b, 64); };
+  if (tiles(rows, classes) > lmt::kMaxWorkgroups || tiles(rows, width) + tiles(classes, width) > lmt::kMaxWorkgroups)
+    return fail(LMT_ERR_LIMIT, "rows times classes, or times width, are more than a launch can have");
+  if (x_ld < width || table_ld < width || (grad_x && grad_x_ld < width) || (grad_table && grad_table_ld < width)) return fail(LMT_ERR_ARG, "a row stride is below width");
+  if (rows == 0) {  // no row has a part in the table's gradient
+    if (grad_table && !(flags & LMT_ACCUMULATE) && classes != 0 && width != 0) return fail(LMT_ERR_ARG, "no rows: a gradient of the table that is not added to would have to be cleared");
+    return 0;
+  }
+  if (classes == 0 || width == 0) return fail(LMT_ERR_ARG, "rows without classes or elements");
+  if (!x || !table || !targets) return fail(LMT_ERR_NULL, "x, table or targets is NULL");
+  if (off(x, 2) || off(table, 2) || off(grad_x, 2) || off(grad_table, size_of(grad_table_dtype)) || off(targets, size_of(target_dtype)) || off(weights, 4) || off(loss, 4) ||
+      off(lse, 4) || off(status, 4))
+    return fail(LMT_ERR_ALIGN, "a pointer is not aligned to its element size");
+  if (const int rc = workspace_error(workspace, workspace_bytes, lmt::linear_loss_workspace(rows, classes, width, grad_x || grad_table))) return rc;
+  const lmt::LinearLoss p{x, table, targets, weights, loss, lse, grad_x, grad_table, workspace, x_ld, table_ld, grad_x_ld, grad_table_ld, (uint32_t)rows, (uint32_t)classes,
+                          (uint32_t)width, target_dtype == LMT_I64, (flags & LMT_ACCUMULATE) != 0, grad_table && grad_table_dtype == LMT_F32, ignore, status};
+  return launched("launching the loss", lmt::launch_linear_loss(p, dtype, (hipStream_t)stream));
+}
+
+int lmt_rotary(const lmt_heads* x, int dtype, uint64_t rows, uint64_t heads, uint64_t size, const void* positions, int position_dtype,
+               const float* frequencies, uint64_t pairs, double magnitude, uint32_t flags, const lmt_heads* out, void* stream) {
+  if (!is_float(dtype)) return fail(LMT_ERR_ARG, "x must be fp32, fp16 or bf16");
+  if (!is_id(position_dtype)) return fail(LMT_ERR_ARG, "positions must be LMT_I32 or LMT_I64");
+  if (flags & ~(LMT_NEIGHBOURS | LMT_INVERSE)) return fail(LMT_ERR_ARG, "unknown flags");
+  if (!std::isfinite((float)magnitude)) return fail(LMT_ERR_ARG, "magnitude is not a finite fp32 number");
+  if (rows > LMT_MAX_ROWS || heads > LMT_MAX_HEADS || size > LMT_MAX_HEAD) return fail(LMT_ERR_LIMIT, "sizes exceed LMT_MAX_ROWS, LMT_MAX_HEADS or LMT_MAX_HEAD");
+  if (pairs > size / 2) return fail(LMT_ERR_ARG, "more pairs than a head has");
+  if (rows == 0 || heads == 0 || size == 0) return 0;
+  lmt::Rotary p = {};
+  if (const int rc = heads_error("x", x, dtype, rows, heads, size, false, &p.x)) return rc;
+  if (const int rc = heads_error("out", out, dtype, rows, heads, size, true, &p.out)) return rc;
+  if (p.x.at == p.out.at && (p.x.row != p.out.row || p.x.head != p.out.head)) return fail(LMT_ERR_ARG, "out in x's place must have its strides");
+  if (pairs != 0 && (!positions || !frequencies)) return fail(LMT_ERR_NULL, "positions or frequencies is NULL");
+  if (off(positions, size_of(position_dtype)) || off(frequencies, 4)) return fail(LMT_ERR_ALIGN, "a pointer is not aligned to its element size");
+  p.positions = positions, p.frequencies = frequencies, p.rows = (uint32_t)rows, p.heads = (uint32_t)heads, p.size = (uint32_t)size, p.pairs = (uint32_t)pairs;
+  p.magnitude = (float)magnitude, p.neighbours = (flags & LMT_NEIGHBOURS) != 0, p.inverse = (flags & LMT_INVERSE) != 0;
+  return launched("launching the rotary positions", lmt::launch_rotary(p, dtype, position_dtype, (hipStream_t)stream));
+}
+
+int lmt_attention(const lmt_attend* a, const lmt_heads* q, const lmt_heads* k, const lmt_heads* v, const lmt_heads* out, float* lse, void* stream) {
+  if (const int rc = attend_error(a)) return rc;
+  if (a->rows == 0 || a->heads == 0 || a->size == 0) return 0;
+  lmt::Attention p = attention_of(*a);
+  if (const int rc = heads_error("q", q, a->dtype, a->rows, a->heads, a->size, false, &p.q)) return rc;
+  if (const int rc = heads_error("k", k, a->dtype, a->rows, a->kv_heads, a->size, false, &p.k)) return rc;
+  if (const int rc = heads_error("v", v, a->dtype, a->rows, a->kv_heads, a->size, false, &p.v)) return rc;
+  if (const int rc = heads_error("out", out, a->dtype, a->rows, a->heads, a->size, true, &p.out)) return rc;
+  if (off(lse, 4)) return fail(LMT_ERR_ALIGN, "lse is not aligned to its element size");
+  p.lse = lse;
+  return launched("launching the attention", lmt::launch_attention(p, a->dtype, (hipStream_t)stream));
+}
+
+uint64_t lmt_attention_grad_workspace(uint64_t rows, uint64_t heads, uint64_t kv_heads, uint64_t size) {
+  if (rows == 0 || heads == 0 || kv_heads == 0 || size == 0 || rows > LMT_MAX_ROWS || heads > LMT_MAX_HEADS || kv_heads > heads || size > LMT_MAX_HEAD) return 0;
+  return lmt::attention_grad_workspace(rows, heads, kv_heads, size);
+}
+
+int lmt_attention_grad(const lmt_attend* a, const lmt_heads* grad_out, const lmt_heads* q, const lmt_heads* k, const lmt_heads* v, const lmt_heads* out,
+                       const float* lse, const lmt_heads* grad_q, const lmt_heads* grad_k, const lmt_heads* grad_v, void* workspace, uint64_t workspace_bytes,
+                       void* stream) {
+  if (const int rc = attend_error(a)) return rc;
+  if (a->rows == 0 || a->heads == 0 || a->size == 0) return 0;
+  lmt::Attention p = attention_of(*a);
+  const uint64_t rows = a->rows, heads = a->heads, kv_heads = a->kv_heads, size = a->size;
+  if (const int rc = heads_error("grad_out", grad_out, a->dtype, rows, heads, size, false, &p.grad_out)) return rc;
+  if (const int rc = heads_error("q", q, a->dtype, rows, heads, size, false, &p.q)) return rc;
+  if (const int rc = heads_error("k", k, a->dtype, rows, kv_heads, size, false, &p.k)) return rc;
+  if (const int rc = heads_error("v", v, a->dtype, rows, kv_heads, size, false, &p.v)) return rc;
+  if (const int rc = heads_error("out", out, a->dtype, rows, heads, size, false, &p.out)) return rc;
+  if (const int rc = heads_error("grad_q", grad_q, a->dtype, rows, heads, size, true, &p.grad_q)) return rc;
+  if (const int rc = heads_error("grad_k", grad_k, a->dtype, rows, kv_heads, size, true, &p.grad_k)) return rc;
+  if (const int rc = heads_error("grad_v", grad_v, a->dtype, rows, kv_heads, size, true, &p.grad_v)) return rc;
+  if (!lse) return fail(LMT_ERR_NULL, "lse is NULL");
+  if (off(lse, 4)) return fail(LMT_ERR_ALIGN, "lse is not aligned to its element size");
+  if (const int rc = workspace_error(workspace, workspace_bytes, lmt::attention_grad_workspace(rows, heads, kv_heads, size))) return rc;
+  p.lse = const_cast<float*>(lse);
+  p.delta = static_cast<float*>(workspace), p.part = p.delta + lmt::round_up(rows * heads, 4), p.parts = lmt::attention_parts(rows, heads, kv_heads, size);
+  return launched("launching the attention's gradient", lmt::launch_attention_grad(p, a->dtype, (hipStream_t)stream));
 }
 
 }  // extern "C"

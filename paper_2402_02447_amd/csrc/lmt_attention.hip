@@ -1,0 +1,893 @@
+// Attention within the sequences of a packed batch, and its gradient (lmt.h).
+//
+// Which rows a row sees is an interval: its sequence, cut at the row itself where it is causal, no further down than the prefix.  The same
+// holds for the rows that see a key.  So every mask is two numbers a row, a workgroup takes a block of rows whatever sequences they are of,
+// and the keys it goes over are those from the first to the last that one of its rows sees; blocks of 32 x 32 inside all rows' intervals are
+// not masked at all, those outside of a wavefront's rows not computed.
+//
+// One pass over the keys: with m a running maximum of the scores (in units of log 2), l = sum 2^(s - m) and o = sum 2^(s - m) v; when
+// a score exceeds m by more than 2^kSlack both are multiplied by 2^(m - m') first.
+//
+// Matrix instructions (32 x 32 x 16, fp32 sums): lane l gives row l % 32 of both operands, eight k from 8 (l / 32) on, and has column
+// l % 32 of the result, rows 8 g + 4 (l / 32) + r in element 4 g + r.  Scores are made as K Q^T, so that a lane has those of one query;
+// what it has of them after exp2 is, in its order, an operand of V^T P^T again: no lane needs another one's.  V^T comes from
+// LDS through the transposing read: 16 lanes read 4 rows of 16 elements, and get 4 rows' elements of a column each.
+#include "lmt_device.h"
+#include "lmt_internal.h"
+
+namespace lmt {
+namespace {
+
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+#define LMT_LDS __attribute__((address_space(3)))
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr float kInf = __builtin_inff();
+
+__device__ __forceinline__ f32x16 mma(bf16_t, const u32x4& a, const u32x4& b, const f32x16& c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x16 mma(_Float16, const u32x4& a, const u32x4& b, const f32x16& c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+}
+__device__ __forceinline__ uint32_t pack2(bf16_t, float x, float y) { return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{x, y}, bf16x2)); }
+__device__ __forceinline__ uint32_t pack2(_Float16, float x, float y) { return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{x, y}, f16x2)); }
+
+__device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
+// The other half's value of the lane 32 further, or back.
+__device__ __forceinline__ float other_half(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float((threadIdx.x & 32u) ? r[0] : r[1]);
+}
+__device__ __forceinline__ bool any(bool x) { return __builtin_amdgcn_ballot_w64(x) != 0; }
+__device__ __forceinline__ int wave_min(int x) {
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) x = min(x, __shfl_xor(x, d));
+  return __builtin_amdgcn_readfirstlane(x);
+}
+__device__ __forceinline__ float wave_max(float x) {
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) x = fmaxf(x, __shfl_xor(x, d));
+  return x;
+}
+__device__ __forceinline__ float wave_sum(float x) {
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) x += __shfl_xor(x, d);
+  return x;
+}
+
+// ---- who sees whom -----------------------------------------------------------------------
+
+// Of kRows rows in a row: the interval of what each sees (or, of keys: of who sees it), [lo, hi), 0 and 0 for nothing; and where all of them lie.
+template <int ROWS>
+struct Seen {
+  int lo[ROWS], hi[ROWS], first, last;
+};
+
+// The sequence of a row is the last one that starts at or before it.  Sequences that start in the block mark their first row, one more
+// pass takes the running maximum; with many sequences the range that can matter is narrowed by a sample of them first.
+template <int ROWS, int THREADS, bool KEYS>
+__device__ __forceinline__ void find_seen(const Attention& p, uint32_t block_row, Seen<ROWS>& s) {
+  static_assert(ROWS <= 128 && ROWS <= THREADS && ROWS % 64 == 0, "a thread a row, at most two wavefronts of them");
+  const int t = (int)threadIdx.x, r0 = (int)block_row, r1 = r0 + ROWS;
+  const LMT_GLOBAL int32_t* starts = (const LMT_GLOBAL int32_t*)p.starts;
+  if (t < ROWS) s.lo[t] = -1;
+  if (t == 0) s.first = 0x7fffffff, s.last = 0;
+  __syncthreads();
+  uint32_t begin = 0, end = p.sequences;
+  while (end - begin > 2u * THREADS) {
+    const uint32_t step = (end - begin + THREADS - 1u) / THREADS, at = begin + (uint32_t)t * step;
+    const int start = at < end ? starts[at] : 0x7fffffff;
+    const uint32_t below = (uint32_t)__syncthreads_count(start <= r0), inside = (uint32_t)__syncthreads_count(start < r1);
+    const uint32_t b = begin + (below ? below - 1u : 0u) * step, e = min(end, begin + inside * step);
+    if (e <= b || e - b >= end - begin) {
+      if (e <= b) end = begin;
+      break;
+    }
+    begin = b, end = e;
+  }
+  for (uint32_t q = begin + (uint32_t)t; q < end; q += THREADS) {
+    const int start = starts[q];
+    if (start < r1) atomicMax(&s.lo[start <= r0 ? 0 : start - r0], (int)q);
+  }
+  __syncthreads();
+  int of = -1, before = -1;
+  if (t < ROWS) {
+    of = s.lo[t];
+    if (t >= 64) before = s.lo[t - 64];
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+      const int x = __shfl_up(of, d);
+      if ((t & 63) >= d) of = max(of, x);
+      before = max(before, __shfl_xor(before, d));
+    }
+    of = max(of, before);
+  }
+  __syncthreads();
+  if (t < ROWS) {
+    const int i = r0 + t, rows = (int)p.rows;
+    int lo = 0, hi = 0;
+    if (of >= 0 && i < rows) {
+      const int start = max(starts[of], 0), next = min(starts[of + 1], rows);
+      int length = max(next - start, 0);
+      if (p.lengths) length = min(length, max(((const LMT_GLOBAL int32_t*)p.lengths)[of], 0));
+      const int stop = start + length;
+      if (i < stop) {
+        const int prefix = p.causal && p.prefixes ? start + min(max(((const LMT_GLOBAL int32_t*)p.prefixes)[of], 0), length) : start;
+        if constexpr (KEYS) lo = p.causal && i >= prefix ? i : start, hi = stop;
+        else lo = start, hi = p.causal ? max(i + 1, prefix) : stop;
+        atomicMin(&s.first, lo), atomicMax(&s.last, hi);
+      }
+    }
+    s.lo[t] = lo, s.hi[t] = hi;
+  }
+  __syncthreads();
+}
+
+// One workgroup of a call looks the table over.
+__device__ __forceinline__ void check_sequences(const Attention& p) {
+  if (!p.status || blockIdx.x != 0) return;
+  const LMT_GLOBAL int32_t* starts = (const LMT_GLOBAL int32_t*)p.starts;
+  const int rows = (int)p.rows;
+  bool bad = false;
+  for (uint32_t s = threadIdx.x; s < p.sequences; s += blockDim.x) {
+    const int a = starts[s], b = starts[s + 1u];
+    bad |= a < 0 || b < a || b > rows;
+    if (p.lengths) {
+      const int n = ((const LMT_GLOBAL int32_t*)p.lengths)[s];
+      bad |= n < 0 || (int64_t)a + n > b;
+    }
+  }
+  if (bad) atomicOr(p.status, LMT_STATUS_BAD_SEQUENCE);
+}
+
+// A lane's row among what its wavefront and block see.
+struct Span {
+  int lo, hi;                              // of the lane's row
+  int any_lo, any_hi, all_lo, all_hi;      // what some row of the wavefront sees, what all that see anything do
+  template <int ROWS>
+  __device__ __forceinline__ void read(const Seen<ROWS>& s, uint32_t row) {
+    lo = s.lo[row], hi = s.hi[row];
+    const bool some = lo < hi;
+    any_lo = wave_min(some ? lo : 0x7fffffff), any_hi = -wave_min(some ? -hi : 0);
+    all_lo = -wave_min(some ? -lo : 0), all_hi = wave_min(some ? hi : 0x7fffffff);
+  }
+  __device__ __forceinline__ bool touches(int at, int n) const { return at < any_hi && at + n > any_lo; }
+  __device__ __forceinline__ bool inside(int at, int n) const { return at >= all_lo && at + n <= all_hi; }
+};
+
+// ---- tiles ----------------------------------------------------------------------------------
+
+// 16 bytes of a row from element 8 * piece on, zeros behind its end.
+template <typename T>
+__device__ __forceinline__ u32x4 load_piece(const T* row, uint32_t piece, uint32_t size) {
+  Vec<T, 8> v;
+  v.w[0] = v.w[1] = v.w[2] = v.w[3] = 0;
+  if (piece * 8u + 8u <= size) load<false>(v, row + piece * 8u);
+  else if (piece * 8u < size) load_end(v, row + piece * 8u, size - piece * 8u, 0.f);
+  return u32x4{v.w[0], v.w[1], v.w[2], v.w[3]};
+}
+template <typename T>
+__device__ __forceinline__ const T* head_of(const Heads& x, uint32_t head) {
+  return static_cast<const T*>(x.at) + (uint64_t)head * x.head;
+}
+template <typename T>
+__device__ __forceinline__ const T* row_of(const T* head, const Heads& x, uint32_t row) {
+  return head + (uint64_t)row * (uint32_t)x.row;
+}
+
+// kTile rows of D elements in LDS.  The 16-byte pieces of a row change places by the row's number: reads of one piece of 16 rows and
+// transposing reads of four rows then meet every bank once.
+constexpr int kTile = 64;
+template <int D>
+__device__ __forceinline__ uint32_t turn(uint32_t row) {
+  if constexpr (D == 64) return (row >> 1 & 1u) << 2 | (row >> 2 & 1u) << 1 | (row >> 3 & 1u);
+  else return (row & 3u) << 2 | (row >> 2 & 3u);
+}
+template <typename T, int D, int THREADS>
+struct Stage {
+  static constexpr int pieces = D / 8, loads = kTile * pieces / THREADS, step = THREADS / pieces;
+  u32x4 w[loads];
+  // Rows behind the last one are the last one again: nobody sees them.
+  __device__ __forceinline__ void fetch(const T* head, const Heads& x, uint32_t first, uint32_t rows, uint32_t size) {
+    const uint32_t piece = threadIdx.x % pieces, r = first + threadIdx.x / pieces;
+#pragma unroll
+    for (int j = 0; j < loads; ++j) w[j] = load_piece(row_of(head, x, min(r + j * step, rows - 1u)), piece, size);
+  }
+  __device__ __forceinline__ void put(uint8_t* tile) const {
+    const uint32_t piece = threadIdx.x % pieces, r = threadIdx.x / pieces;
+#pragma unroll
+    for (int j = 0; j < loads; ++j) *reinterpret_cast<u32x4*>(tile + (r + j * step) * (D * 2) + (piece ^ turn<D>(r + j * step)) * 16u) = w[j];
+  }
+};
+// A lane's own row in registers, as an operand for all of k = 0 .. D - 1.
+template <typename T, int D>
+struct Row {
+  u32x4 w[D / 16];
+  __device__ __forceinline__ void read(const T* row, uint32_t size) {
+    const uint32_t half = (threadIdx.x & 63u) >> 5;
+#pragma unroll
+    for (int c = 0; c < D / 16; ++c) w[c] = load_piece(row, 2 * c + half, size);
+  }
+};
+// Rows of a tile as operands: along the row (k is the element), and across (k is the row).
+template <int D>
+struct Along {
+  uint32_t at[D / 16];
+  __device__ __forceinline__ void set() {
+    const uint32_t lane = threadIdx.x & 63u, row = lane & 31u;
+#pragma unroll
+    for (uint32_t c = 0; c < D / 16; ++c) at[c] = row * (D * 2) + ((2u * c + (lane >> 5)) ^ turn<D>(row)) * 16u;
+  }
+  __device__ __forceinline__ u32x4 read(const uint8_t* tile, int sub, int c) const { return *reinterpret_cast<const u32x4*>(tile + sub * 32 * (D * 2) + at[c]); }
+};
+template <int D>
+struct Across {
+  uint32_t at[D / 32][2];
+  __device__ __forceinline__ void set() {
+    const uint32_t lane = threadIdx.x & 63u, i = lane & 15u, col = 16u * (lane >> 4 & 1u) + 4u * (i & 3u);
+#pragma unroll
+    for (uint32_t d = 0; d < D / 32; ++d)
+#pragma unroll
+      for (uint32_t e = 0; e < 2; ++e) {
+        const uint32_t row = 8u * e + 4u * (lane >> 5) + i / 4u;
+        at[d][e] = row * (D * 2) + ((d * 32u + col) / 8u ^ turn<D>(row)) * 16u + (i & 1u) * 8u;
+      }
+  }
+  // Elements 32 d + l % 32 of the rows that a lane has of a score's column in elements 8 c .. 8 c + 7.
+  __device__ __forceinline__ u32x4 read(const uint8_t* tile, int sub, int c, int d) const {
+    const uint8_t* from = tile + (sub * 32 + c * 16) * (D * 2);
+    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LMT_LDS s16x4*)(from + at[d][0]));
+    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LMT_LDS s16x4*)(from + at[d][1]));
+    const u32x2 a = __builtin_bit_cast(u32x2, lo), b = __builtin_bit_cast(u32x2, hi);
+    return u32x4{a.x, a.y, b.x, b.y};
+  }
+};
+// Column of scores as an operand.
+template <typename T>
+__device__ __forceinline__ u32x4 packed(const f32x16& x, int c) {
+  return u32x4{pack2(T{}, x[8 * c], x[8 * c + 1]), pack2(T{}, x[8 * c + 2], x[8 * c + 3]), pack2(T{}, x[8 * c + 4], x[8 * c + 5]), pack2(T{}, x[8 * c + 6], x[8 * c + 7])};
+}
+// Sums whose column is the lane's row and whose rows are its elements, times `by`, to memory: the halves of a wavefront change places
+// with what the other one has, so that each lane writes 8 neighbours.
+template <typename T, int D>
+__device__ __forceinline__ void store_row(T* row, const f32x16 (&x)[D / 32], float by, uint32_t size, bool here) {
+  const uint32_t half = (threadIdx.x & 63u) >> 5;
+#pragma unroll
+  for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      uint32_t w[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w[i] = pack2(T{}, x[d][8 * c + 2 * i] * by, x[d][8 * c + 2 * i + 1] * by);
+      const auto a = __builtin_amdgcn_permlane32_swap(w[0], w[2], false, false), b = __builtin_amdgcn_permlane32_swap(w[1], w[3], false, false);
+      Vec<T, 8> v;
+      v.w[0] = a[0], v.w[1] = b[0], v.w[2] = a[1], v.w[3] = b[1];
+      const uint32_t from = 32u * d + 16u * c + 8u * half;
+      if (here) {
+        if (from + 8u <= size) store<false>(row + from, v);
+        else if (from < size) store_end(row + from, v, size - from);
+      }
+    }
+}
+__device__ __forceinline__ bool finite(float x) { return __builtin_fabsf(x) < kInf; }
+template <int D>
+__device__ __forceinline__ bool finite(const f32x16 (&x)[D / 32]) {
+  float top = 0;
+#pragma unroll
+  for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) top = __builtin_fmaf(x[d][i], 0.f, top);  // 0, or NaN
+  return top == 0.f;
+}
+
+// ---- scores -----------------------------------------------------------------------------------
+
+// A score in units of log 2 from a product.  PLAIN: scale > 0 alone; otherwise any scale, a cap and a slope.
+// tanh(x) = 1 - 2 / (e^2x + 1), and by its series where that would cancel: up to 0.3 its terms to x^9 leave 5e-8.
+struct Score {
+  float by, cap, to_cap, slope;  // by: scale * log2(e);  cap, slope: in units of log 2;  to_cap: scale / the cap
+  __device__ __forceinline__ void set(const Attention& p, uint32_t head) {
+    by = p.scale * kLog2e, cap = p.cap * kLog2e, to_cap = p.cap != 0.f ? p.scale / p.cap : 0.f;
+    slope = p.slopes ? load1(p.slopes + head) * kLog2e : 0.f;
+  }
+  static __device__ __forceinline__ float tanh_of(float x) {
+    const float y = x * x;
+    float s = __builtin_fmaf(y, 0.021869488536f, -0.053968253968f);
+    s = __builtin_fmaf(s, y, 0.133333333333f), s = __builtin_fmaf(s, y, -0.333333333333f);
+    s = __builtin_fmaf(s * y, x, x);
+    const float e = exp2_of(__builtin_fabsf(x) * (2.f * kLog2e)), t = 1.f - 2.f * __builtin_amdgcn_rcpf(e + 1.f);
+    return __builtin_fabsf(x) < 0.3f ? s : __builtin_copysignf(t, x);
+  }
+  // apart: |i - j|; bend: what the cap multiplies derivatives by.
+  __device__ __forceinline__ float of(float x, int apart, float* bend = nullptr) const {
+    float y = x * by;
+    if (cap != 0.f) {
+      const float t = tanh_of(x * to_cap);
+      y = cap * t;
+      if (bend) *bend = __builtin_fmaf(-t, t, 1.f);
+    } else if (bend) {
+      *bend = 1.f;
+    }
+    return __builtin_fmaf(-slope, (float)apart, y);
+  }
+};
+
+template <typename T>
+__device__ __forceinline__ float dot(const T* x, const T* y, uint32_t size) {
+  float s = 0;
+  for (uint32_t d = 0; d < size; ++d) s = __builtin_fmaf(to_f32(load1(x + d)), to_f32(load1(y + d)), s);
+  return s;
+}
+
+// fp16's range: weights are at most 2^kSlack, and 2^kShift times as large in fp16, so that the small ones lose fewer bits.
+constexpr float kSlack = 8.f;
+template <typename T>
+constexpr float kShift = 0.f;
+template <>
+constexpr float kShift<_Float16> = 7.f;
+
+// Which head and block of rows a workgroup has.  XCD x, which takes every eighth workgroup, gets an eighth of the list, so that its L2 sees
+// one head's keys again and again; causal: long rows first.
+__device__ __forceinline__ void place(uint32_t tiles, uint32_t lists, bool backwards, uint32_t* tile, uint32_t* list) {
+  constexpr uint32_t kXcds = 8;
+  const uint32_t n = tiles * lists, x = blockIdx.x % kXcds, share = n / kXcds, extra = n % kXcds, id = x * share + min(x, extra) + blockIdx.x / kXcds;
+  *list = id / tiles, *tile = id % tiles;
+  if (backwards) *tile = tiles - 1u - *tile;
+}
+
+// ---- forward ------------------------------------------------------------------------------------
+
+// One row, a wavefront: only of what the row sees, so that infinities and NaN elsewhere stay there.
+template <typename T>
+__device__ __forceinline__ void attend_row(const Attention& p, uint32_t head, uint32_t kv, uint32_t i, int lo, int hi) {
+  const uint32_t lane = threadIdx.x & 63u;
+  const T *k = head_of<T>(p.k, kv), *v = head_of<T>(p.v, kv), *q = row_of(head_of<T>(p.q, head), p.q, i);
+  Score score;
+  score.set(p, head);
+  float m = -kInf, l = 0, o[2] = {};
+  for (int j0 = lo; j0 < hi; j0 += 64) {
+    const int j = j0 + (int)lane;
+    float s = -kInf;
+    if (j < hi) s = score.of(dot(q, row_of(k, p.k, (uint32_t)j), p.size), abs((int)i - j));
+    const float top = fmaxf(m, wave_max(s)), base = top == -kInf ? 0.f : top;
+    const float w = j < hi ? exp2_of(s - base) : 0.f, by = m == -kInf ? 0.f : exp2_of(m - base);
+    m = top, l = __builtin_fmaf(l, by, wave_sum(w)), o[0] *= by, o[1] *= by;
+    for (int n = 0; n < min(64, hi - j0); ++n) {
+      const float x = __shfl(w, n);
+      const T* row = row_of(v, p.v, (uint32_t)(j0 + n));
+#pragma unroll
+      for (uint32_t e = 0; e < 2; ++e)
+        if (lane + 64u * e < p.size) o[e] = __builtin_fmaf(x, to_f32(load1(row + lane + 64u * e)), o[e]);
+    }
+  }
+  T* out = const_cast<T*>(row_of(head_of<T>(p.out, head), p.out, i));
+#pragma unroll
+  for (uint32_t e = 0; e < 2; ++e)
+    if (lane + 64u * e < p.size) store1(out + lane + 64u * e, from_f32<T>(l == 0.f ? 0.f : o[e] / l));
+  if (p.lse && lane == 0) store1(p.lse + (uint64_t)head * p.rows + i, l == 0.f ? -kInf : (m + __builtin_amdgcn_logf(l)) * kLn2);
+}
+
+template <typename T, int D, bool PLAIN, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, 2) void k_attend(const Attention p, uint32_t tiles) {
+  constexpr int ROWS = 32 * WAVES, THREADS = 64 * WAVES;
+  __shared__ __align__(16) uint8_t keys[2][kTile * D * 2], values[2][kTile * D * 2];
+  __shared__ Seen<ROWS> seen;
+  uint32_t tile, head;
+  place(tiles, p.heads, p.causal, &tile, &head);
+  const uint32_t kv = head / p.group, wave = threadIdx.x >> 6, lane = threadIdx.x & 63u, row = wave * 32u + (lane & 31u), i = tile * ROWS + row;
+  const T *k = head_of<T>(p.k, kv), *v = head_of<T>(p.v, kv);
+  check_sequences(p);
+  Row<T, D> q;
+  q.read(row_of(head_of<T>(p.q, head), p.q, min(i, p.rows - 1u)), p.size);
+  find_seen<ROWS, THREADS, false>(p, tile * ROWS, seen);
+  Span span;
+  span.read(seen, row);
+  const int first = seen.first, last = seen.last;
+  Score score;
+  score.set(p, head);
+  Along<D> along;
+  Across<D> across;
+  along.set(), across.set();
+  float m = -kInf, l = 0;
+  f32x16 o[D / 32] = {};
+  Stage<T, D, THREADS> next_k, next_v;
+  if (first < last) {
+    next_k.fetch(k, p.k, (uint32_t)first, p.rows, p.size), next_v.fetch(v, p.v, (uint32_t)first, p.rows, p.size);
+    next_k.put(keys[0]), next_v.put(values[0]);
+  }
+  __syncthreads();
+  uint32_t now = 0;
+  for (int at = first; at < last; at += kTile, now ^= 1u) {
+    const bool more = at + kTile < last;
+    if (more) next_k.fetch(k, p.k, (uint32_t)(at + kTile), p.rows, p.size), next_v.fetch(v, p.v, (uint32_t)(at + kTile), p.rows, p.size);
+    if (span.touches(at, kTile)) {
+      f32x16 s[2] = {};
+#pragma unroll
+      for (int c = 0; c < D / 16; ++c)
+#pragma unroll
+        for (int b = 0; b < 2; ++b) s[b] = mma(T{}, along.read(keys[now], b, c), q.w[c], s[b]);
+      const int j0 = at + 4 * (int)(lane >> 5);
+      if constexpr (!PLAIN) {
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) s[b][e] = score.of(s[b][e], abs(j0 + 32 * b + 8 * (e / 4) + e % 4 - (int)i));
+      }
+      if (!span.inside(at, kTile)) {
+        const uint32_t from = (uint32_t)(j0 - span.lo), n = (uint32_t)(span.hi - span.lo);
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) s[b][e] = from + (uint32_t)(32 * b + 8 * (e / 4) + e % 4) < n ? s[b][e] : -kInf;
+      }
+      float top = s[0][0];
+#pragma unroll
+      for (int e = 1; e < 32; ++e) top = fmaxf(top, s[e / 16][e % 16]);
+      top = fmaxf(top, other_half(top));
+      if constexpr (PLAIN) top *= score.by;
+      if (any(top > m + kSlack)) {
+        const float up = fmaxf(m, top), by = m == -kInf ? 0.f : exp2_of(m - up);
+        m = up, l *= by;
+#pragma unroll
+        for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) o[d][e] *= by;
+      }
+      const float base = (m == -kInf ? 0.f : m) - kShift<T>;
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          s[b][e] = exp2_of(PLAIN ? __builtin_fmaf(s[b][e], score.by, -base) : s[b][e] - base);
+          l += s[b][e];
+        }
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          const u32x4 w = packed<T>(s[b], c);
+#pragma unroll
+          for (int d = 0; d < D / 32; ++d) o[d] = mma(T{}, across.read(values[now], b, c, d), w, o[d]);
+        }
+    }
+    if (more) next_k.put(keys[now ^ 1u]), next_v.put(values[now ^ 1u]);
+    __syncthreads();
+  }
+  l += other_half(l);
+  const bool some = span.lo < span.hi, here = i < p.rows;
+  const bool again = some && !(finite<D>(o) && finite(l));
+  const uint64_t rows_again = __builtin_amdgcn_ballot_w64(again);
+  const uint32_t redo = (uint32_t)rows_again | (uint32_t)(rows_again >> 32);
+  const bool mine = here && !(redo >> (lane & 31u) & 1u);
+  if (!some || l == 0.f) {
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d) o[d] = f32x16{};
+    l = 0.f;
+  }
+  store_row<T, D>(const_cast<T*>(row_of(head_of<T>(p.out, head), p.out, min(i, p.rows - 1u))), o, l == 0.f ? 0.f : 1.f / l, p.size, mine);
+  if (p.lse && mine && lane < 32u) store1(p.lse + (uint64_t)head * p.rows + i, l == 0.f ? -kInf : (m - kShift<T> + __builtin_amdgcn_logf(l)) * kLn2);
+  for (uint32_t left = redo; left; left &= left - 1u) {
+    const uint32_t r = wave * 32u + (uint32_t)__builtin_ctz(left);
+    attend_row<T>(p, head, kv, tile * ROWS + r, seen.lo[r], seen.hi[r]);
+  }
+}
+
+// ---- gradient -------------------------------------------------------------------------------------
+
+// What a wavefront's d are multiplied by before they are rounded to fp16: a power of two that brings the largest so far to 2^14 or below.  The sums
+// follow when it changes.  bf16 has fp32's range.
+template <typename T>
+struct Range {
+  float by = 1.f;
+  __device__ __forceinline__ void begin() {
+    if constexpr (sizeof(T) == 2 && kShift<T> != 0.f) by = 0x1p60f;
+  }
+  // True if x, times by, are too large: then `by` is smaller, x and the sums have followed.
+  template <int N, int M>
+  __device__ __forceinline__ void fit(f32x16 (&x)[N], f32x16 (&sums)[M]) {
+    if constexpr (kShift<T> != 0.f) {
+      float top = 0;
+#pragma unroll
+      for (int b = 0; b < N; ++b)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) top = fmaxf(top, __builtin_fabsf(x[b][e]));
+      if (any(top > 0x1p15f)) {
+        top = wave_max(top);
+        if (!(top < kInf)) top = 0x1p15f;  // it goes wrong anyway, and is computed once more
+        const float down = __uint_as_float((127u + 14u + 127u - (__float_as_uint(top) >> 23)) << 23);
+        by *= down;
+#pragma unroll
+        for (int b = 0; b < N; ++b) x[b] *= down;
+#pragma unroll
+        for (int b = 0; b < M; ++b) sums[b] *= down;
+      }
+    }
+  }
+};
+
+// Row i's gradient of q, a wavefront.
+template <typename T>
+__device__ __forceinline__ void grad_q_row(const Attention& p, uint32_t head, uint32_t kv, uint32_t i, int lo, int hi, float lse, float delta) {
+  const uint32_t lane = threadIdx.x & 63u;
+  const T *k = head_of<T>(p.k, kv), *v = head_of<T>(p.v, kv), *q = row_of(head_of<T>(p.q, head), p.q, i), *go = row_of(head_of<T>(p.grad_out, head), p.grad_out, i);
+  Score score;
+  score.set(p, head);
+  float sum[2] = {};
+  for (int j0 = lo; j0 < hi; j0 += 64) {
+    const int j = j0 + (int)lane;
+    float d = 0;
+    if (j < hi) {
+      float bend;
+      const float s = score.of(dot(q, row_of(k, p.k, (uint32_t)j), p.size), abs((int)i - j), &bend);
+      d = exp2_of(s - lse) * (dot(go, row_of(v, p.v, (uint32_t)j), p.size) - delta) * bend;
+    }
+    for (int n = 0; n < min(64, hi - j0); ++n) {
+      const float x = __shfl(d, n);
+      const T* row = row_of(k, p.k, (uint32_t)(j0 + n));
+#pragma unroll
+      for (uint32_t e = 0; e < 2; ++e)
+        if (lane + 64u * e < p.size) sum[e] = __builtin_fmaf(x, to_f32(load1(row + lane + 64u * e)), sum[e]);
+    }
+  }
+  T* to = const_cast<T*>(row_of(head_of<T>(p.grad_q, head), p.grad_q, i));
+#pragma unroll
+  for (uint32_t e = 0; e < 2; ++e)
+    if (lane + 64u * e < p.size) store1(to + lane + 64u * e, from_f32<T>(sum[e] * p.scale));
+}
+
+// lse in units of log 2, as what is subtracted from scores: a row without weights has none.
+__device__ __forceinline__ float subtracted(float lse) { return lse == -kInf ? kInf : lse * kLog2e; }
+
+// Gradient of q and, for the next kernel, delta = grad_out . out of every row: as the forward pass, scores and products with v from a tile of each, d into the
+// sums with k across.
+template <typename T, int D, bool PLAIN, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, 2) void k_attend_grad_q(const Attention p, uint32_t tiles) {
+  constexpr int ROWS = 32 * WAVES, THREADS = 64 * WAVES;
+  __shared__ __align__(16) uint8_t keys[2][kTile * D * 2], values[2][kTile * D * 2];
+  __shared__ Seen<ROWS> seen;
+  uint32_t tile, head;
+  place(tiles, p.heads, p.causal, &tile, &head);
+  const uint32_t kv = head / p.group, wave = threadIdx.x >> 6, lane = threadIdx.x & 63u, row = wave * 32u + (lane & 31u), i = tile * ROWS + row, held = min(i, p.rows - 1u);
+  const T *k = head_of<T>(p.k, kv), *v = head_of<T>(p.v, kv);
+  check_sequences(p);
+  Row<T, D> q, go;
+  q.read(row_of(head_of<T>(p.q, head), p.q, held), p.size), go.read(row_of(head_of<T>(p.grad_out, head), p.grad_out, held), p.size);
+  float delta = 0;
+  {
+    Row<T, D> out;
+    out.read(row_of(head_of<T>(p.out, head), p.out, held), p.size);
+#pragma unroll
+    for (int c = 0; c < D / 16; ++c) {
+      const Vec<T, 8> a = __builtin_bit_cast(Vec<T, 8>, out.w[c]), b = __builtin_bit_cast(Vec<T, 8>, go.w[c]);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) delta = __builtin_fmaf(a.get(e), b.get(e), delta);
+    }
+    delta += other_half(delta);
+  }
+  const float lse = subtracted(load1(p.lse + (uint64_t)head * p.rows + held));
+  find_seen<ROWS, THREADS, false>(p, tile * ROWS, seen);
+  Span span;
+  span.read(seen, row);
+  const bool some = span.lo < span.hi;
+  if (i < p.rows && lane < 32u) store1(p.delta + (uint64_t)head * p.rows + i, delta);
+  const int first = seen.first, last = seen.last;
+  Score score;
+  score.set(p, head);
+  Along<D> along;
+  Across<D> across;
+  along.set(), across.set();
+  Range<T> range;
+  range.begin();
+  f32x16 sum[D / 32] = {};
+  Stage<T, D, THREADS> next_k, next_v;
+  if (first < last) {
+    next_k.fetch(k, p.k, (uint32_t)first, p.rows, p.size), next_v.fetch(v, p.v, (uint32_t)first, p.rows, p.size);
+    next_k.put(keys[0]), next_v.put(values[0]);
+  }
+  __syncthreads();
+  uint32_t now = 0;
+  for (int at = first; at < last; at += kTile, now ^= 1u) {
+    const bool more = at + kTile < last;
+    if (more) next_k.fetch(k, p.k, (uint32_t)(at + kTile), p.rows, p.size), next_v.fetch(v, p.v, (uint32_t)(at + kTile), p.rows, p.size);
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      const int at_b = at + 32 * b;
+      if (!span.touches(at_b, 32)) continue;
+      f32x16 s[1] = {}, dp = {};
+#pragma unroll
+      for (int c = 0; c < D / 16; ++c) {
+        s[0] = mma(T{}, along.read(keys[now], b, c), q.w[c], s[0]);
+        dp = mma(T{}, along.read(values[now], b, c), go.w[c], dp);
+      }
+      const int j0 = at_b + 4 * (int)(lane >> 5);
+      const bool inside = span.inside(at_b, 32);
+      const uint32_t from = (uint32_t)(j0 - span.lo), n = (uint32_t)(span.hi - span.lo);
+      const float less = delta * range.by;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        float bend = 1.f, w;
+        if constexpr (PLAIN) w = exp2_of(__builtin_fmaf(s[0][e], score.by, -lse));
+        else w = exp2_of(score.of(s[0][e], abs(j0 + 8 * (e / 4) + e % 4 - (int)i), &bend) - lse);
+        float d = __builtin_fmaf(dp[e], range.by, -less) * w;
+        if constexpr (!PLAIN) d *= bend;
+        s[0][e] = d;
+      }
+      if (!inside) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) s[0][e] = from + (uint32_t)(8 * (e / 4) + e % 4) < n ? s[0][e] : 0.f;
+      }
+      range.fit(s, sum);
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        const u32x4 w = packed<T>(s[0], c);
+#pragma unroll
+        for (int d = 0; d < D / 32; ++d) sum[d] = mma(T{}, across.read(keys[now], b, c, d), w, sum[d]);
+      }
+    }
+    if (more) next_k.put(keys[now ^ 1u]), next_v.put(values[now ^ 1u]);
+    __syncthreads();
+  }
+  const uint64_t rows_again = __builtin_amdgcn_ballot_w64(some && !finite<D>(sum));
+  const uint32_t redo = (uint32_t)rows_again | (uint32_t)(rows_again >> 32);
+  if (!some) {
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d) sum[d] = f32x16{};
+  }
+  store_row<T, D>(const_cast<T*>(row_of(head_of<T>(p.grad_q, head), p.grad_q, held)), sum, p.scale / range.by, p.size, i < p.rows && !(redo >> (lane & 31u) & 1u));
+  for (uint32_t left = redo; left; left &= left - 1u) {
+    const int b = __builtin_ctz(left);
+    const uint32_t r = wave * 32u + (uint32_t)b;
+    grad_q_row<T>(p, head, kv, tile * ROWS + r, seen.lo[r], seen.hi[r], __shfl(lse, b), __shfl(delta, b));
+  }
+}
+
+// Where the gradients of a key go: the tensors, or a part's sums.
+template <typename T, int D>
+__device__ __forceinline__ void store_key(const Attention& p, const Heads& to, float* part, uint32_t kv, uint32_t j, const f32x16 (&x)[D / 32], float by, bool here) {
+  if (p.parts == 1u) {
+    store_row<T, D>(const_cast<T*>(row_of(head_of<T>(to, kv), to, min(j, p.rows - 1u))), x, by, p.size, here);
+    return;
+  }
+  if (!here) return;
+  float* row = part + ((uint64_t)kv * p.rows + j) * D + 4u * ((threadIdx.x & 63u) >> 5);
+#pragma unroll
+  for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+    for (int g = 0; g < 4; ++g)
+      *(LMT_GLOBAL f32x4*)(row + 32 * d + 8 * g) = f32x4{x[d][4 * g] * by, x[d][4 * g + 1] * by, x[d][4 * g + 2] * by, x[d][4 * g + 3] * by};
+}
+
+// Key j's gradients from query heads [h0, h1), a wavefront.
+template <typename T, int D>
+__device__ __forceinline__ void grad_kv_row(const Attention& p, uint32_t kv, uint32_t h0, uint32_t h1, uint32_t j, int lo, int hi, float* part_k, float* part_v) {
+  const uint32_t lane = threadIdx.x & 63u;
+  const T *k = row_of(head_of<T>(p.k, kv), p.k, j), *v = row_of(head_of<T>(p.v, kv), p.v, j);
+  float dk[2] = {}, dv[2] = {};
+  for (uint32_t head = h0; head < h1; ++head) {
+    const T *q = head_of<T>(p.q, head), *go = head_of<T>(p.grad_out, head);
+    Score score;
+    score.set(p, head);
+    for (int i0 = lo; i0 < hi; i0 += 64) {
+      const int i = i0 + (int)lane;
+      float w = 0, d = 0;
+      if (i < hi) {
+        float bend;
+        const uint64_t at = (uint64_t)head * p.rows + (uint32_t)i;
+        w = exp2_of(score.of(dot(row_of(q, p.q, (uint32_t)i), k, p.size), abs(i - (int)j), &bend) - subtracted(load1(p.lse + at)));
+        d = w * (dot(row_of(go, p.grad_out, (uint32_t)i), v, p.size) - load1(p.delta + at)) * bend;
+      }
+      for (int n = 0; n < min(64, hi - i0); ++n) {
+        const float x = __shfl(d, n), y = __shfl(w, n);
+        const T *a = row_of(q, p.q, (uint32_t)(i0 + n)), *b = row_of(go, p.grad_out, (uint32_t)(i0 + n));
+#pragma unroll
+        for (uint32_t e = 0; e < 2; ++e)
+          if (lane + 64u * e < p.size) {
+            dk[e] = __builtin_fmaf(x, to_f32(load1(a + lane + 64u * e)), dk[e]);
+            dv[e] = __builtin_fmaf(y, to_f32(load1(b + lane + 64u * e)), dv[e]);
+          }
+      }
+    }
+  }
+#pragma unroll
+  for (uint32_t e = 0; e < 2; ++e) {
+    const uint32_t c = lane + 64u * e;
+    if (c >= p.size) continue;
+    if (p.parts == 1u) {
+      store1(const_cast<T*>(row_of(head_of<T>(p.grad_k, kv), p.grad_k, j)) + c, from_f32<T>(dk[e] * p.scale));
+      store1(const_cast<T*>(row_of(head_of<T>(p.grad_v, kv), p.grad_v, j)) + c, from_f32<T>(dv[e]));
+    } else {
+      store1(part_k + ((uint64_t)kv * p.rows + j) * D + c, dk[e] * p.scale);
+      store1(part_v + ((uint64_t)kv * p.rows + j) * D + c, dv[e]);
+    }
+  }
+}
+
+// Gradients of k and v: a lane has a key, the rows that see it come by in tiles, for one query head after the other.  Scores as Q K^T, so that
+// what a lane has of them is an operand of dO^T P and Q^T d.
+template <typename T, int D, bool PLAIN, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, D == 64 ? 2 : 1) void k_attend_grad_kv(const Attention p, uint32_t tiles) {
+  constexpr int ROWS = 32 * WAVES, THREADS = 64 * WAVES;
+  __shared__ __align__(16) uint8_t queries[2][kTile * D * 2], grads[2][kTile * D * 2];
+  __shared__ __align__(16) float lse[2][kTile], delta[2][kTile];
+  __shared__ Seen<ROWS> seen;
+  uint32_t tile, list;
+  place(tiles, p.kv_heads * p.parts, false, &tile, &list);
+  const uint32_t kv = list / p.parts, part = list % p.parts, h0 = kv * p.group + part * p.group / p.parts, h1 = kv * p.group + (part + 1u) * p.group / p.parts;
+  const uint32_t wave = threadIdx.x >> 6, lane = threadIdx.x & 63u, row = wave * 32u + (lane & 31u), j = tile * ROWS + row, held = min(j, p.rows - 1u);
+  Row<T, D> k, v;
+  k.read(row_of(head_of<T>(p.k, kv), p.k, held), p.size), v.read(row_of(head_of<T>(p.v, kv), p.v, held), p.size);
+  find_seen<ROWS, THREADS, true>(p, tile * ROWS, seen);
+  Span span;
+  span.read(seen, row);
+  const int first = seen.first, last = seen.last;
+  Along<D> along;
+  Across<D> across;
+  along.set(), across.set();
+  Range<T> range;
+  range.begin();
+  f32x16 dk[D / 32] = {}, dv[D / 32] = {};
+  Stage<T, D, THREADS> next_q, next_go;
+  float next_lse = 0, next_delta = 0;
+  const auto fetch = [&](uint32_t head, int at) {
+    next_q.fetch(head_of<T>(p.q, head), p.q, (uint32_t)at, p.rows, p.size), next_go.fetch(head_of<T>(p.grad_out, head), p.grad_out, (uint32_t)at, p.rows, p.size);
+    if (threadIdx.x < kTile) {
+      const uint64_t from = (uint64_t)head * p.rows + min((uint32_t)at + threadIdx.x, p.rows - 1u);
+      next_lse = load1(p.lse + from), next_delta = load1(p.delta + from);
+    }
+  };
+  const auto put = [&](uint32_t to) {
+    next_q.put(queries[to]), next_go.put(grads[to]);
+    if (threadIdx.x < kTile) lse[to][threadIdx.x] = subtracted(next_lse), delta[to][threadIdx.x] = next_delta;
+  };
+  if (first < last) fetch(h0, first), put(0);
+  __syncthreads();
+  uint32_t now = 0;
+  for (uint32_t head = h0; first < last && head < h1; ++head) {
+    Score score;
+    score.set(p, head);
+    for (int at = first; at < last; at += kTile, now ^= 1u) {
+      const bool wrap = at + kTile >= last, more = !wrap || head + 1u < h1;
+      if (more) fetch(wrap ? head + 1u : head, wrap ? first : at + kTile);
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        const int at_b = at + 32 * b;
+        if (!span.touches(at_b, 32)) continue;
+        f32x16 s = {}, d[1] = {};
+#pragma unroll
+        for (int c = 0; c < D / 16; ++c) {
+          s = mma(T{}, along.read(queries[now], b, c), k.w[c], s);
+          d[0] = mma(T{}, along.read(grads[now], b, c), v.w[c], d[0]);
+        }
+        const int half = 4 * (int)(lane >> 5), i0 = at_b + half;
+        const bool inside = span.inside(at_b, 32);
+        const uint32_t from = (uint32_t)(i0 - span.lo), n = (uint32_t)(span.hi - span.lo);
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const f32x4 less = *reinterpret_cast<const f32x4*>(&lse[now][32 * b + 8 * g + half]), dot_out = *reinterpret_cast<const f32x4*>(&delta[now][32 * b + 8 * g + half]);
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const int e = 4 * g + r;
+            float bend = 1.f, w;
+            if constexpr (PLAIN) w = exp2_of(__builtin_fmaf(s[e], score.by, -less[r]));
+            else w = exp2_of(score.of(s[e], abs(i0 + 8 * g + r - (int)j), &bend) - less[r]);
+            float x = __builtin_fmaf(d[0][e], range.by, -dot_out[r] * range.by) * w;
+            if constexpr (!PLAIN) x *= bend;
+            s[e] = w, d[0][e] = x;
+          }
+        }
+        if (!inside) {
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const bool in = from + (uint32_t)(8 * (e / 4) + e % 4) < n;
+            s[e] = in ? s[e] : 0.f, d[0][e] = in ? d[0][e] : 0.f;
+          }
+        }
+        range.fit(d, dk);
+        if constexpr (kShift<T> != 0.f) s *= 0x1p14f;  // weights are at most 1
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          const u32x4 w = packed<T>(s, c), x = packed<T>(d[0], c);
+#pragma unroll
+          for (int e = 0; e < D / 32; ++e) {
+            dv[e] = mma(T{}, across.read(grads[now], b, c, e), w, dv[e]);
+            dk[e] = mma(T{}, across.read(queries[now], b, c, e), x, dk[e]);
+          }
+        }
+      }
+      if (more) put(now ^ 1u);
+      __syncthreads();
+    }
+  }
+  const bool some = span.lo < span.hi;
+  const uint64_t rows_again = __builtin_amdgcn_ballot_w64(some && !(finite<D>(dk) && finite<D>(dv)));
+  const uint32_t redo = (uint32_t)rows_again | (uint32_t)(rows_again >> 32);
+  if (!some) {
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d) dk[d] = dv[d] = f32x16{};
+  }
+  const bool mine = j < p.rows && !(redo >> (lane & 31u) & 1u);
+  float *part_k = p.part + (uint64_t)part * 2u * p.kv_heads * p.rows * D, *part_v = part_k + (uint64_t)p.kv_heads * p.rows * D;
+  store_key<T, D>(p, p.grad_k, part_k, kv, j, dk, p.scale / range.by, mine);
+  store_key<T, D>(p, p.grad_v, part_v, kv, j, dv, kShift<T> != 0.f ? 0x1p-14f : 1.f, mine);
+  for (uint32_t left = redo; left; left &= left - 1u) {
+    const uint32_t r = wave * 32u + (uint32_t)__builtin_ctz(left);
+    grad_kv_row<T, D>(p, kv, h0, h1, tile * ROWS + r, seen.lo[r], seen.hi[r], part_k, part_v);
+  }
+}
+
+// Adds the parts' sums in order: a thread 8 elements of a key.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void k_attend_join(const Attention p) {
+  const uint64_t n = (uint64_t)2 * p.kv_heads * p.rows * (D / 8), of = (uint64_t)blockIdx.x * 256u + threadIdx.x;
+  if (of >= n) return;
+  const uint32_t piece = (uint32_t)(of % (D / 8));
+  if (piece * 8u >= p.size) return;
+  const uint64_t key = of / (D / 8), j = key % p.rows, kv = key / p.rows % p.kv_heads;
+  float x[8] = {};
+  for (uint32_t part = 0; part < p.parts; ++part) {
+    const float* from = p.part + (uint64_t)part * 2u * p.kv_heads * p.rows * D + of * 8u;
+    const f32x4 a = *(const LMT_GLOBAL f32x4*)from, b = *(const LMT_GLOBAL f32x4*)(from + 4);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] += a[e], x[4 + e] += b[e];
+  }
+  const Heads& to = key / p.rows < p.kv_heads ? p.grad_k : p.grad_v;
+  T* row = const_cast<T*>(row_of(head_of<T>(to, (uint32_t)kv), to, (uint32_t)j)) + piece * 8u;
+  Vec<T, 8> v;
+  v.set(x);
+  if (piece * 8u + 8u <= p.size) store<false>(row, v);
+  else store_end(row, v, p.size - piece * 8u);
+}
+
+constexpr int kWaves = 4;
+
+template <typename F>
+hipError_t with_form(const Attention& p, int dtype, F f) {
+  const bool plain = p.cap == 0.f && !p.slopes && p.scale > 0.f;
+  const auto sized = [&](auto t, auto wide) {
+    if (plain) return f(t, wide, std::true_type{});
+    return f(t, wide, std::false_type{});
+  };
+  const auto typed = [&](auto t) {
+    if (p.size <= 64u) return sized(t, std::integral_constant<int, 64>{});
+    return sized(t, std::integral_constant<int, 128>{});
+  };
+  return dtype == LMT_F16 ? typed(_Float16{}) : typed(bf16_t{});
+}
+
+}  // namespace
+
+uint32_t attention_parts(uint64_t, uint64_t, uint64_t, uint64_t) { return 1; }
+
+uint64_t attention_grad_workspace(uint64_t rows, uint64_t heads, uint64_t kv_heads, uint64_t size) {
+  const uint64_t parts = attention_parts(rows, heads, kv_heads, size);
+  return round_up(4 * rows * heads, 16) + (parts > 1 ? 8 * parts * kv_heads * rows * (size <= 64 ? 64 : 128) : 0);
+}
+
+uint64_t attention_launches(uint64_t rows, uint64_t heads) { return ceil_div(rows, 32 * kWaves) * heads; }
+
+hipError_t launch_attention(const Attention& p, int dtype, hipStream_t s) {
+  return with_form(p, dtype, [&](auto t, auto d, auto plain) {
+    const uint32_t tiles = (uint32_t)ceil_div(p.rows, 32 * kWaves);
+    hipLaunchKernelGGL((k_attend<decltype(t), decltype(d)::value, decltype(plain)::value, kWaves>), dim3(tiles * p.heads), dim3(64 * kWaves), 0, s, p, tiles);
+    return hipGetLastError();
+  });
+}
+
+hipError_t launch_attention_grad(const Attention& p, int dtype, hipStream_t s) {
+  return with_form(p, dtype, [&](auto t, auto d, auto plain) {
+    const uint32_t tiles = (uint32_t)ceil_div(p.rows, 32 * kWaves);
+    hipLaunchKernelGGL((k_attend_grad_q<decltype(t), decltype(d)::value, decltype(plain)::value, kWaves>), dim3(tiles * p.heads), dim3(64 * kWaves), 0, s, p, tiles);
+    hipLaunchKernelGGL((k_attend_grad_kv<decltype(t), decltype(d)::value, decltype(plain)::value, kWaves>), dim3(tiles * p.kv_heads * p.parts), dim3(64 * kWaves), 0, s, p, tiles);
+    if (p.parts > 1u)
+      hipLaunchKernelGGL((k_attend_join<decltype(t), decltype(d)::value>), dim3((uint32_t)ceil_div((uint64_t)2 * p.kv_heads * p.rows * (decltype(d)::value / 8), 256)), dim3(256), 0, s, p);
+    return hipGetLastError();
+  });
+}
+
+}  // namespace lmt

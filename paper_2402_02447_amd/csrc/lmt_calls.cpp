@@ -15,6 +15,10 @@ struct Functions {
   decltype(&lmt_quantize) quantize;
   decltype(&lmt_matmul) matmul;
   decltype(&lmt_cross_entropy) cross_entropy;
+  decltype(&lmt_linear_cross_entropy) linear_cross_entropy;
+  decltype(&lmt_rotary) rotary;
+  decltype(&lmt_attention) attention;
+  decltype(&lmt_attention_grad) attention_grad;
   PyObject *types, *current_device;  // {dtype: LMT_* or kBytes}; the device that is current, as a callable
 };
 constexpr int kBytes = 7;  // 8-bit whole numbers: scales, workspaces
@@ -102,6 +106,49 @@ struct Args {
     Py_XDECREF(shape), Py_XDECREF(stride), Py_XDECREF(dtype), Py_XDECREF(where), Py_XDECREF(at);
     return ok;
   }
+  // Rows of heads: three dimensions, any strides between rows and heads.
+  struct Heads : lmt_heads {
+    int type = -1;
+    uint64_t rows = 0, heads = 0, size = 0;
+    bool like(const Heads& x) const { return type == x.type && rows == x.rows && heads == x.heads && size == x.size; }
+  };
+  void heads(const char* name, Heads* t) {
+    t->at = nullptr, t->row = t->head = 0;
+    if (!ok) return;
+    PyObject* x = a[i++];
+    if (x == Py_None) return refuse(name, "a tensor is wanted, not None");
+    PyObject* shape = PyObject_GetAttr(x, s_shape);
+    PyObject* stride = shape ? PyObject_CallMethodNoArgs(x, s_stride) : nullptr;
+    PyObject* dtype = stride ? PyObject_GetAttr(x, s_dtype) : nullptr;
+    PyObject* where = dtype ? PyObject_CallMethodNoArgs(x, s_get_device) : nullptr;
+    PyObject* at = where ? PyObject_CallMethodNoArgs(x, s_data_ptr) : nullptr;
+    ok = at != nullptr;
+    if (ok) {
+      PyObject* type = PyDict_GetItemWithError(f->types, dtype);
+      const long place = PyLong_AsLong(where);
+      t->at = (void*)(uintptr_t)PyLong_AsUnsignedLongLongMask(at);
+      int64_t size[3], step[3];
+      if (PyErr_Occurred()) {
+        ok = false;
+      } else if (!PyTuple_Check(shape) || !PyTuple_Check(stride) || PyTuple_GET_SIZE(shape) != 3 || PyTuple_GET_SIZE(stride) != 3) {
+        refuse(name, "three dimensions are wanted");
+      } else if (!type) {
+        refuse(name, "not a type that is taken");
+      } else if (place < 0) {
+        refuse(name, "not on a GPU");
+      } else if (device >= 0 && place != device) {
+        refuse(name, "not on the device that the others are on");
+      } else {
+        device = place;
+        t->type = (int)PyLong_AsLong(type);
+        ok = numbers(shape, 3, size) && numbers(stride, 3, step);
+        need(size[2] <= 1 || step[2] == 1, name, "elements of a head have to lie one behind the other");
+        need(step[0] >= 0 && step[1] >= 0, name, "strides below 0");
+        if (ok) t->rows = (uint64_t)size[0], t->heads = (uint64_t)size[1], t->size = (uint64_t)size[2], t->row = (uint64_t)step[0], t->head = (uint64_t)step[1];
+      }
+    }
+    Py_XDECREF(shape), Py_XDECREF(stride), Py_XDECREF(dtype), Py_XDECREF(where), Py_XDECREF(at);
+  }
   void matrix(const char* name, Tensor* t) {
     if (tensor(name, 2, t)) need(t->type == LMT_F32 || t->type == LMT_F16 || t->type == LMT_BF16, name, "fp32, fp16 or bf16 is wanted");
   }
@@ -166,6 +213,14 @@ struct Args {
     Py_XDECREF(number);
     ok = !PyErr_Occurred();
     return s;
+  }
+  template <typename P, typename F>
+  PyObject* call(P there, F go) {
+    if (ok && !there) {
+      PyErr_SetString(PyExc_TypeError, "connected without this function");
+      return nullptr;
+    }
+    return call(go);
   }
   template <typename F>
   PyObject* call(F go) {
@@ -271,20 +326,135 @@ PyObject* call_cross_entropy(PyObject*, PyObject* const* args, Py_ssize_t n) {
   });
 }
 
+// lmt_linear_cross_entropy(functions, x, table, targets, workspace, loss, lse, grad_x, grad_table, weights, ignore, accumulate, status, stream)
+PyObject* call_linear_cross_entropy(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  Args a(args, n, 14);
+  Tensor x, table, targets, gx, gt;
+  uint64_t bytes;
+  a.matrix("x", &x), a.matrix("table", &table), a.ids("targets", &targets);
+  void* workspace = a.workspace(&bytes);
+  float* loss = static_cast<float*>(a.vector("loss", LMT_F32, x.rows()));
+  float* lse = static_cast<float*>(a.vector("lse", LMT_F32, x.rows()));
+  const bool has_x = a.tensor("grad_x", 2, &gx, true), has_table = a.tensor("grad_table", 2, &gt, true);
+  const float* weights = static_cast<float*>(a.vector("weights", LMT_F32, x.rows()));
+  const int64_t ignore = a.number();
+  const uint32_t flags = a.truth() ? LMT_ACCUMULATE : 0u;
+  int32_t* status = static_cast<int32_t*>(a.vector("status", LMT_I32, 1));
+  void* s = a.stream();
+  a.need(table.type == x.type && table.cols() == x.cols(), "table", "x's type and rows as long as x's are wanted");
+  a.need(targets.cols() == x.rows(), "targets", "one for every row is wanted");
+  a.need(!has_x || (gx.type == x.type && gx.rows() == x.rows() && gx.cols() == x.cols()), "grad_x", "x's type and shape are wanted");
+  a.need(!has_table || ((gt.type == x.type || gt.type == LMT_F32) && gt.rows() == table.rows() && gt.cols() == table.cols()), "grad_table", "the table's shape, and its type or fp32, are wanted");
+  return a.call(a.ok ? a.f->linear_cross_entropy : nullptr, [&] {
+    return a.f->linear_cross_entropy(x.at, x.ld(), table.at, table.ld(), x.type, x.rows(), table.rows(), x.cols(), targets.at, targets.type, ignore, weights, loss, lse, gx.at, gx.ld(), gt.at,
+                                     has_table ? gt.type : x.type, gt.ld(), flags, status, workspace, bytes, s);
+  });
+}
+
+// lmt_rotary(functions, x, positions, frequencies, out, neighbours, magnitude, inverse, stream)
+PyObject* call_rotary(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  Args a(args, n, 9);
+  Args::Heads x, out;
+  Tensor positions, frequencies;
+  a.heads("x", &x), a.ids("positions", &positions);
+  if (a.tensor("frequencies", 1, &frequencies)) a.need(frequencies.type == LMT_F32, "frequencies", "fp32 is wanted");
+  a.heads("out", &out);
+  uint32_t flags = a.truth() ? LMT_NEIGHBOURS : 0u;
+  const double magnitude = a.real();
+  if (a.truth()) flags |= LMT_INVERSE;
+  void* s = a.stream();
+  a.need(positions.cols() == x.rows, "positions", "one for every row is wanted");
+  a.need(out.like(x), "out", "x's type and shape are wanted");
+  return a.call(a.ok ? a.f->rotary : nullptr, [&] {
+    return a.f->rotary(&x, x.type, x.rows, x.heads, x.size, positions.at, positions.type, static_cast<float*>(frequencies.at), frequencies.cols(), magnitude, flags, &out, s);
+  });
+}
+
+// starts, lengths, prefixes, slopes, scale, cap, causal, status
+void masks(Args& a, const Args::Heads& q, const Args::Heads& k, lmt_attend* to) {
+  Tensor starts;
+  if (a.tensor("starts", 1, &starts)) a.need(starts.type == LMT_I32 && starts.cols() >= 1, "starts", "32-bit whole numbers, one more than there are sequences, are wanted");
+  const uint64_t sequences = starts.cols() - 1u;
+  const auto each = [&](const char* name, int type, uint64_t n) -> void* {
+    Tensor t;
+    if (!a.tensor(name, 1, &t, true)) return nullptr;
+    a.need(t.type == type, name, type == LMT_F32 ? "fp32 is wanted" : "32-bit whole numbers are wanted");
+    a.need(t.cols() == n, name, "has another number of elements");
+    return t.at;
+  };
+  to->starts = static_cast<int32_t*>(starts.at), to->sequences = sequences;
+  to->lengths = static_cast<int32_t*>(each("lengths", LMT_I32, sequences)), to->prefixes = static_cast<int32_t*>(each("prefixes", LMT_I32, sequences));
+  to->slopes = static_cast<float*>(each("slopes", LMT_F32, q.heads));
+  to->scale = a.real(), to->cap = a.real();
+  to->flags = a.truth() ? LMT_CAUSAL : 0u;
+  to->status = static_cast<int32_t*>(a.vector("status", LMT_I32, 1));
+  to->dtype = q.type, to->rows = q.rows, to->heads = q.heads, to->kv_heads = k.heads, to->size = q.size;
+}
+void keys(Args& a, const Args::Heads& q, const Args::Heads& k, const Args::Heads& v) {
+  a.need(q.type == LMT_F16 || q.type == LMT_BF16, "q", "fp16 or bf16 is wanted");
+  a.need(k.type == q.type && k.rows == q.rows && k.size == q.size, "k", "q's type, rows and head size are wanted");
+  a.need(v.like(k), "v", "k's type and shape are wanted");
+}
+// The rows of lse are the heads.
+void* lse_of(Args& a, const Args::Heads& q, bool may_be_none) {
+  Tensor t;
+  if (!a.tensor("lse", 2, &t, may_be_none)) return nullptr;
+  a.need(t.type == LMT_F32 && t.rows() == q.heads && t.cols() == q.rows && t.ld() == t.cols(), "lse", "fp32, a row without gaps for every head, is wanted");
+  return t.at;
+}
+
+// lmt_attention(functions, q, k, v, out, lse, starts, lengths, prefixes, slopes, scale, cap, causal, status, stream)
+PyObject* call_attention(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  Args a(args, n, 15);
+  Args::Heads q, k, v, out;
+  lmt_attend by = {};
+  a.heads("q", &q), a.heads("k", &k), a.heads("v", &v), a.heads("out", &out);
+  float* lse = static_cast<float*>(lse_of(a, q, true));
+  masks(a, q, k, &by);
+  void* s = a.stream();
+  keys(a, q, k, v);
+  a.need(out.like(q), "out", "q's type and shape are wanted");
+  return a.call(a.ok ? a.f->attention : nullptr, [&] { return a.f->attention(&by, &q, &k, &v, &out, lse, s); });
+}
+
+// lmt_attention_grad(functions, grad_out, q, k, v, out, lse, grad_q, grad_k, grad_v, workspace, starts, lengths, prefixes, slopes, scale, cap, causal, status, stream)
+PyObject* call_attention_grad(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  Args a(args, n, 20);
+  Args::Heads go, q, k, v, out, gq, gk, gv;
+  lmt_attend by = {};
+  uint64_t bytes;
+  a.heads("grad_out", &go), a.heads("q", &q), a.heads("k", &k), a.heads("v", &v), a.heads("out", &out);
+  const float* lse = static_cast<float*>(lse_of(a, q, false));
+  a.heads("grad_q", &gq), a.heads("grad_k", &gk), a.heads("grad_v", &gv);
+  void* workspace = a.workspace(&bytes);
+  masks(a, q, k, &by);
+  void* s = a.stream();
+  keys(a, q, k, v);
+  a.need(go.like(q), "grad_out", "q's type and shape are wanted");
+  a.need(out.like(q), "out", "q's type and shape are wanted");
+  a.need(gq.like(q), "grad_q", "q's type and shape are wanted");
+  a.need(gk.like(k), "grad_k", "k's type and shape are wanted");
+  a.need(gv.like(k), "grad_v", "k's type and shape are wanted");
+  return a.call(a.ok ? a.f->attention_grad : nullptr, [&] { return a.f->attention_grad(&by, &go, &q, &k, &v, &out, lse, &gq, &gk, &gv, workspace, bytes, s); });
+}
+
 void release(PyObject* capsule) {
   Functions* f = static_cast<Functions*>(PyCapsule_GetPointer(capsule, "lmt.functions"));
   Py_XDECREF(f->types), Py_XDECREF(f->current_device);
   PyMem_Free(f);
 }
 
-// lmt_connect(addresses of the five functions in the order of Functions, types, current_device) -> what every call takes first
+// lmt_connect(addresses of the functions in the order of Functions, types, current_device) -> what every call takes first.  The first five are what
+// a caller has who does without the others.
+constexpr int kFunctions = 9, kFewest = 5;
 PyObject* connect(PyObject*, PyObject* const* args, Py_ssize_t n) {
-  if (n != 7 || !PyDict_Check(args[5]) || !PyCallable_Check(args[6])) {
-    PyErr_SetString(PyExc_TypeError, "five addresses, a dict and a callable are wanted");
+  const Py_ssize_t given = n - 2;
+  if ((given != kFunctions && given != kFewest) || !PyDict_Check(args[given]) || !PyCallable_Check(args[given + 1])) {
+    PyErr_SetString(PyExc_TypeError, "nine or five addresses, a dict and a callable are wanted");
     return nullptr;
   }
-  void* at[5];
-  for (int i = 0; i < 5; ++i) {
+  void* at[kFunctions] = {};
+  for (int i = 0; i < given; ++i) {
     at[i] = (void*)(uintptr_t)PyLong_AsUnsignedLongLong(args[i]);
     if (PyErr_Occurred()) return nullptr;
   }
@@ -292,8 +462,9 @@ PyObject* connect(PyObject*, PyObject* const* args, Py_ssize_t n) {
   if (!f) return PyErr_NoMemory();
   f->embed = (decltype(f->embed))at[0], f->embed_grad = (decltype(f->embed_grad))at[1];
   f->quantize = (decltype(f->quantize))at[2], f->matmul = (decltype(f->matmul))at[3];
-  f->cross_entropy = (decltype(f->cross_entropy))at[4];
-  f->types = args[5], f->current_device = args[6];
+  f->cross_entropy = (decltype(f->cross_entropy))at[4], f->linear_cross_entropy = (decltype(f->linear_cross_entropy))at[5];
+  f->rotary = (decltype(f->rotary))at[6], f->attention = (decltype(f->attention))at[7], f->attention_grad = (decltype(f->attention_grad))at[8];
+  f->types = args[given], f->current_device = args[given + 1];
   PyObject* capsule = PyCapsule_New(f, "lmt.functions", release);
   if (!capsule) {
     PyMem_Free(f);
@@ -305,7 +476,8 @@ PyObject* connect(PyObject*, PyObject* const* args, Py_ssize_t n) {
 
 #define METHOD(name, function) {name, (PyCFunction)(void (*)(void))function, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {METHOD("lmt_connect", connect), METHOD("lmt_embed", call_embed), METHOD("lmt_embed_grad", call_embed_grad), METHOD("lmt_quantize", call_quantize),
-                         METHOD("lmt_matmul", call_matmul), METHOD("lmt_cross_entropy", call_cross_entropy), {nullptr, nullptr, 0, nullptr}};
+                         METHOD("lmt_matmul", call_matmul), METHOD("lmt_cross_entropy", call_cross_entropy), METHOD("lmt_linear_cross_entropy", call_linear_cross_entropy),
+                         METHOD("lmt_rotary", call_rotary), METHOD("lmt_attention", call_attention), METHOD("lmt_attention_grad", call_attention_grad), {nullptr, nullptr, 0, nullptr}};
 
 }  // namespace
 

@@ -1,4 +1,5 @@
-// Between the argument checks (lmt.cpp) and the kernels' launches (lmt_embed.hip, lmt_fp8.hip, lmt_loss.hip) of lmt.h.
+// Between the argument checks (lmt.cpp) and the kernels' launches (lmt_embed.hip, lmt_fp8.hip, lmt_loss.hip, lmt_rotary.hip,
+// lmt_attention.hip, lmt_linear_loss.hip) of lmt.h.
 // Launchers take checked arguments, only enqueue, and return the last HIP error.
 #ifndef LMT_INTERNAL_H_
 #define LMT_INTERNAL_H_
@@ -72,6 +73,53 @@ struct CrossEntropy {
   int32_t* status;
 };
 hipError_t launch_cross_entropy(const CrossEntropy& p, int dtype, int target_dtype, hipStream_t s);
+
+struct Heads {  // lmt_heads
+  void* at;
+  uint64_t row, head;
+};
+
+struct Rotary {
+  Heads x, out;
+  const void* positions;
+  const float* frequencies;
+  uint32_t rows, heads, size, pairs;
+  float magnitude;
+  bool neighbours, inverse;
+};
+hipError_t launch_rotary(const Rotary& p, int dtype, int position_dtype, hipStream_t s);
+
+struct Attention {
+  Heads q, k, v, out, grad_out, grad_q, grad_k, grad_v;
+  float *lse, *delta, *part;  // delta: [heads][rows]; part: sums of parts of a key head's query heads
+  const int32_t *starts, *lengths, *prefixes;
+  const float* slopes;
+  int32_t* status;
+  uint32_t rows, heads, kv_heads, group, parts, size, sequences;  // group: query heads of a key head
+  float scale, cap;
+  bool causal;
+};
+constexpr uint64_t kMaxStride = 0x7fffffffu;    // between rows, in elements
+constexpr uint64_t kMaxWorkgroups = 0x7fffffu;  // of up to 512 threads: a launch has fewer than 2^32 threads
+uint64_t attention_launches(uint64_t rows, uint64_t heads);  // workgroups of the largest launch
+uint32_t attention_parts(uint64_t rows, uint64_t heads, uint64_t kv_heads, uint64_t size);
+uint64_t attention_grad_workspace(uint64_t rows, uint64_t heads, uint64_t kv_heads, uint64_t size);
+hipError_t launch_attention(const Attention& p, int dtype, hipStream_t s);
+hipError_t launch_attention_grad(const Attention& p, int dtype, hipStream_t s);
+
+struct LinearLoss {
+  const void *x, *table, *targets;
+  const float* weights;
+  float *loss, *lse;
+  void *grad_x, *grad_table, *workspace;
+  uint64_t x_ld, table_ld, grad_x_ld, grad_table_ld;
+  uint32_t rows, classes, width;
+  bool wide_targets, accumulate, grad_table_f32;
+  int64_t ignore;
+  int32_t* status;
+};
+uint64_t linear_loss_workspace(uint64_t rows, uint64_t classes, uint64_t width, bool gradients);
+hipError_t launch_linear_loss(const LinearLoss& p, int dtype, hipStream_t s);
 
 }  // namespace lmt
 #endif  // LMT_INTERNAL_H_

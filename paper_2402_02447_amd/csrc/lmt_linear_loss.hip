@@ -1,0 +1,556 @@
+// Cross entropy of x table^T without the logits, and the gradients of both (lmt.h).
+//
+// Logits are made twice.  The first time each tile leaves its rows' maxima and sums of exponentials, which are joined to a maximum and a sum a
+// row; the second time, a piece of the classes at a time, tiles become g = softmax - onehot in 16 bits, as rows and as columns, which are multiplied by
+// the transposed table (grad_x, summed over the pieces) and the transposed x (grad_table).  Four products where three would do with the logits
+// in memory; what is kept instead is one piece of g, 2 x 2 bytes an element.
+#include "lmt_device.h"
+#include "lmt_internal.h"
+#include "lmt_tiles.h"
+
+namespace lmt {
+namespace {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f, kInf = __builtin_inff();
+
+__device__ __forceinline__ f32x16 mma(bf16_t, const u32x4& a, const u32x4& b, const f32x16& c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x16 mma(_Float16, const u32x4& a, const u32x4& b, const f32x16& c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+}
+__device__ __forceinline__ float other_half(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float((threadIdx.x & 32u) ? r[0] : r[1]);
+}
+
+// What the second pass knows of a row.  target: -1 for rows that are not counted.
+struct RowOf {
+  float top, log_sum, weight;  // log_sum: of the sum of exp(x - top), in units of log 2
+  int target;
+};
+
+// ---- transposes and padded copies ---------------------------------------------------------
+
+// A matrix by squares of 64 x 64: its copy with rows of whole blocks of 64, zeros behind their end, its transpose likewise, or both.
+struct Lay {
+  const void* from;
+  uint64_t ld;
+  uint32_t rows, cols, tiles_across, tiles;
+  void *copy, *turned;  // either may be nullptr
+};
+__device__ __forceinline__ int target_of(const void* targets, bool wide, uint64_t i, int64_t ignore, uint32_t classes, bool* bad) {
+  const int64_t t = wide ? id_at<int64_t>(targets, i) : id_at<int32_t>(targets, i);
+  *bad = t != ignore && (t < 0 || t >= (int64_t)classes);
+  return t == ignore || *bad ? -1 : (int)t;
+}
+// Rows of x that are not counted are zeros in its transpose.
+template <typename T>
+__global__ __launch_bounds__(256) void k_lay(const Lay x, const Lay table, const LinearLoss p, uint32_t* largest) {
+  __shared__ uint16_t square[64][66];
+  const bool of_x = blockIdx.x < x.tiles;
+  const Lay& a = of_x ? x : table;
+  if (blockIdx.x == 0 && threadIdx.x == 0) *largest = 0;
+  const uint32_t tile = of_x ? blockIdx.x : blockIdx.x - x.tiles, r0 = tile / a.tiles_across * 64u, c0 = tile % a.tiles_across * 64u;
+  const uint32_t r = threadIdx.x / 8u, c = c0 + threadIdx.x % 8u * 8u;
+  const uint64_t row_out = round_up(a.cols, 64), row_turned = round_up(a.rows, 64);
+#pragma unroll
+  for (uint32_t k = 0; k < 2; ++k) {
+    const uint32_t i = r0 + r + 32u * k;
+    Vec<T, 8> v;
+    v.w[0] = v.w[1] = v.w[2] = v.w[3] = 0;
+    if (i < a.rows && c < a.cols) {
+      const T* from = static_cast<const T*>(a.from) + (uint64_t)i * a.ld + c;
+      if (c + 8u <= a.cols) load<false>(v, from);
+      else load_end(v, from, a.cols - c, 0.f);
+    }
+    if (a.copy && i < a.rows) *(LMT_GLOBAL u32x4*)(static_cast<T*>(a.copy) + i * row_out + c) = u32x4{v.w[0], v.w[1], v.w[2], v.w[3]};
+    bool bad;
+    const bool none = of_x && i < a.rows && target_of(p.targets, p.wide_targets, i, p.ignore, p.classes, &bad) < 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) square[r + 32u * k][threadIdx.x % 8u * 8u + e] = none ? (uint16_t)0 : (uint16_t)(v.w[e / 2] >> (16 * (e & 1)));
+  }
+  if (!a.turned) return;
+  __syncthreads();
+#pragma unroll
+  for (uint32_t k = 0; k < 2; ++k) {
+    const uint32_t j = r + 32u * k;  // a column of the square
+    uint32_t w[4];
+#pragma unroll
+    for (uint32_t e = 0; e < 4; ++e) w[e] = (uint32_t)square[threadIdx.x % 8u * 8u + 2 * e][j] | (uint32_t)square[threadIdx.x % 8u * 8u + 2 * e + 1][j] << 16;
+    if (c0 + j < a.cols) *(LMT_GLOBAL u32x4*)(static_cast<T*>(a.turned) + (c0 + j) * row_turned + r0 + threadIdx.x % 8u * 8u) = u32x4{w[0], w[1], w[2], w[3]};
+  }
+}
+
+// ---- products -------------------------------------------------------------------------------
+
+// c[i][j] = sum over k of a[i][k] b[j][k]: rows of both in whole blocks of 64 elements, 16-byte aligned.
+struct Product {
+  const uint8_t *a, *b;
+  uint32_t a_row, b_row;  // bytes from row to row
+  uint32_t m, n, blocks;
+  Tiles t;
+  // what becomes of it
+  const RowOf* rows;
+  float2* sums;      // kStats: [tile of n][m]: maximum and sum of exp(x - maximum)
+  float* hit;        // kStats: logit of the row's target
+  void *g, *gt;      // kGrad: [m][g_ld] and [piece's class][gt_ld], columns up to `cols`
+  uint64_t g_ld, gt_ld;
+  uint32_t first_class, cols, classes;
+  const uint32_t* largest;  // kGrad: bits of the largest weight
+  void* c;           // kSum
+  uint64_t ldc;
+  bool accumulate, by_row;
+  float* part;
+};
+enum Mode { kStats, kGrad, kSum };
+
+// fp16: elements of g are multiplied by 2^14 as rows, where they are at most 1, and by a power of two that brings the largest weight to
+// 2^14 as columns.  bf16 has fp32's range.
+template <typename T>
+constexpr bool kNarrow = false;
+template <>
+constexpr bool kNarrow<_Float16> = true;
+template <typename T>
+constexpr float kRowScale = kNarrow<T> ? 0x1p14f : 1.f;
+template <typename T>
+__device__ __forceinline__ float column_scale(uint32_t largest) {
+  if constexpr (!kNarrow<T>) return 1.f;
+  const uint32_t e = max(largest >> 23, 1u);  // 2^(e - 127) <= largest < 2^(e - 126)
+  return __uint_as_float(min(127u + 13u + 127u - min(e, 254u), 254u) << 23);
+}
+
+template <typename TC, int N>
+__device__ __forceinline__ void put(TC* row, uint32_t j, uint32_t end, float (&f)[N], bool accumulate) {
+  if (j >= end) return;
+  TC* to = row + j;
+  const uint32_t n = min((uint32_t)N, end - j);
+  Vec<TC, N> y = {};
+  if (accumulate) {
+    if (n == N) load<false>(y, to);
+    else load_end(y, to, n, 0.f);
+#pragma unroll
+    for (int r = 0; r < N; ++r) f[r] += y.get(r);
+  }
+  y.set(f);
+  if (n == N) store<false>(to, y);
+  else store_end(to, y, n);
+}
+
+// The loop is that of 8-bit products (one block of k arrives while another is multiplied, two groups of wavefronts in turns where there are
+// eight), with 64 elements of 16 bits to a block.
+template <typename S, typename T, Mode MODE, typename TC>
+__global__ __launch_bounds__(S::threads, 2) void k_linear(const Product p) {
+  __shared__ __align__(16) uint8_t stage[S::lds];
+  __shared__ RowOf row_of[S::rows_m];
+  constexpr uint32_t kStage = S::rows * 128;
+  const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave / S::WN, wn = wave % S::WN;
+  const uint32_t n_tiles = p.t.across * p.t.down, split = blockIdx.x / n_tiles;
+  uint32_t tile_m, tile_n;
+  tile_of(p.t, blockIdx.x - split * n_tiles, &tile_m, &tile_n);
+  const uint32_t m0 = tile_m * S::rows_m, n0 = tile_n * S::rows_n;
+  const uint32_t first = split * p.t.split_blocks, end = min(p.blocks, first + p.t.split_blocks);
+  const uint8_t *a0 = p.a + (uint64_t)m0 * p.a_row, *b0 = p.b + (uint64_t)n0 * p.b_row;
+  const uint32_t last_m = p.m - 1u - m0, last_n = p.n - 1u - n0;
+  uint32_t from[S::loads];
+#pragma unroll
+  for (int j = 0; j < S::loads; ++j) {
+    const uint32_t r = (j * S::waves + wave) * 8u + lane / 8u;
+    const uint32_t piece = ((lane & 7u) ^ (r >> 1 & 7u)) * 16u;
+    from[j] = (j * S::waves * 8 < S::rows_m ? min(r, last_m) * p.a_row : min(r - S::rows_m, last_n) * p.b_row) + piece;
+  }
+  const auto fetch = [&](uint32_t block, uint32_t at) {
+#pragma unroll
+    for (int j = 0; j < S::loads; ++j)
+      load_to_lds(j * S::waves * 8 < S::rows_m ? a0 : b0, from[j], block * 128u, stage + at + (j * S::waves + wave) * 1024u);
+  };
+  uint32_t at[2][2];
+#pragma unroll
+  for (uint32_t h = 0; h < 2; ++h)
+#pragma unroll
+    for (uint32_t q = 0; q < 2; ++q) at[h][q] = (lane & 31u) * 128u + ((4u * h + 2u * q + (lane >> 5)) ^ (lane >> 1 & 7u)) * 16u;
+  const uint32_t a_at = wm * S::TM * 4096u, b_at = S::rows_m * 128u + wn * S::TN * 4096u;
+  if constexpr (MODE == kStats || MODE == kGrad) {
+    if (threadIdx.x < S::rows_m) {
+      RowOf r = {0.f, 0.f, 0.f, -1};
+      if (m0 + threadIdx.x < p.m) r = p.rows[m0 + threadIdx.x];
+      row_of[threadIdx.x] = r;
+    }
+  }
+  f32x16 acc[S::TM][S::TN] = {};
+  uint32_t now = 0;
+  if (first < end) fetch(first, 0);
+  u32x4 x[S::TN][2], y[S::TM][2];
+  if constexpr (S::turns) {
+    wait_and_meet<0>();
+    if (wave >= S::waves / 2) meet();
+  }
+  for (uint32_t block = first; block < end; ++block) {
+    if constexpr (!S::turns) wait_and_meet<0>();
+    if (block + 1u < end) fetch(block + 1u, kStage - now);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+#pragma unroll
+      for (int f = 0; f < S::TN; ++f)
+#pragma unroll
+        for (int q = 0; q < 2; ++q) x[f][q] = *reinterpret_cast<const u32x4*>(stage + now + b_at + f * 4096 + at[h][q]);
+#pragma unroll
+      for (int f = 0; f < S::TM; ++f)
+#pragma unroll
+        for (int q = 0; q < 2; ++q) y[f][q] = *reinterpret_cast<const u32x4*>(stage + now + a_at + f * 4096 + at[h][q]);
+      if constexpr (S::turns) {
+        if (h == 0) reads_done_and_meet();
+        else wait_and_meet<0>();
+        __builtin_amdgcn_s_setprio(1);
+      }
+#pragma unroll
+      for (int q = 0; q < 2; ++q)
+#pragma unroll
+        for (int i = 0; i < S::TM; ++i)
+#pragma unroll
+          for (int j = 0; j < S::TN; ++j) acc[i][j] = mma(T{}, x[j][q], y[i][q], acc[i][j]);
+      settle<S>(acc);
+      if constexpr (S::turns) {
+        __builtin_amdgcn_s_setprio(0);
+        meet();
+      }
+    }
+    now = kStage - now;
+  }
+  if constexpr (S::turns) {
+    if (wave < S::waves / 2) meet();
+  }
+  wait_and_meet<0>();
+  // lane l has row l % 32 of a's square, and of b's the rows 8 g + 4 (l / 32) + r in element 4 g + r
+  if constexpr (MODE == kStats) {
+    float2* part = reinterpret_cast<float2*>(stage);  // [wn][rows_m]
+    const uint32_t c0 = n0 + wn * S::TN * 32u + 4u * (lane >> 5);
+    const bool whole = n0 + S::rows_n <= p.n;
+#pragma unroll
+    for (int i = 0; i < S::TM; ++i) {
+      const uint32_t r = (wm * S::TM + i) * 32u + (lane & 31u);
+      const int target = row_of[r].target;
+      if (!whole) {
+#pragma unroll
+        for (int j = 0; j < S::TN; ++j)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) acc[i][j][e] = c0 + 32u * j + 8u * (e / 4) + e % 4 < p.n ? acc[i][j][e] : -kInf;
+      }
+      float top = -kInf, sum = 0;
+#pragma unroll
+      for (int j = 0; j < S::TN; ++j)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) top = fmaxf(top, acc[i][j][e]);
+      top = fmaxf(top, other_half(top));
+      const float base = top == -kInf ? 0.f : top;
+#pragma unroll
+      for (int j = 0; j < S::TN; ++j)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) sum += __builtin_amdgcn_exp2f((acc[i][j][e] - base) * kLog2e);
+      sum += other_half(sum);
+      const uint32_t in = (uint32_t)target - c0;
+      if (__builtin_amdgcn_ballot_w64(target >= 0 && in < 32u * S::TN) != 0) {
+#pragma unroll
+        for (int j = 0; j < S::TN; ++j)
+#pragma unroll
+          for (int e = 0; e < 16; ++e)
+            if (in == 32u * j + 8u * (e / 4) + e % 4 && target >= 0 && m0 + r < p.m) store1(p.hit + m0 + r, acc[i][j][e]);
+      }
+      if (lane < 32u) part[wn * S::rows_m + r] = {top, sum};
+    }
+    __syncthreads();
+    if (threadIdx.x < S::rows_m && m0 + threadIdx.x < p.m) {
+      float2 t[S::WN];
+      float top = -kInf, sum = 0;
+#pragma unroll
+      for (int w = 0; w < S::WN; ++w) t[w] = part[w * S::rows_m + threadIdx.x], top = fmaxf(top, t[w].x);
+#pragma unroll
+      for (int w = 0; w < S::WN; ++w) sum += t[w].y == 0.f ? 0.f : t[w].y * __builtin_amdgcn_exp2f((t[w].x - top) * kLog2e);
+      p.sums[(uint64_t)tile_n * p.m + m0 + threadIdx.x] = {top, sum};
+    }
+    return;
+  }
+  // 64 rows of 64 at a time through LDS, a wavefront in its own part of it
+  float* mine = reinterpret_cast<float*>(stage) + wave * (64 * 64);
+  const float columns = MODE == kGrad ? column_scale<T>(load1(p.largest)) : MODE == kSum && p.largest ? 1.f / column_scale<T>(load1(p.largest)) : 1.f;
+  float* part = MODE == kSum && p.part ? p.part + (uint64_t)split * p.m * p.n : nullptr;
+#pragma unroll
+  for (int half = 0; half < S::TM / 2; ++half) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int j = 0; j < S::TN; ++j)
+#pragma unroll
+        for (uint32_t g = 0; g < 4; ++g) {
+          const f32x16& d = acc[2 * half + i][j];
+          const uint32_t r = i * 32u + (lane & 31u), piece = j * 8u + g * 2u + (lane >> 5);
+          *reinterpret_cast<f32x4*>(mine + r * 64u + (piece ^ (r & 15u)) * 4u) = f32x4{d[4 * g], d[4 * g + 1], d[4 * g + 2], d[4 * g + 3]};
+        }
+    __builtin_amdgcn_wave_barrier();
+    const uint32_t r0 = (wm * S::TM + 2 * half) * 32u, c0 = n0 + wn * 64u;
+    constexpr int N = MODE == kGrad ? 8 : 16 / sizeof(TC);  // elements a lane writes
+#pragma unroll
+    for (uint32_t it = 0; it < 64u * 64u / (64u * N); ++it) {
+      const uint32_t e = it * 64u + lane, r = e / (64u / N), col = e % (64u / N) * N;
+      float f[N];
+#pragma unroll
+      for (uint32_t v = 0; v < N; v += 4) {
+        const f32x4 d = *reinterpret_cast<const f32x4*>(mine + r * 64u + ((col / 4u + v / 4u) ^ (r & 15u)) * 4u);
+        f[v] = d.x, f[v + 1] = d.y, f[v + 2] = d.z, f[v + 3] = d.w;
+      }
+      const uint32_t i = m0 + r0 + r, j = c0 + col;
+      if constexpr (MODE == kGrad) {
+        const RowOf of = row_of[r0 + r];
+#pragma unroll
+        for (int v = 0; v < N; ++v) {
+          const uint32_t c = p.first_class + j + v;
+          const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(f[v] - of.top, kLog2e, -of.log_sum)) - ((int)c == of.target ? 1.f : 0.f);
+          f[v] = of.target >= 0 && c < p.classes ? w : 0.f;
+        }
+#pragma unroll
+        for (uint32_t v = 0; v < N; v += 4) *reinterpret_cast<f32x4*>(mine + r * 64u + ((col / 4u + v / 4u) ^ (r & 15u)) * 4u) = f32x4{f[v], f[v + 1], f[v + 2], f[v + 3]};
+        if (p.g && i < p.m && j < p.cols) {
+          Vec<T, 8> out;
+#pragma unroll
+          for (int v = 0; v < N; ++v) f[v] *= kRowScale<T>;
+          out.set(f);
+          *(LMT_GLOBAL u32x4*)(static_cast<T*>(p.g) + (uint64_t)i * p.g_ld + j) = u32x4{out.w[0], out.w[1], out.w[2], out.w[3]};
+        }
+      } else if (i < p.m) {
+        if (part) {
+          put<float, N>(part + (uint64_t)i * p.n, j, p.n, f, false);
+        } else {
+          const float by = p.by_row ? p.rows[i].weight * (1.f / kRowScale<T>) : columns;
+          const bool none = p.by_row && p.rows[i].target < 0;
+#pragma unroll
+          for (int v = 0; v < N; ++v) f[v] = none ? 0.f : f[v] * by;
+          put<TC, N>(static_cast<TC*>(p.c) + (uint64_t)i * p.ldc, j, p.n, f, p.accumulate);
+        }
+      }
+    }
+    __builtin_amdgcn_wave_barrier();
+    if constexpr (MODE == kGrad) {
+      if (p.gt) {
+#pragma unroll
+        for (uint32_t it = 0; it < 8; ++it) {  // lane: a class; 8 rows
+          float f[8];
+#pragma unroll
+          for (uint32_t v = 0; v < 8; ++v) {
+            const uint32_t r = it * 8u + v;
+            f[v] = mine[r * 64u + ((lane / 4u) ^ (r & 15u)) * 4u + (lane & 3u)] * (row_of[r0 + r].weight * columns);
+            if (row_of[r0 + r].target < 0) f[v] = 0.f;
+          }
+          Vec<T, 8> out;
+          out.set(f);
+          const uint32_t i = m0 + r0 + it * 8u;
+          if (i < p.gt_ld && c0 + lane < p.cols) *(LMT_GLOBAL u32x4*)(static_cast<T*>(p.gt) + (uint64_t)(c0 + lane) * p.gt_ld + i) = u32x4{out.w[0], out.w[1], out.w[2], out.w[3]};
+        }
+        __builtin_amdgcn_wave_barrier();
+      }
+    }
+  }
+}
+
+// Adds the parts of a product in order, a thread 4 neighbours.
+template <typename T, typename TC>
+__global__ __launch_bounds__(256) void k_linear_join(const Product p, uint32_t parts) {
+  const uint64_t across = ceil_div(p.n, 4), n = (uint64_t)p.m * across;
+  for (uint64_t of = (uint64_t)blockIdx.x * 256u + threadIdx.x; of < n; of += (uint64_t)gridDim.x * 256u) {
+    const uint64_t i = of / across;
+    const uint32_t j = (uint32_t)(of % across) * 4u, left = min(4u, p.n - j);
+    float f[4] = {};
+    for (uint32_t part = 0; part < parts; ++part) {
+      const float* from = p.part + ((uint64_t)part * p.m + i) * p.n + j;
+      Vec<float, 4> v;
+      if (left == 4u) load<false>(v, from);
+      else load_end(v, from, left, 0.f);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) f[e] += v.get(e);
+    }
+    const float by = p.by_row ? p.rows[i].weight * (1.f / kRowScale<T>) : 1.f / column_scale<T>(load1(p.largest));
+    const bool none = p.by_row && p.rows[i].target < 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) f[e] = none ? 0.f : f[e] * by;
+    put<TC, 4>(static_cast<TC*>(p.c) + i * p.ldc, j, p.n, f, p.accumulate);
+  }
+}
+
+// ---- rows ---------------------------------------------------------------------------------------
+
+// In front of the first pass: what a row's target and weight are.
+__global__ __launch_bounds__(256) void k_linear_targets(const LinearLoss p, RowOf* rows) {
+  const uint32_t i = blockIdx.x * 256u + threadIdx.x;
+  if (i >= p.rows) return;
+  bool bad;
+  const int t = target_of(p.targets, p.wide_targets, i, p.ignore, p.classes, &bad);
+  if (bad && p.status) atomicOr(p.status, LMT_STATUS_BAD_TARGET);
+  rows[i] = {0.f, 0.f, t < 0 ? 0.f : p.weights ? load1(p.weights + i) : 1.f, t};
+}
+// Behind it: the tiles' maxima and sums joined, the loss.
+__global__ __launch_bounds__(256) void k_linear_rows(const LinearLoss p, RowOf* rows, const float2* sums, const float* hit, uint32_t tiles, uint32_t* largest) {
+  const uint32_t i = blockIdx.x * 256u + threadIdx.x;
+  uint32_t size = 0;
+  if (i < p.rows) {
+    float top = -kInf, sum = 0;
+    for (uint32_t t = 0; t < tiles; ++t) {
+      const float2 x = sums[(uint64_t)t * p.rows + i];
+      const float up = fmaxf(top, x.x);
+      sum = (sum == 0.f ? 0.f : sum * __builtin_amdgcn_exp2f((top - up) * kLog2e)) + (x.y == 0.f ? 0.f : x.y * __builtin_amdgcn_exp2f((x.x - up) * kLog2e));
+      top = up;
+    }
+    RowOf r = rows[i];
+    const float log_sum = __builtin_amdgcn_logf(sum);
+    if (p.lse) store1(p.lse + i, __builtin_fmaf(log_sum, kLn2, top));
+    if (p.loss) store1(p.loss + i, r.target < 0 ? 0.f : r.weight * __builtin_fmaf(log_sum, kLn2, top - load1(hit + i)));
+    r.top = top, r.log_sum = log_sum;
+    rows[i] = r;
+    size = __float_as_uint(r.weight) & 0x7fffffffu;
+    if (size >= 0x7f800000u) size = 0;
+  }
+  if (largest) {
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) size = max(size, (uint32_t)__shfl_xor((int)size, d));
+    if ((threadIdx.x & 63u) == 0 && size) atomicMax(largest, size);
+  }
+}
+
+// ---- host ---------------------------------------------------------------------------------------
+
+typedef Shape<2, 4, 4, 2> Large;   // 256 x 256
+typedef Shape<2, 2, 2, 2> Medium;  // 128 x 128
+
+struct Choice {
+  bool large;
+  Tiles t;
+  uint32_t tiles() const { return t.across * t.down; }
+};
+Choice choose(uint64_t m, uint64_t n, uint64_t blocks, bool split) {
+  const uint64_t large = ceil_div(m, Large::rows_m) * ceil_div(n, Large::rows_n), medium = ceil_div(m, Medium::rows_m) * ceil_div(n, Medium::rows_n);
+  const bool wide = medium > 2 * kCus && 5 * ceil_div(large, kCus) <= 3 * ceil_div(medium, 2 * kCus);
+  const uint64_t tile = wide ? 256 : 128, tiles = wide ? large : medium;
+  uint64_t splits = 1;
+  if (split) splits = std::max<uint64_t>(1, std::min<uint64_t>({(wide ? 1u : 2u) * kCus / tiles, blocks / 8, 16}));
+  const uint64_t per = std::max<uint64_t>(1, ceil_div(blocks, splits));
+  return {wide, {(uint32_t)ceil_div(n, tile), (uint32_t)ceil_div(m, tile), (uint32_t)std::max<uint64_t>(1, ceil_div(blocks, per)), (uint32_t)per}};
+}
+
+// Where things lie in the workspace, in bytes.
+struct Plan {
+  uint64_t piece, pieces;             // classes of a piece, a multiple of 256
+  uint64_t x_row, rows_row, t_row;    // elements of padded rows: of x and table, of x's transpose and g's, of the table's
+  Choice stats, grad_x, grad_t;
+  uint64_t rows, sums, hit, largest, x, table, xt, tt, g, gt, part_x, part_t, end;
+};
+constexpr uint64_t kPiece = 1ull << 27;  // elements of g at a time: 256 MB, twice
+Plan plan_of(uint64_t n, uint64_t classes, uint64_t width, bool gradients) {
+  Plan w = {};
+  w.x_row = round_up(width, 64), w.rows_row = round_up(n, 64), w.t_row = round_up(classes, 64);
+  w.pieces = std::max<uint64_t>(1, ceil_div(n * classes, kPiece));
+  w.piece = std::min(round_up(ceil_div(classes, w.pieces), 256), round_up(classes, 256));
+  w.pieces = ceil_div(classes, w.piece);
+  w.stats = choose(n, classes, w.x_row / 64, false);
+  w.grad_x = choose(n, width, w.piece / 64, true);
+  w.grad_t = choose(w.piece, width, w.rows_row / 64, true);
+  const auto take = [&](uint64_t bytes) {
+    const uint64_t at = w.end;
+    w.end += round_up(bytes, 256);
+    return at;
+  };
+  w.rows = take(n * sizeof(RowOf)), w.sums = take(w.stats.t.across * n * sizeof(float2)), w.hit = take(n * 4), w.largest = take(4);
+  w.x = take(n * w.x_row * 2), w.table = take(classes * w.x_row * 2);
+  if (gradients) {
+    w.xt = take(width * w.rows_row * 2), w.tt = take(width * w.t_row * 2);
+    w.g = take(n * w.piece * 2), w.gt = take(w.piece * w.rows_row * 2);
+    if (w.pieces * w.grad_x.t.splits > 1) w.part_x = take(w.pieces * w.grad_x.t.splits * n * width * 4);
+    if (w.grad_t.t.splits > 1) w.part_t = take(w.grad_t.t.splits * w.piece * width * 4);
+  }
+  return w;
+}
+
+template <typename T, Mode MODE, typename TC>
+void launch(const Product& p, bool large, hipStream_t s) {
+  const uint32_t grid = p.t.across * p.t.down * p.t.splits;
+  if (large) hipLaunchKernelGGL((k_linear<Large, T, MODE, TC>), dim3(grid), dim3(Large::threads), 0, s, p);
+  else hipLaunchKernelGGL((k_linear<Medium, T, MODE, TC>), dim3(grid), dim3(Medium::threads), 0, s, p);
+}
+
+template <typename T>
+hipError_t launch_typed(const LinearLoss& q, hipStream_t s) {
+  const bool gradients = q.grad_x || q.grad_table;
+  const Plan w = plan_of(q.rows, q.classes, q.width, gradients);
+  uint8_t* base = static_cast<uint8_t*>(q.workspace);
+  const auto at = [&](uint64_t offset) { return base + offset; };
+  RowOf* rows = reinterpret_cast<RowOf*>(at(w.rows));
+  uint32_t* largest = gradients ? reinterpret_cast<uint32_t*>(at(w.largest)) : nullptr;
+  const auto as_it_is = [&](const void* x, uint64_t ld) { return q.width % 64 == 0 && ld % 8 == 0 && ((uintptr_t)x & 15u) == 0 && ld * 2 * 256 < 0xffffffffull; };
+  const bool x_copy = !as_it_is(q.x, q.x_ld), table_copy = !as_it_is(q.table, q.table_ld);
+  const auto lay = [&](const void* from, uint64_t ld, uint32_t n, bool copy, uint64_t copy_at, bool turn, uint64_t turn_at) {
+    const uint32_t across = (uint32_t)ceil_div(q.width, 64);
+    return Lay{from, ld, n, q.width, across, copy || turn ? across * (uint32_t)ceil_div(n, 64) : 0u, copy ? at(copy_at) : nullptr, turn ? at(turn_at) : nullptr};
+  };
+  const Lay x = lay(q.x, q.x_ld, q.rows, x_copy, w.x, q.grad_table != nullptr, w.xt);
+  const Lay table = lay(q.table, q.table_ld, q.classes, table_copy, w.table, q.grad_x != nullptr, w.tt);
+  hipLaunchKernelGGL(k_linear_targets, dim3((uint32_t)ceil_div(q.rows, 256)), dim3(256), 0, s, q, rows);
+  if (x.tiles + table.tiles) hipLaunchKernelGGL((k_lay<T>), dim3(x.tiles + table.tiles), dim3(256), 0, s, x, table, q, reinterpret_cast<uint32_t*>(at(w.largest)));
+  Product p = {};
+  p.a = x_copy ? at(w.x) : static_cast<const uint8_t*>(q.x), p.a_row = (uint32_t)(2 * (x_copy ? w.x_row : q.x_ld));
+  p.b = table_copy ? at(w.table) : static_cast<const uint8_t*>(q.table), p.b_row = (uint32_t)(2 * (table_copy ? w.x_row : q.table_ld));
+  p.m = q.rows, p.n = q.classes, p.blocks = (uint32_t)(w.x_row / 64), p.t = w.stats.t, p.rows = rows;
+  p.sums = reinterpret_cast<float2*>(at(w.sums)), p.hit = reinterpret_cast<float*>(at(w.hit));
+  p.classes = q.classes, p.largest = largest;
+  launch<T, kStats, float>(p, w.stats.large, s);
+  hipLaunchKernelGGL(k_linear_rows, dim3((uint32_t)ceil_div(q.rows, 256)), dim3(256), 0, s, q, rows, p.sums, p.hit, w.stats.t.across, largest);
+  if (!gradients) return hipGetLastError();
+  for (uint64_t piece = 0; piece < w.pieces; ++piece) {
+    const uint32_t first = (uint32_t)(piece * w.piece), n = (uint32_t)std::min<uint64_t>(w.piece, q.classes - first);
+    Product g = p;
+    g.b = p.b + (uint64_t)first * p.b_row, g.n = n, g.first_class = first, g.cols = (uint32_t)round_up(n, 64);
+    const Choice c = choose(q.rows, n, p.blocks, false);
+    g.t = c.t, g.g = q.grad_x ? at(w.g) : nullptr, g.g_ld = w.piece, g.gt = q.grad_table ? at(w.gt) : nullptr, g.gt_ld = w.rows_row;
+    launch<T, kGrad, T>(g, c.large, s);
+    if (q.grad_x) {
+      Product d = {};
+      d.a = at(w.g), d.a_row = (uint32_t)(2 * w.piece), d.b = at(w.tt) + 2ull * first, d.b_row = (uint32_t)(2 * w.t_row);
+      d.m = q.rows, d.n = q.width, d.blocks = g.cols / 64, d.t = w.grad_x.t, d.rows = rows, d.by_row = true;
+      d.c = q.grad_x, d.ldc = q.grad_x_ld;
+      const uint32_t parts = (uint32_t)w.pieces * d.t.splits;
+      float* sums = reinterpret_cast<float*>(at(w.part_x));
+      if (parts > 1) d.part = sums + piece * d.t.splits * (uint64_t)q.rows * q.width;
+      launch<T, kSum, T>(d, w.grad_x.large, s);
+      if (parts > 1 && piece + 1 == w.pieces) {
+        d.part = sums;
+        hipLaunchKernelGGL((k_linear_join<T, T>), dim3((uint32_t)std::min<uint64_t>(ceil_div((uint64_t)d.m * ceil_div(d.n, 4), 256), 1u << 16)), dim3(256), 0, s, d, parts);
+      }
+    }
+    if (q.grad_table) {
+      const auto typed = [&](auto tc) {
+        typedef decltype(tc) TC;
+        Product d = {};
+        d.a = at(w.gt), d.a_row = (uint32_t)(2 * w.rows_row), d.b = at(w.xt), d.b_row = (uint32_t)(2 * w.rows_row);
+        d.m = n, d.n = q.width, d.blocks = (uint32_t)(w.rows_row / 64), d.rows = rows, d.largest = largest, d.accumulate = q.accumulate;
+        d.t = w.grad_t.t, d.t.down = (uint32_t)ceil_div(n, w.grad_t.large ? Large::rows_m : Medium::rows_m);
+        d.c = static_cast<TC*>(q.grad_table) + (uint64_t)first * q.grad_table_ld, d.ldc = q.grad_table_ld;
+        if (d.t.splits > 1) d.part = reinterpret_cast<float*>(at(w.part_t));
+        launch<T, kSum, TC>(d, w.grad_t.large, s);
+        if (d.t.splits > 1)
+          hipLaunchKernelGGL((k_linear_join<T, TC>), dim3((uint32_t)std::min<uint64_t>(ceil_div((uint64_t)d.m * ceil_div(d.n, 4), 256), 1u << 16)), dim3(256), 0, s, d, d.t.splits);
+      };
+      if (q.grad_table_f32) typed(float{});
+      else typed(T{});
+    }
+  }
+  return hipGetLastError();
+}
+
+}  // namespace
+
+uint64_t linear_loss_workspace(uint64_t rows, uint64_t classes, uint64_t width, bool gradients) {
+  return rows && classes ? plan_of(rows, classes, width, gradients).end : 0;
+}
+hipError_t launch_linear_loss(const LinearLoss& p, int dtype, hipStream_t s) {
+  return dtype == LMT_F16 ? launch_typed<_Float16>(p, s) : launch_typed<bf16_t>(p, s);
+}
+
+}  // namespace lmt
