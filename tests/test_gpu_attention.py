@@ -1,0 +1,343 @@
+"""Attention and its gradient against their formulas in 64 bits (GPU)."""
+import numpy as np
+import pytest
+import torch
+
+import attention_reference as A
+from lmt_gpu import DT, typed, within
+from paper_2402_02447_amd import lmt
+
+pytestmark = pytest.mark.gpu
+
+
+class Heads:
+    """[rows, heads, size] in a buffer of one repeated byte: rows one behind the other, or heads in front of rows, with gaps, from any element on."""
+
+    def __init__(self, rows, heads, size, kind, gap=0, offset=0, heads_first=False, values=None):
+        inner, outer = (rows, heads) if heads_first else (heads, rows)
+        small, large = size + gap, inner * (size + gap) + gap
+        self.buffer = torch.full((2 * (offset + outer * large + 8),), 0x5A, dtype=torch.uint8, device="cuda")
+        flat = self.buffer.view(DT[kind])
+        self.step = (small, large) if heads_first else (large, small)
+        self.view = torch.as_strided(flat, (rows, heads, size), (*self.step, 1), offset)
+        self.offset = offset
+        if values is not None:
+            self.view.copy_(torch.as_tensor(values))
+
+    def numpy(self):
+        return self.view.double().cpu().numpy()
+
+    def untouched_outside(self):
+        inside = torch.zeros(self.buffer.numel() // 2, dtype=torch.bool, device="cuda")
+        torch.as_strided(inside, self.view.shape, (*self.step, 1), self.offset).fill_(True)
+        return bool((self.buffer.view(-1, 2)[~inside] == 0x5A).all())
+
+
+def device(x, dtype):
+    return None if x is None else torch.tensor(np.asarray(x), dtype=dtype, device="cuda")
+
+
+def check(starts, heads=2, kv_heads=2, size=16, kind="bf16", rows=None, lengths=None, prefixes=None, slopes=None, scale=None, cap=0.0, causal=False, gap=0, offset=0,
+          heads_first=False, sigma=1.0, seed=0, spoil=None, stream=None, only_forward=False):
+    """spoil(q, k, v, go): puts other values in; what nobody sees of them must not matter."""
+    rng = np.random.default_rng(seed)
+    T = int(starts[-1]) if rows is None else rows
+    scale = 1 / np.sqrt(size) if scale is None else scale
+    q, go = (typed(rng.normal(0, s, (T, heads, size)), kind) for s in (sigma, 0.1))
+    k, v = (typed(rng.normal(0, s, (T, kv_heads, size)), kind) for s in (sigma, 1.0))
+    if spoil:
+        spoil(q, k, v, go)
+    masks = dict(lengths=lengths, prefixes=prefixes, slopes=slopes, scale=scale, cap=cap, causal=causal)
+    on = dict(lengths=device(lengths, torch.int32), prefixes=device(prefixes, torch.int32), slopes=device(slopes, torch.float32), scale=scale, cap=cap, causal=causal)
+    if slopes is not None:
+        masks["slopes"] = on["slopes"].double().cpu().numpy()
+    shape = dict(gap=gap, offset=offset, heads_first=heads_first)
+    Q, GO = (Heads(T, heads, size, kind, values=x, **shape) for x in (q, go))
+    K, V = (Heads(T, kv_heads, size, kind, values=x, **shape) for x in (k, v))
+    O, GQ = (Heads(T, heads, size, kind, gap + 1, offset + 1, heads_first) for _ in range(2))
+    GK, GV = (Heads(T, kv_heads, size, kind, gap + 1, offset + 1, not heads_first) for _ in range(2))
+    lse = torch.full((heads, T), 77.0, device="cuda")
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    st = device(starts, torch.int32)
+    torch.cuda.synchronize()
+    lmt.attention(Q.view, K.view, V.view, O.view, lse, st, status=status, stream=stream, **on)
+    torch.cuda.synchronize()
+    with np.errstate(all="ignore"):
+        (o, bo), (l, bl) = A.attention(q, k, v, starts, kind, **masks)
+    within(lse.cpu().numpy(), l, bl)
+    within(O.numpy(), o, bo)
+    assert O.untouched_outside()
+    if only_forward:
+        return O, lse
+    workspace = torch.full((lmt.attention_grad_workspace(T, heads, kv_heads, size),), 0xFF, dtype=torch.uint8, device="cuda")
+    torch.cuda.synchronize()
+    lmt.attention_grad(GO.view, Q.view, K.view, V.view, O.view, lse, GQ.view, GK.view, GV.view, workspace, st, status=status, stream=stream, **on)
+    torch.cuda.synchronize()
+    assert int(status.item()) == 0
+    with np.errstate(all="ignore"):
+        grads = A.attention_grad(go, q, k, v, O.numpy(), lse.double().cpu().numpy(), starts, kind, **masks)
+    for got, (want, bound) in zip((GQ, GK, GV), grads):
+        within(got.numpy(), want, bound)
+        assert got.untouched_outside()
+    for x, was in ((Q, q), (K, k), (V, v), (GO, go)):
+        assert np.array_equal(x.numpy(), was, equal_nan=True) and x.untouched_outside()
+    return O, lse, GQ, GK, GV
+
+
+def at(*lengths):
+    return np.concatenate([[0], np.cumsum(lengths)])
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+@pytest.mark.parametrize("size", [1, 2, 7, 8, 9, 16, 31, 33, 63, 64, 65, 72, 96, 127, 128])
+def test_head_sizes(size, kind):
+    check(at(50, 3, 90), size=size, kind=kind)
+    check(at(50, 3, 90), size=size, kind=kind, causal=True, slopes=[0.1, 0.01], cap=5.0, gap=3, offset=1)
+
+
+@pytest.mark.parametrize("size", [64, 128])
+@pytest.mark.parametrize("n", [1, 2, 31, 32, 33, 63, 64, 65, 96, 127, 128, 129, 130, 191, 192, 193, 257, 400])
+def test_lengths(n, size):
+    check(at(n), heads=1, kv_heads=1, size=size)
+    check(at(n), heads=1, kv_heads=1, size=size, causal=True, kind="f16")
+    check(at(n, 7, n), heads=2, kv_heads=1, size=size, causal=True, prefixes=[n // 2, 0, n])
+
+
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+def test_gaps_empty_sequences_and_rows_of_none(causal, kind):
+    starts, lengths = [5, 60, 60, 60, 130, 300, 310], [40, 0, 0, 70, 128, 1]
+    check(starts, heads=4, kv_heads=2, size=64, rows=340, lengths=lengths, causal=causal, kind=kind)
+    check([0, 0, 0], heads=1, kv_heads=1, rows=70, causal=causal, kind=kind)                    # sequences, and none has a row
+    check([70], heads=1, kv_heads=1, rows=70, causal=causal, kind=kind)                         # no sequences
+    check([0, 512, 1024, 1536], heads=2, kv_heads=2, size=64, rows=1536, lengths=[512, 1, 300], causal=causal, kind=kind)
+
+
+def test_many_short_sequences():
+    rng = np.random.default_rng(1)
+    n = rng.integers(0, 4, 3000)
+    check(at(*n), heads=2, kv_heads=1, size=32)
+    check(at(*n), heads=1, kv_heads=1, size=32, causal=True, slopes=[0.5], rows=int(n.sum()) + 77)
+    check(at(*([1] * 300)), heads=3, kv_heads=3, size=24, causal=True)
+    check(at(*([0] * 1500 + [200] + [0] * 1500)), heads=1, kv_heads=1, size=64)
+
+
+@pytest.mark.parametrize("heads,kv_heads", [(1, 1), (2, 1), (3, 3), (8, 1), (12, 4), (16, 2)])
+@pytest.mark.parametrize("size", [64, 128])
+def test_shared_heads(heads, kv_heads, size):
+    check(at(140, 30), heads=heads, kv_heads=kv_heads, size=size, causal=True, slopes=np.linspace(0.01, 0.5, heads) if heads > 2 else None)
+    check(at(140, 30), heads=heads, kv_heads=kv_heads, size=size, kind="f16")
+
+
+@pytest.mark.parametrize("masks", [dict(cap=3.0), dict(cap=0.5, causal=True), dict(slopes=[1.0, -0.01]), dict(slopes=[0.0, 8.0], causal=True, prefixes=[10, 500, -3]), dict(scale=0.0), dict(scale=-0.3),
+                                   dict(scale=2.0), dict(cap=50.0, slopes=[0.5, 0.1], scale=1.0)], ids=str)
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+def test_scores(masks, kind):
+    for size in (48, 128):
+        if "prefixes" in masks:
+            seen = np.clip(masks["prefixes"], 0, [90, 64, 150])
+            O = check(at(90, 64, 150), size=size, kind=kind, **dict(masks, prefixes=seen))
+            P = check_bits(at(90, 64, 150), size, kind, masks)
+            assert torch.equal(O[0].view, P)
+        else:
+            check(at(90, 64, 150), size=size, kind=kind, **masks)
+
+
+def check_bits(starts, size, kind, masks):
+    """Prefixes below 0 and beyond a sequence are its ends."""
+    rng = np.random.default_rng(0)
+    T = int(starts[-1])
+    q, _ = (torch.tensor(rng.normal(0, s, (T, 2, size))).to(DT[kind]).cuda() for s in (1.0, 0.1))
+    k, v = (torch.tensor(rng.normal(0, 1.0, (T, 2, size))).to(DT[kind]).cuda() for _ in range(2))
+    out = torch.empty_like(q)
+    lmt.attention(q, k, v, out, None, device(starts, torch.int32), prefixes=device(masks["prefixes"], torch.int32), slopes=device(masks["slopes"], torch.float32), scale=1 / np.sqrt(size), causal=True)
+    torch.cuda.synchronize()
+    return out
+
+
+@pytest.mark.parametrize("sigma", [0.01, 4.0, 30.0])
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+def test_flat_and_peaked_rows(sigma, kind):
+    check(at(200, 33), size=64, kind=kind, sigma=sigma)
+    check(at(200, 33), size=64, kind=kind, sigma=sigma, causal=True, cap=20.0)
+
+
+@pytest.mark.parametrize("gap,offset,heads_first", [(0, 0, True), (1, 0, False), (3, 1, True), (8, 8, False), (24, 3, False)])
+@pytest.mark.parametrize("size", [40, 64, 128])
+def test_strides_and_starts(gap, offset, heads_first, size):
+    check(at(70, 65), heads=4, kv_heads=2, size=size, gap=gap, offset=offset, heads_first=heads_first, causal=True)
+
+
+def bad_values(*places):
+    def spoil(q, k, v, go):
+        for x in (q, k, v, go):
+            for n, rows in enumerate(places):
+                x[rows] = (np.nan, np.inf, -np.inf)[n % 3]
+    return spoil
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+@pytest.mark.parametrize("size", [64, 100])
+@pytest.mark.parametrize("general", [dict(), dict(cap=4.0, slopes=[0.1, 0.2])], ids=["plain", "general"])
+def test_infinities_and_nan_in_rows_of_no_sequence(kind, size, general):
+    check([3, 60, 200], size=size, rows=260, lengths=[50, 100], kind=kind, spoil=bad_values(slice(0, 3), slice(53, 60), slice(160, 260)), **general)
+    check([3, 60, 200], size=size, rows=260, lengths=[50, 100], kind=kind, spoil=bad_values(slice(0, 3), slice(53, 60), slice(160, 260)), causal=True, **general)
+
+
+def nan_rows(got, first, end):
+    bad = ~torch.isfinite(got.view).flatten(1).all(1).cpu().numpy()
+    want = np.zeros(len(bad), bool)
+    want[first:end] = True
+    return np.array_equal(bad, want)
+
+
+@pytest.mark.parametrize("causal", [False, True])
+def test_nan_stays_with_those_who_see_it(causal):
+    """A key's NaN is in the rows of its sequence that see it and in no other's; the other sequences' bounds are checked by the reference."""
+    def spoil(q, k, v, go):
+        v[70] = np.nan                                      # row 30 of the second sequence, which has rows 40 to 109
+    rng = np.random.default_rng(0)
+    starts, T, size = at(40, 70, 50), 160, 64
+    q, k, v = (rng.normal(0, 1, (T, 2, size)) for _ in range(3))
+    q, k, v = (typed(x, "bf16") for x in (q, k, v))
+    spoil(q, k, v, None)
+    Q, K, V = (Heads(T, 2, size, "bf16", values=x) for x in (q, k, v))
+    O = Heads(T, 2, size, "bf16")
+    lmt.attention(Q.view, K.view, V.view, O.view, None, device(starts, torch.int32), scale=0.125, causal=causal)
+    torch.cuda.synchronize()
+    first = 70 if causal else 40
+    assert nan_rows(O, first, 110)
+    v[70] = 0
+    (o, b), _ = A.attention(q, k, v, starts, "bf16", scale=0.125, causal=causal)
+    got = O.numpy()
+    rest = np.r_[0:first, 110:T]
+    within(got[rest], o[rest], b[rest])
+
+
+def test_gradients_of_nan_stay_with_those_who_see_it():
+    rng = np.random.default_rng(0)
+    starts, T, size = at(40, 70, 50), 160, 64
+    x = [typed(rng.normal(0, 1, (T, 2, size)), "bf16") for _ in range(4)]
+    (o, _), (l, _) = A.attention(*x[:3], starts, "bf16", scale=0.125, causal=True)
+    Q, K, V, GO = (Heads(T, 2, size, "bf16", values=a) for a in x)
+    O = Heads(T, 2, size, "bf16", values=typed(o, "bf16"))
+    GO.view[70] = float("nan")
+    lse = torch.tensor(l, dtype=torch.float32, device="cuda")
+    G = [Heads(T, 2, size, "bf16") for _ in range(3)]
+    ws = torch.empty(lmt.attention_grad_workspace(T, 2, 2, size), dtype=torch.uint8, device="cuda")
+    lmt.attention_grad(GO.view, Q.view, K.view, V.view, O.view, lse, *(g.view for g in G), ws, device(starts, torch.int32), scale=0.125, causal=True)
+    torch.cuda.synchronize()
+    assert nan_rows(G[0], 70, 71) and nan_rows(G[1], 40, 71) and nan_rows(G[2], 40, 71)
+    go = x[3].copy()
+    go[70] = 0
+    want = A.attention_grad(go, *x[:3], O.numpy(), lse.double().cpu().numpy(), starts, "bf16", scale=0.125, causal=True)
+    for g, (w, b), rest in zip(G, want, (np.r_[0:70, 71:T], np.r_[0:40, 71:T], np.r_[0:40, 71:T])):
+        within(g.numpy()[rest], w[rest], b[rest])
+
+
+def test_rows_without_any_weight():
+    """Scores of -inf alone: zeros, -inf, and no gradient."""
+    rng = np.random.default_rng(0)
+    x = [typed(np.abs(rng.normal(0, 1, (80, 2, 32))), "bf16") for _ in range(3)]
+    x[1][:30] = -np.inf
+    Q, K, V = (Heads(80, 2, 32, "bf16", values=a) for a in x)
+    O, lse = Heads(80, 2, 32, "bf16"), torch.full((2, 80), 5.0, device="cuda")
+    lmt.attention(Q.view, K.view, V.view, O.view, lse, device(at(30, 50), torch.int32), scale=0.2)
+    torch.cuda.synchronize()
+    assert bool((lse[:, :30] == -np.inf).all()) and not O.view[:30].any() and bool(torch.isfinite(lse[:, 30:]).all())
+    G = [Heads(80, 2, 32, "bf16") for _ in range(3)]
+    ws = torch.empty(lmt.attention_grad_workspace(80, 2, 2, 32), dtype=torch.uint8, device="cuda")
+    lmt.attention_grad(Q.view, Q.view, K.view, V.view, O.view, lse, *(g.view for g in G), ws, device(at(30, 50), torch.int32), scale=0.2)
+    torch.cuda.synchronize()
+    assert not G[2].view[:30].any() and bool(torch.isfinite(G[0].view[30:]).all()) and bool(torch.isfinite(G[1].view[30:]).all())
+
+
+def test_tables_that_are_wrong_are_reported_and_do_no_harm():
+    q = torch.randn(200, 2, 32, device="cuda").bfloat16()
+    out, lse = torch.empty_like(q), torch.empty(2, 200, device="cuda")
+    g = [torch.empty_like(q) for _ in range(3)]
+    ws = torch.empty(lmt.attention_grad_workspace(200, 2, 2, 32), dtype=torch.uint8, device="cuda")
+    for starts, lengths in (([0, 100, 50, 200], None), ([-5, 100, 200], None), ([0, 100, 201], None), ([0, 100, 2 ** 31 - 1], None), ([-2 ** 31, 2 ** 31 - 1], None), ([200, 100, 0], None),
+                            ([0, 100, 200], [101, 100]), ([0, 100, 200], [-1, 100]), ([0, 100, 200], [2 ** 31 - 1, 2 ** 31 - 1])):
+        for causal in (False, True):
+            status = torch.zeros(1, dtype=torch.int32, device="cuda")
+            lmt.attention(q, q, q, out, lse, device(starts, torch.int32), lengths=device(lengths, torch.int32), scale=0.2, causal=causal, status=status)
+            torch.cuda.synchronize()
+            assert int(status.item()) == lmt.LMT_STATUS_BAD_SEQUENCE and bool(torch.isfinite(out).all())
+            status.zero_()
+            lmt.attention_grad(q, q, q, q, out, lse, *g, ws, device(starts, torch.int32), lengths=device(lengths, torch.int32), scale=0.2, causal=causal, status=status)
+            torch.cuda.synchronize()
+            assert int(status.item()) == lmt.LMT_STATUS_BAD_SEQUENCE and all(bool(torch.isfinite(x).all()) for x in g)
+
+
+def test_the_same_call_gives_the_same_bits_and_a_graph_follows_its_inputs():
+    """Captured on another stream and replayed on other sequences, beside eager calls with the same workspace size."""
+    rng = np.random.default_rng(7)
+    T, H, G, D = 700, 4, 2, 64
+    q, go = (torch.randn(T, H, D, device="cuda").bfloat16() for _ in range(2))
+    k, v = (torch.randn(T, G, D, device="cuda").bfloat16() for _ in range(2))
+
+    def state():
+        return [torch.zeros_like(q), torch.zeros(H, T, device="cuda"), torch.zeros_like(q), torch.zeros_like(k), torch.zeros_like(v), torch.empty(lmt.attention_grad_workspace(T, H, G, D), dtype=torch.uint8, device="cuda")]
+
+    def step(starts, s, stream=None):
+        lmt.attention(q, k, v, s[0], s[1], starts, scale=0.125, causal=True, stream=stream)
+        lmt.attention_grad(go, q, k, v, s[0], s[1], s[2], s[3], s[4], s[5], starts, scale=0.125, causal=True, stream=stream)
+    held, a, b, c = torch.zeros(6, dtype=torch.int32, device="cuda"), state(), state(), state()
+    stream, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=stream):
+        step(held, b, stream)
+    for _ in range(4):
+        starts = device(np.concatenate([[0], np.sort(rng.integers(0, T, 4)), [T - rng.integers(0, 50)]]), torch.int32)
+        held.copy_(starts)
+        q.copy_(torch.randn_like(q.float()))
+        torch.cuda.synchronize()
+        graph.replay()
+        step(starts, a)
+        torch.cuda.synchronize()
+        step(starts, c)
+        torch.cuda.synchronize()
+        for x, y, z in zip(a[:5], b[:5], c[:5]):
+            assert torch.equal(x, y) and torch.equal(x, z)
+
+
+def test_offsets_beyond_32_bits():
+    """70 rows 2^26 elements apart: the last one lies 8.6 GiB behind the first."""
+    step, T, D = 1 << 26, 70, 64
+    flat = torch.empty(step * (T - 1) + 7 * D, dtype=torch.bfloat16, device="cuda")
+    views = [torch.as_strided(flat, (T, 1, D), (step, D, 1), n * D) for n in range(4)]
+    g = torch.Generator(device="cuda")
+    g.manual_seed(1)
+    for x in views[:3]:
+        x.copy_(torch.randn(T, 1, D, generator=g, device="cuda"))
+    starts, lse = device([0, T], torch.int32), torch.empty(1, T, device="cuda")
+    lmt.attention(*views, lse, starts, scale=0.125)
+    torch.cuda.synchronize()
+    near = [x.contiguous() for x in views[:3]]
+    out, lse2 = torch.empty_like(near[0]), torch.empty_like(lse)
+    lmt.attention(*near, out, lse2, starts, scale=0.125)
+    torch.cuda.synchronize()
+    assert torch.equal(out, views[3].contiguous()) and torch.equal(lse, lse2)
+    ws = torch.empty(lmt.attention_grad_workspace(T, 1, 1, D), dtype=torch.uint8, device="cuda")
+    a, b = [torch.as_strided(flat, (T, 1, D), (step, D, 1), n * D) for n in (4, 5, 6)], [torch.empty_like(x) for x in near]
+    lmt.attention_grad(views[0], *views, lse, *a, ws, starts, scale=0.125)
+    lmt.attention_grad(near[0], *near, out, lse2, *b, ws, starts, scale=0.125)
+    torch.cuda.synchronize()
+    assert all(torch.equal(x.contiguous(), y) for x, y in zip(a, b))
+
+
+def test_broadcast_inputs():
+    """Rows and heads that are one in memory: read as many, and their gradients are every one's own."""
+    T, D = 60, 32
+    rng = np.random.default_rng(3)
+    q = typed(rng.normal(0, 1, (T, 4, D)), "bf16")
+    one = typed(rng.normal(0, 1, (T, 1, D)), "bf16")
+    Q, K = torch.tensor(q).bfloat16().cuda(), torch.tensor(one).bfloat16().cuda().expand(T, 4, D)
+    out, lse = torch.empty_like(Q), torch.empty(4, T, device="cuda")
+    lmt.attention(Q, K, K, out, lse, device([0, T], torch.int32), scale=0.2)
+    torch.cuda.synchronize()
+    (o, b), _ = A.attention(q, np.repeat(one, 4, 1), np.repeat(one, 4, 1), [0, T], "bf16", scale=0.2)
+    within(out.double().cpu().numpy(), o, b)
+    with pytest.raises(lmt.LmtError, match="one place"):
+        lmt.attention(Q, K, K, K, lse, device([0, T], torch.int32), scale=0.2)
