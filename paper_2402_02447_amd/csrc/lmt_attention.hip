@@ -14,18 +14,19 @@
 // LDS through the transposing read: 16 lanes read 4 rows of 16 elements, and get 4 rows' elements of a column each.
 #include "lmt_device.h"
 #include "lmt_internal.h"
+#include "lmt_tiles.h"
 
 namespace lmt {
 namespace {
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
-typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 #define LMT_LDS __attribute__((address_space(3)))
 
+constexpr int kWaves = 4, kRows = 32 * kWaves, kThreads = 64 * kWaves;  // a wavefront has 32 rows
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kInf = __builtin_inff();
 
@@ -163,14 +164,23 @@ struct Span {
 
 // ---- tiles ----------------------------------------------------------------------------------
 
-// 16 bytes of a row from element 8 * piece on, zeros behind its end.
+// A row of a head goes by pieces of 8 elements, 16 bytes.  Where its size is no multiple of 8 the last piece is the last 8 elements, which
+// repeats some: products along a row need one side without them (Row), products across rows give them twice and one is stored.  Pieces behind the last one
+// repeat the first.  So every load is 16 bytes of the row itself, wherever it starts; rows of fewer than 8 elements are taken one by one.
+__device__ __forceinline__ uint32_t piece_at(uint32_t piece, uint32_t size) {
+  return piece * 8u + 8u <= size ? piece * 8u : piece * 8u < size && size >= 8u ? size - 8u : 0u;
+}
 template <typename T>
 __device__ __forceinline__ u32x4 load_piece(const T* row, uint32_t piece, uint32_t size) {
   Vec<T, 8> v;
-  v.w[0] = v.w[1] = v.w[2] = v.w[3] = 0;
-  if (piece * 8u + 8u <= size) load<false>(v, row + piece * 8u);
-  else if (piece * 8u < size) load_end(v, row + piece * 8u, size - piece * 8u, 0.f);
+  if (size >= 8u) load<false>(v, row + piece_at(piece, size));
+  else load_end(v, row, size, 0.f);
   return u32x4{v.w[0], v.w[1], v.w[2], v.w[3]};
+}
+// How many elements at a piece's start are none of its own, and how many there are in front of its end (8, but for small sizes).
+__device__ __forceinline__ void own_part(uint32_t piece, uint32_t size, uint32_t* begin, uint32_t* end) {
+  const uint32_t left = piece * 8u < size ? size - piece * 8u : 0u;
+  *begin = left >= 8u || size < 8u ? 0u : 8u - left, *end = size < 8u ? left : 8u;
 }
 template <typename T>
 __device__ __forceinline__ const T* head_of(const Heads& x, uint32_t head) {
@@ -189,33 +199,58 @@ __device__ __forceinline__ uint32_t turn(uint32_t row) {
   if constexpr (D == 64) return (row >> 1 & 1u) << 2 | (row >> 2 & 1u) << 1 | (row >> 3 & 1u);
   else return (row & 3u) << 2 | (row >> 2 & 3u);
 }
-template <typename T, int D, int THREADS>
+// DIRECT: from memory to LDS without registers, where all rows start on 16 bytes; else through registers.  Rows behind the last one are the last
+// one again: nobody sees them.
+template <typename T, int D, int THREADS, bool DIRECT>
 struct Stage {
   static constexpr int pieces = D / 8, loads = kTile * pieces / THREADS, step = THREADS / pieces;
-  u32x4 w[loads];
-  // Rows behind the last one are the last one again: nobody sees them.
-  __device__ __forceinline__ void fetch(const T* head, const Heads& x, uint32_t first, uint32_t rows, uint32_t size) {
-    const uint32_t piece = threadIdx.x % pieces, r = first + threadIdx.x / pieces;
+  static_assert(step % 16 == 0, "rows that a thread loads turn their pieces alike");
+  u32x4 w[DIRECT ? 1 : loads];
+  __device__ __forceinline__ void fetch(const T* head, const Heads& x, uint32_t first, uint32_t rows, uint32_t size, uint8_t* tile) {
+    const uint32_t r = threadIdx.x / pieces, slot = threadIdx.x % pieces;
+    if constexpr (DIRECT) {
+      const uint32_t row = (uint32_t)x.row * 2u, at = piece_at(slot ^ turn<D>(r), size) * 2u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+      const uint8_t* base = reinterpret_cast<const uint8_t*>(row_of(head, x, first));
+      const uint32_t last = rows - 1u - first;
 #pragma unroll
-    for (int j = 0; j < loads; ++j) w[j] = load_piece(row_of(head, x, min(r + j * step, rows - 1u)), piece, size);
+      for (int j = 0; j < loads; ++j) load_to_lds(base, min(r + j * step, last) * row + at, 0, tile + (j * THREADS + wave * 64u) * 16u);
+    } else {
+#pragma unroll
+      for (int j = 0; j < loads; ++j) w[j] = load_piece(row_of(head, x, min(first + r + j * step, rows - 1u)), slot, size);
+    }
   }
   __device__ __forceinline__ void put(uint8_t* tile) const {
-    const uint32_t piece = threadIdx.x % pieces, r = threadIdx.x / pieces;
+    if constexpr (!DIRECT) {
+      const uint32_t piece = threadIdx.x % pieces, r = threadIdx.x / pieces;
 #pragma unroll
-    for (int j = 0; j < loads; ++j) *reinterpret_cast<u32x4*>(tile + (r + j * step) * (D * 2) + (piece ^ turn<D>(r + j * step)) * 16u) = w[j];
+      for (int j = 0; j < loads; ++j) *reinterpret_cast<u32x4*>(tile + (r + j * step) * (D * 2) + (piece ^ turn<D>(r)) * 16u) = w[j];
+    }
   }
 };
-// A lane's own row in registers, as an operand for all of k = 0 .. D - 1.
+// What this wavefront has fetched and put is in LDS, and everybody's is.
+__device__ __forceinline__ void arrived() { wait_and_meet<0>(); }
+// A lane's own row in registers, as an operand for all of k = 0 .. D - 1, zeros where there is no element.
 template <typename T, int D>
 struct Row {
   u32x4 w[D / 16];
   __device__ __forceinline__ void read(const T* row, uint32_t size) {
     const uint32_t half = (threadIdx.x & 63u) >> 5;
 #pragma unroll
-    for (int c = 0; c < D / 16; ++c) w[c] = load_piece(row, 2 * c + half, size);
+    for (int c = 0; c < D / 16; ++c) {
+      const uint32_t piece = 2 * c + half;
+      w[c] = load_piece(row, piece, size);
+      if (size != D) {
+        uint32_t begin, end;
+        own_part(piece, size, &begin, &end);
+#pragma unroll
+        for (uint32_t e = 0; e < 4; ++e) {
+          const uint32_t lo = 2 * e >= begin && 2 * e < end && piece * 8u < size ? 0xffffu : 0u, hi = 2 * e + 1 >= begin && 2 * e + 1 < end && piece * 8u < size ? 0xffff0000u : 0u;
+          w[c][e] &= lo | hi;
+        }
+      }
+    }
   }
 };
-// Rows of a tile as operands: along the row (k is the element), and across (k is the row).
 template <int D>
 struct Along {
   uint32_t at[D / 16];
@@ -253,6 +288,19 @@ template <typename T>
 __device__ __forceinline__ u32x4 packed(const f32x16& x, int c) {
   return u32x4{pack2(T{}, x[8 * c], x[8 * c + 1]), pack2(T{}, x[8 * c + 2], x[8 * c + 3]), pack2(T{}, x[8 * c + 4], x[8 * c + 5]), pack2(T{}, x[8 * c + 6], x[8 * c + 7])};
 }
+template <typename T>
+__device__ __forceinline__ void store_piece(T* row, uint32_t piece, const Vec<T, 8>& v, uint32_t size) {
+  if (piece * 8u + 8u <= size) {
+    store<false>(row + piece * 8u, v);
+  } else if (piece * 8u < size) {
+    uint32_t begin, end;
+    own_part(piece, size, &begin, &end);
+    T* to = row + piece_at(piece, size);
+#pragma unroll
+    for (uint32_t e = 0; e < 8; ++e)
+      if (e >= begin && e < end) store1(to + e, from_f32<T>(v.get(e)));
+  }
+}
 // Sums whose column is the lane's row and whose rows are its elements, times `by`, to memory: the halves of a wavefront change places
 // with what the other one has, so that each lane writes 8 neighbours.
 template <typename T, int D>
@@ -268,11 +316,7 @@ __device__ __forceinline__ void store_row(T* row, const f32x16 (&x)[D / 32], flo
       const auto a = __builtin_amdgcn_permlane32_swap(w[0], w[2], false, false), b = __builtin_amdgcn_permlane32_swap(w[1], w[3], false, false);
       Vec<T, 8> v;
       v.w[0] = a[0], v.w[1] = b[0], v.w[2] = a[1], v.w[3] = b[1];
-      const uint32_t from = 32u * d + 16u * c + 8u * half;
-      if (here) {
-        if (from + 8u <= size) store<false>(row + from, v);
-        else if (from < size) store_end(row + from, v, size - from);
-      }
+      if (here) store_piece(row, 4u * d + 2u * c + half, v, size);
     }
 }
 __device__ __forceinline__ bool finite(float x) { return __builtin_fabsf(x) < kInf; }
@@ -288,33 +332,78 @@ __device__ __forceinline__ bool finite(const f32x16 (&x)[D / 32]) {
 
 // ---- scores -----------------------------------------------------------------------------------
 
-// A score in units of log 2 from a product.  PLAIN: scale > 0 alone; otherwise any scale, a cap and a slope.
-// tanh(x) = 1 - 2 / (e^2x + 1), and by its series where that would cancel: up to 0.3 its terms to x^9 leave 5e-8.
+// Scores in units of log 2 from products.  PLAIN kernels: scale > 0 alone; others any scale, a cap and a slope.
+// tanh(x) by its series up to 0.3, where its terms to x^9 leave 5e-8, else 1 - 2 / (e^2x + 1), which cancels near 0.  Scores
+// are mostly far below their cap, so that a wavefront seldom needs the second form.
 struct Score {
   float by, cap, to_cap, slope;  // by: scale * log2(e);  cap, slope: in units of log 2;  to_cap: scale / the cap
   __device__ __forceinline__ void set(const Attention& p, uint32_t head) {
     by = p.scale * kLog2e, cap = p.cap * kLog2e, to_cap = p.cap != 0.f ? p.scale / p.cap : 0.f;
     slope = p.slopes ? load1(p.slopes + head) * kLog2e : 0.f;
   }
-  static __device__ __forceinline__ float tanh_of(float x) {
+  static __device__ __forceinline__ float series(float x) {
     const float y = x * x;
     float s = __builtin_fmaf(y, 0.021869488536f, -0.053968253968f);
     s = __builtin_fmaf(s, y, 0.133333333333f), s = __builtin_fmaf(s, y, -0.333333333333f);
-    s = __builtin_fmaf(s * y, x, x);
-    const float e = exp2_of(__builtin_fabsf(x) * (2.f * kLog2e)), t = 1.f - 2.f * __builtin_amdgcn_rcpf(e + 1.f);
-    return __builtin_fabsf(x) < 0.3f ? s : __builtin_copysignf(t, x);
+    return __builtin_fmaf(s * y, x, x);
   }
-  // apart: |i - j|; bend: what the cap multiplies derivatives by.
+  static __device__ __forceinline__ float tanh_of(float x) {
+    const float e = exp2_of(__builtin_fabsf(x) * (2.f * kLog2e)), t = 1.f - 2.f * __builtin_amdgcn_rcpf(e + 1.f);
+    return __builtin_fabsf(x) < 0.3f ? series(x) : __builtin_copysignf(t, x);
+  }
+  // N elements of a lane's column, from distance `apart` (the column's own row subtracted) on; bend: what the cap multiplies derivatives by.
+  template <int N, bool BEND>
+  __device__ __forceinline__ void of(f32x16 (&s)[N], float apart, f32x16 (&bend)[N]) const {
+    if (cap != 0.f) {
+      float top = 0;
+#pragma unroll
+      for (int b = 0; b < N; ++b)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) s[b][e] *= to_cap, top = fmaxf(top, __builtin_fabsf(s[b][e]));
+      if (any(!(top < 0.3f))) {
+#pragma unroll
+        for (int b = 0; b < N; ++b)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) s[b][e] = tanh_of(s[b][e]);
+      } else {
+#pragma unroll
+        for (int b = 0; b < N; ++b)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) s[b][e] = series(s[b][e]);
+      }
+#pragma unroll
+      for (int b = 0; b < N; ++b)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          if constexpr (BEND) bend[b][e] = __builtin_fmaf(-s[b][e], s[b][e], 1.f);
+          s[b][e] *= cap;
+        }
+    } else {
+#pragma unroll
+      for (int b = 0; b < N; ++b)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          if constexpr (BEND) bend[b][e] = 1.f;
+          s[b][e] *= by;
+        }
+    }
+    if (slope != 0.f) {
+#pragma unroll
+      for (int b = 0; b < N; ++b)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) s[b][e] = __builtin_fmaf(-slope, __builtin_fabsf(apart + (float)(32 * b + 8 * (e / 4) + e % 4)), s[b][e]);
+    }
+  }
+  // One score.
   __device__ __forceinline__ float of(float x, int apart, float* bend = nullptr) const {
     float y = x * by;
+    if (bend) *bend = 1.f;
     if (cap != 0.f) {
       const float t = tanh_of(x * to_cap);
       y = cap * t;
       if (bend) *bend = __builtin_fmaf(-t, t, 1.f);
-    } else if (bend) {
-      *bend = 1.f;
     }
-    return __builtin_fmaf(-slope, (float)apart, y);
+    return slope != 0.f ? __builtin_fmaf(-slope, __builtin_fabsf((float)apart), y) : y;
   }
 };
 
@@ -332,11 +421,10 @@ constexpr float kShift = 0.f;
 template <>
 constexpr float kShift<_Float16> = 7.f;
 
-// Which head and block of rows a workgroup has.  XCD x, which takes every eighth workgroup, gets an eighth of the list, so that its L2 sees
-// one head's keys again and again; causal: long rows first.
+// Which head and block of rows a workgroup has: an XCD has one head after the other, so that its L2 sees the same keys again and again; causal: long
+// rows first.
 __device__ __forceinline__ void place(uint32_t tiles, uint32_t lists, bool backwards, uint32_t* tile, uint32_t* list) {
-  constexpr uint32_t kXcds = 8;
-  const uint32_t n = tiles * lists, x = blockIdx.x % kXcds, share = n / kXcds, extra = n % kXcds, id = x * share + min(x, extra) + blockIdx.x / kXcds;
+  const uint32_t id = (uint32_t)neighbours(blockIdx.x, tiles * lists);
   *list = id / tiles, *tile = id % tiles;
   if (backwards) *tile = tiles - 1u - *tile;
 }
@@ -373,52 +461,52 @@ __device__ __forceinline__ void attend_row(const Attention& p, uint32_t head, ui
   if (p.lse && lane == 0) store1(p.lse + (uint64_t)head * p.rows + i, l == 0.f ? -kInf : (m + __builtin_amdgcn_logf(l)) * kLn2);
 }
 
-template <typename T, int D, bool PLAIN, int WAVES>
-__global__ __launch_bounds__(64 * WAVES, 2) void k_attend(const Attention p, uint32_t tiles) {
-  constexpr int ROWS = 32 * WAVES, THREADS = 64 * WAVES;
+// The scores of the next tile are made while those of this one go through exp2: matrix instructions and the others take turns in the
+// instruction stream, as one wavefront's do not overlap unless they are side by side in it.
+template <typename T, int D, bool PLAIN, bool DIRECT>
+__global__ __launch_bounds__(kThreads, 2) void k_attend(const Attention p, uint32_t tiles) {
   __shared__ __align__(16) uint8_t keys[2][kTile * D * 2], values[2][kTile * D * 2];
-  __shared__ Seen<ROWS> seen;
+  __shared__ Seen<kRows> seen;
   uint32_t tile, head;
   place(tiles, p.heads, p.causal, &tile, &head);
-  const uint32_t kv = head / p.group, wave = threadIdx.x >> 6, lane = threadIdx.x & 63u, row = wave * 32u + (lane & 31u), i = tile * ROWS + row;
+  const uint32_t kv = head / p.group, wave = threadIdx.x >> 6, lane = threadIdx.x & 63u, row = wave * 32u + (lane & 31u), i = tile * kRows + row;
   const T *k = head_of<T>(p.k, kv), *v = head_of<T>(p.v, kv);
   check_sequences(p);
   Row<T, D> q;
   q.read(row_of(head_of<T>(p.q, head), p.q, min(i, p.rows - 1u)), p.size);
-  find_seen<ROWS, THREADS, false>(p, tile * ROWS, seen);
+  find_seen<kRows, kThreads, false>(p, tile * kRows, seen);
   Span span;
   span.read(seen, row);
-  const int first = seen.first, last = seen.last;
+  const int first = __builtin_amdgcn_readfirstlane(seen.first), last = __builtin_amdgcn_readfirstlane(seen.last);
   Score score;
   score.set(p, head);
   Along<D> along;
   Across<D> across;
   along.set(), across.set();
   float m = -kInf, l = 0;
-  f32x16 o[D / 32] = {};
-  Stage<T, D, THREADS> next_k, next_v;
+  f32x16 o[D / 32] = {}, s[2] = {};
+  Stage<T, D, kThreads, DIRECT> next_k, next_v;
   if (first < last) {
-    next_k.fetch(k, p.k, (uint32_t)first, p.rows, p.size), next_v.fetch(v, p.v, (uint32_t)first, p.rows, p.size);
+    next_k.fetch(k, p.k, (uint32_t)first, p.rows, p.size, keys[0]), next_v.fetch(v, p.v, (uint32_t)first, p.rows, p.size, values[0]);
     next_k.put(keys[0]), next_v.put(values[0]);
+    arrived();
+    const bool more = first + kTile < last;
+    if (more) next_k.fetch(k, p.k, (uint32_t)(first + kTile), p.rows, p.size, keys[1]);
+#pragma unroll
+    for (int c = 0; c < D / 16; ++c)
+#pragma unroll
+      for (int b = 0; b < 2; ++b) s[b] = mma(T{}, along.read(keys[0], b, c), q.w[c], s[b]);
+    if (more) next_k.put(keys[1]);
+    arrived();
   }
-  __syncthreads();
   uint32_t now = 0;
   for (int at = first; at < last; at += kTile, now ^= 1u) {
-    const bool more = at + kTile < last;
-    if (more) next_k.fetch(k, p.k, (uint32_t)(at + kTile), p.rows, p.size), next_v.fetch(v, p.v, (uint32_t)(at + kTile), p.rows, p.size);
+    const bool more = at + kTile < last, more_keys = at + 2 * kTile < last;
+    if (more_keys) next_k.fetch(k, p.k, (uint32_t)(at + 2 * kTile), p.rows, p.size, keys[now]);
+    if (more) next_v.fetch(v, p.v, (uint32_t)(at + kTile), p.rows, p.size, values[now ^ 1u]);
     if (span.touches(at, kTile)) {
-      f32x16 s[2] = {};
-#pragma unroll
-      for (int c = 0; c < D / 16; ++c)
-#pragma unroll
-        for (int b = 0; b < 2; ++b) s[b] = mma(T{}, along.read(keys[now], b, c), q.w[c], s[b]);
       const int j0 = at + 4 * (int)(lane >> 5);
-      if constexpr (!PLAIN) {
-#pragma unroll
-        for (int b = 0; b < 2; ++b)
-#pragma unroll
-          for (int e = 0; e < 16; ++e) s[b][e] = score.of(s[b][e], abs(j0 + 32 * b + 8 * (e / 4) + e % 4 - (int)i));
-      }
+      if constexpr (!PLAIN) score.of<2, false>(s, (float)(j0 - (int)i), s);
       if (!span.inside(at, kTile)) {
         const uint32_t from = (uint32_t)(j0 - span.lo), n = (uint32_t)(span.hi - span.lo);
 #pragma unroll
@@ -440,24 +528,38 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_attend(const Attention p, uin
           for (int e = 0; e < 16; ++e) o[d][e] *= by;
       }
       const float base = (m == -kInf ? 0.f : m) - kShift<T>;
+      f32x16 next[2] = {};
+      u32x4 w[2][2];
+      constexpr int kSteps = 2 * (D / 16), kEach = 32 / kSteps;  // scores' instructions, elements behind each of them
+#pragma unroll
+      for (int t = 0; t < kSteps; ++t) {
+        next[t % 2] = mma(T{}, along.read(keys[now ^ 1u], t % 2, t / 2), q.w[t / 2], next[t % 2]);  // behind the last tile: of no concern
+#pragma unroll
+        for (int e = t * kEach; e < (t + 1) * kEach; ++e) {
+          const float x = exp2_of(PLAIN ? __builtin_fmaf(s[e / 16][e % 16], score.by, -base) : s[e / 16][e % 16] - base);
+          s[e / 16][e % 16] = x, l += x;
+        }
+        if ((t + 1) * kEach % 8 == 0) w[((t + 1) * kEach - 8) / 16][((t + 1) * kEach - 8) / 8 % 2] = packed<T>(s[((t + 1) * kEach - 8) / 16], ((t + 1) * kEach - 8) / 8 % 2);
+      }
 #pragma unroll
       for (int b = 0; b < 2; ++b)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          s[b][e] = exp2_of(PLAIN ? __builtin_fmaf(s[b][e], score.by, -base) : s[b][e] - base);
-          l += s[b][e];
-        }
+        for (int c = 0; c < 2; ++c)
 #pragma unroll
-      for (int b = 0; b < 2; ++b)
+          for (int d = 0; d < D / 32; ++d) o[d] = mma(T{}, across.read(values[now], b, c, d), w[b][c], o[d]);
 #pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          const u32x4 w = packed<T>(s[b], c);
+      for (int b = 0; b < 2; ++b) s[b] = next[b];
+    } else if (more && span.touches(at + kTile, kTile)) {
 #pragma unroll
-          for (int d = 0; d < D / 32; ++d) o[d] = mma(T{}, across.read(values[now], b, c, d), w, o[d]);
-        }
+      for (int b = 0; b < 2; ++b) s[b] = f32x16{};
+#pragma unroll
+      for (int c = 0; c < D / 16; ++c)
+#pragma unroll
+        for (int b = 0; b < 2; ++b) s[b] = mma(T{}, along.read(keys[now ^ 1u], b, c), q.w[c], s[b]);
     }
-    if (more) next_k.put(keys[now ^ 1u]), next_v.put(values[now ^ 1u]);
-    __syncthreads();
+    if (more_keys) next_k.put(keys[now]);
+    if (more) next_v.put(values[now ^ 1u]);
+    arrived();
   }
   l += other_half(l);
   const bool some = span.lo < span.hi, here = i < p.rows;
@@ -474,7 +576,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_attend(const Attention p, uin
   if (p.lse && mine && lane < 32u) store1(p.lse + (uint64_t)head * p.rows + i, l == 0.f ? -kInf : (m - kShift<T> + __builtin_amdgcn_logf(l)) * kLn2);
   for (uint32_t left = redo; left; left &= left - 1u) {
     const uint32_t r = wave * 32u + (uint32_t)__builtin_ctz(left);
-    attend_row<T>(p, head, kv, tile * ROWS + r, seen.lo[r], seen.hi[r]);
+    attend_row<T>(p, head, kv, tile * kRows + r, seen.lo[r], seen.hi[r]);
   }
 }
 
@@ -546,14 +648,13 @@ __device__ __forceinline__ float subtracted(float lse) { return lse == -kInf ? k
 
 // Gradient of q and, for the next kernel, delta = grad_out . out of every row: as the forward pass, scores and products with v from a tile of each, d into the
 // sums with k across.
-template <typename T, int D, bool PLAIN, int WAVES>
-__global__ __launch_bounds__(64 * WAVES, 2) void k_attend_grad_q(const Attention p, uint32_t tiles) {
-  constexpr int ROWS = 32 * WAVES, THREADS = 64 * WAVES;
+template <typename T, int D, bool PLAIN, bool DIRECT>
+__global__ __launch_bounds__(kThreads, 2) void k_attend_grad_q(const Attention p, uint32_t tiles) {
   __shared__ __align__(16) uint8_t keys[2][kTile * D * 2], values[2][kTile * D * 2];
-  __shared__ Seen<ROWS> seen;
+  __shared__ Seen<kRows> seen;
   uint32_t tile, head;
   place(tiles, p.heads, p.causal, &tile, &head);
-  const uint32_t kv = head / p.group, wave = threadIdx.x >> 6, lane = threadIdx.x & 63u, row = wave * 32u + (lane & 31u), i = tile * ROWS + row, held = min(i, p.rows - 1u);
+  const uint32_t kv = head / p.group, wave = threadIdx.x >> 6, lane = threadIdx.x & 63u, row = wave * 32u + (lane & 31u), i = tile * kRows + row, held = min(i, p.rows - 1u);
   const T *k = head_of<T>(p.k, kv), *v = head_of<T>(p.v, kv);
   check_sequences(p);
   Row<T, D> q, go;
@@ -571,12 +672,12 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_attend_grad_q(const Attention
     delta += other_half(delta);
   }
   const float lse = subtracted(load1(p.lse + (uint64_t)head * p.rows + held));
-  find_seen<ROWS, THREADS, false>(p, tile * ROWS, seen);
+  find_seen<kRows, kThreads, false>(p, tile * kRows, seen);
   Span span;
   span.read(seen, row);
   const bool some = span.lo < span.hi;
   if (i < p.rows && lane < 32u) store1(p.delta + (uint64_t)head * p.rows + i, delta);
-  const int first = seen.first, last = seen.last;
+  const int first = __builtin_amdgcn_readfirstlane(seen.first), last = __builtin_amdgcn_readfirstlane(seen.last);
   Score score;
   score.set(p, head);
   Along<D> along;
@@ -585,16 +686,16 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_attend_grad_q(const Attention
   Range<T> range;
   range.begin();
   f32x16 sum[D / 32] = {};
-  Stage<T, D, THREADS> next_k, next_v;
+  Stage<T, D, kThreads, DIRECT> next_k, next_v;
   if (first < last) {
-    next_k.fetch(k, p.k, (uint32_t)first, p.rows, p.size), next_v.fetch(v, p.v, (uint32_t)first, p.rows, p.size);
+    next_k.fetch(k, p.k, (uint32_t)first, p.rows, p.size, keys[0]), next_v.fetch(v, p.v, (uint32_t)first, p.rows, p.size, values[0]);
     next_k.put(keys[0]), next_v.put(values[0]);
   }
-  __syncthreads();
+  arrived();
   uint32_t now = 0;
   for (int at = first; at < last; at += kTile, now ^= 1u) {
     const bool more = at + kTile < last;
-    if (more) next_k.fetch(k, p.k, (uint32_t)(at + kTile), p.rows, p.size), next_v.fetch(v, p.v, (uint32_t)(at + kTile), p.rows, p.size);
+    if (more) next_k.fetch(k, p.k, (uint32_t)(at + kTile), p.rows, p.size, keys[now ^ 1u]), next_v.fetch(v, p.v, (uint32_t)(at + kTile), p.rows, p.size, values[now ^ 1u]);
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
       const int at_b = at + 32 * b;
@@ -609,14 +710,13 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_attend_grad_q(const Attention
       const bool inside = span.inside(at_b, 32);
       const uint32_t from = (uint32_t)(j0 - span.lo), n = (uint32_t)(span.hi - span.lo);
       const float less = delta * range.by;
+      f32x16 bend[1];
+      if constexpr (!PLAIN) score.of<1, true>(s, (float)(j0 - (int)i), bend);
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
-        float bend = 1.f, w;
-        if constexpr (PLAIN) w = exp2_of(__builtin_fmaf(s[0][e], score.by, -lse));
-        else w = exp2_of(score.of(s[0][e], abs(j0 + 8 * (e / 4) + e % 4 - (int)i), &bend) - lse);
-        float d = __builtin_fmaf(dp[e], range.by, -less) * w;
-        if constexpr (!PLAIN) d *= bend;
-        s[0][e] = d;
+        const float w = exp2_of(PLAIN ? __builtin_fmaf(s[0][e], score.by, -lse) : s[0][e] - lse);
+        s[0][e] = __builtin_fmaf(dp[e], range.by, -less) * w;
+        if constexpr (!PLAIN) s[0][e] *= bend[0][e];
       }
       if (!inside) {
 #pragma unroll
@@ -631,7 +731,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_attend_grad_q(const Attention
       }
     }
     if (more) next_k.put(keys[now ^ 1u]), next_v.put(values[now ^ 1u]);
-    __syncthreads();
+    arrived();
   }
   const uint64_t rows_again = __builtin_amdgcn_ballot_w64(some && !finite<D>(sum));
   const uint32_t redo = (uint32_t)rows_again | (uint32_t)(rows_again >> 32);
@@ -643,7 +743,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_attend_grad_q(const Attention
   for (uint32_t left = redo; left; left &= left - 1u) {
     const int b = __builtin_ctz(left);
     const uint32_t r = wave * 32u + (uint32_t)b;
-    grad_q_row<T>(p, head, kv, tile * ROWS + r, seen.lo[r], seen.hi[r], __shfl(lse, b), __shfl(delta, b));
+    grad_q_row<T>(p, head, kv, tile * kRows + r, seen.lo[r], seen.hi[r], __shfl(lse, b), __shfl(delta, b));
   }
 }
 
@@ -702,40 +802,40 @@ __device__ __forceinline__ void grad_kv_row(const Attention& p, uint32_t kv, uin
       store1(const_cast<T*>(row_of(head_of<T>(p.grad_k, kv), p.grad_k, j)) + c, from_f32<T>(dk[e] * p.scale));
       store1(const_cast<T*>(row_of(head_of<T>(p.grad_v, kv), p.grad_v, j)) + c, from_f32<T>(dv[e]));
     } else {
-      store1(part_k + ((uint64_t)kv * p.rows + j) * D + c, dk[e] * p.scale);
-      store1(part_v + ((uint64_t)kv * p.rows + j) * D + c, dv[e]);
+      const uint32_t in = c / 8u * 8u + 8u <= p.size || p.size < 8u ? c : c + 8u - p.size % 8u;  // the last piece ends with the row
+      store1(part_k + ((uint64_t)kv * p.rows + j) * D + in, dk[e] * p.scale);
+      store1(part_v + ((uint64_t)kv * p.rows + j) * D + in, dv[e]);
     }
   }
 }
 
 // Gradients of k and v: a lane has a key, the rows that see it come by in tiles, for one query head after the other.  Scores as Q K^T, so that
 // what a lane has of them is an operand of dO^T P and Q^T d.
-template <typename T, int D, bool PLAIN, int WAVES>
-__global__ __launch_bounds__(64 * WAVES, D == 64 ? 2 : 1) void k_attend_grad_kv(const Attention p, uint32_t tiles) {
-  constexpr int ROWS = 32 * WAVES, THREADS = 64 * WAVES;
+template <typename T, int D, bool PLAIN, bool DIRECT>
+__global__ __launch_bounds__(kThreads, D == 64 ? 2 : 1) void k_attend_grad_kv(const Attention p, uint32_t tiles) {
   __shared__ __align__(16) uint8_t queries[2][kTile * D * 2], grads[2][kTile * D * 2];
   __shared__ __align__(16) float lse[2][kTile], delta[2][kTile];
-  __shared__ Seen<ROWS> seen;
+  __shared__ Seen<kRows> seen;
   uint32_t tile, list;
   place(tiles, p.kv_heads * p.parts, false, &tile, &list);
   const uint32_t kv = list / p.parts, part = list % p.parts, h0 = kv * p.group + part * p.group / p.parts, h1 = kv * p.group + (part + 1u) * p.group / p.parts;
-  const uint32_t wave = threadIdx.x >> 6, lane = threadIdx.x & 63u, row = wave * 32u + (lane & 31u), j = tile * ROWS + row, held = min(j, p.rows - 1u);
+  const uint32_t wave = threadIdx.x >> 6, lane = threadIdx.x & 63u, row = wave * 32u + (lane & 31u), j = tile * kRows + row, held = min(j, p.rows - 1u);
   Row<T, D> k, v;
   k.read(row_of(head_of<T>(p.k, kv), p.k, held), p.size), v.read(row_of(head_of<T>(p.v, kv), p.v, held), p.size);
-  find_seen<ROWS, THREADS, true>(p, tile * ROWS, seen);
+  find_seen<kRows, kThreads, true>(p, tile * kRows, seen);
   Span span;
   span.read(seen, row);
-  const int first = seen.first, last = seen.last;
+  const int first = __builtin_amdgcn_readfirstlane(seen.first), last = __builtin_amdgcn_readfirstlane(seen.last);
   Along<D> along;
   Across<D> across;
   along.set(), across.set();
   Range<T> range;
   range.begin();
   f32x16 dk[D / 32] = {}, dv[D / 32] = {};
-  Stage<T, D, THREADS> next_q, next_go;
+  Stage<T, D, kThreads, DIRECT> next_q, next_go;
   float next_lse = 0, next_delta = 0;
-  const auto fetch = [&](uint32_t head, int at) {
-    next_q.fetch(head_of<T>(p.q, head), p.q, (uint32_t)at, p.rows, p.size), next_go.fetch(head_of<T>(p.grad_out, head), p.grad_out, (uint32_t)at, p.rows, p.size);
+  const auto fetch = [&](uint32_t head, int at, uint32_t to) {
+    next_q.fetch(head_of<T>(p.q, head), p.q, (uint32_t)at, p.rows, p.size, queries[to]), next_go.fetch(head_of<T>(p.grad_out, head), p.grad_out, (uint32_t)at, p.rows, p.size, grads[to]);
     if (threadIdx.x < kTile) {
       const uint64_t from = (uint64_t)head * p.rows + min((uint32_t)at + threadIdx.x, p.rows - 1u);
       next_lse = load1(p.lse + from), next_delta = load1(p.delta + from);
@@ -745,54 +845,52 @@ __global__ __launch_bounds__(64 * WAVES, D == 64 ? 2 : 1) void k_attend_grad_kv(
     next_q.put(queries[to]), next_go.put(grads[to]);
     if (threadIdx.x < kTile) lse[to][threadIdx.x] = subtracted(next_lse), delta[to][threadIdx.x] = next_delta;
   };
-  if (first < last) fetch(h0, first), put(0);
-  __syncthreads();
+  if (first < last) fetch(h0, first, 0), put(0);
+  arrived();
   uint32_t now = 0;
   for (uint32_t head = h0; first < last && head < h1; ++head) {
     Score score;
     score.set(p, head);
     for (int at = first; at < last; at += kTile, now ^= 1u) {
       const bool wrap = at + kTile >= last, more = !wrap || head + 1u < h1;
-      if (more) fetch(wrap ? head + 1u : head, wrap ? first : at + kTile);
+      if (more) fetch(wrap ? head + 1u : head, wrap ? first : at + kTile, now ^ 1u);
 #pragma unroll
       for (int b = 0; b < 2; ++b) {
         const int at_b = at + 32 * b;
         if (!span.touches(at_b, 32)) continue;
-        f32x16 s = {}, d[1] = {};
+        f32x16 s[1] = {}, d[1] = {}, bend[1];
 #pragma unroll
         for (int c = 0; c < D / 16; ++c) {
-          s = mma(T{}, along.read(queries[now], b, c), k.w[c], s);
+          s[0] = mma(T{}, along.read(queries[now], b, c), k.w[c], s[0]);
           d[0] = mma(T{}, along.read(grads[now], b, c), v.w[c], d[0]);
         }
         const int half = 4 * (int)(lane >> 5), i0 = at_b + half;
         const bool inside = span.inside(at_b, 32);
         const uint32_t from = (uint32_t)(i0 - span.lo), n = (uint32_t)(span.hi - span.lo);
+        if constexpr (!PLAIN) score.of<1, true>(s, (float)(i0 - (int)j), bend);
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
           const f32x4 less = *reinterpret_cast<const f32x4*>(&lse[now][32 * b + 8 * g + half]), dot_out = *reinterpret_cast<const f32x4*>(&delta[now][32 * b + 8 * g + half]);
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
             const int e = 4 * g + r;
-            float bend = 1.f, w;
-            if constexpr (PLAIN) w = exp2_of(__builtin_fmaf(s[e], score.by, -less[r]));
-            else w = exp2_of(score.of(s[e], abs(i0 + 8 * g + r - (int)j), &bend) - less[r]);
-            float x = __builtin_fmaf(d[0][e], range.by, -dot_out[r] * range.by) * w;
-            if constexpr (!PLAIN) x *= bend;
-            s[e] = w, d[0][e] = x;
+            const float w = exp2_of(PLAIN ? __builtin_fmaf(s[0][e], score.by, -less[r]) : s[0][e] - less[r]);
+            s[0][e] = w, d[0][e] = __builtin_fmaf(d[0][e], range.by, -dot_out[r] * range.by) * w;
+            if constexpr (!PLAIN) d[0][e] *= bend[0][e];
           }
         }
         if (!inside) {
 #pragma unroll
           for (int e = 0; e < 16; ++e) {
             const bool in = from + (uint32_t)(8 * (e / 4) + e % 4) < n;
-            s[e] = in ? s[e] : 0.f, d[0][e] = in ? d[0][e] : 0.f;
+            s[0][e] = in ? s[0][e] : 0.f, d[0][e] = in ? d[0][e] : 0.f;
           }
         }
         range.fit(d, dk);
-        if constexpr (kShift<T> != 0.f) s *= 0x1p14f;  // weights are at most 1
+        if constexpr (kShift<T> != 0.f) s[0] *= 0x1p14f;  // weights are at most 1
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
-          const u32x4 w = packed<T>(s, c), x = packed<T>(d[0], c);
+          const u32x4 w = packed<T>(s[0], c), x = packed<T>(d[0], c);
 #pragma unroll
           for (int e = 0; e < D / 32; ++e) {
             dv[e] = mma(T{}, across.read(grads[now], b, c, e), w, dv[e]);
@@ -801,7 +899,7 @@ __global__ __launch_bounds__(64 * WAVES, D == 64 ? 2 : 1) void k_attend_grad_kv(
         }
       }
       if (more) put(now ^ 1u);
-      __syncthreads();
+      arrived();
     }
   }
   const bool some = span.lo < span.hi;
@@ -817,7 +915,7 @@ __global__ __launch_bounds__(64 * WAVES, D == 64 ? 2 : 1) void k_attend_grad_kv(
   store_key<T, D>(p, p.grad_v, part_v, kv, j, dv, kShift<T> != 0.f ? 0x1p-14f : 1.f, mine);
   for (uint32_t left = redo; left; left &= left - 1u) {
     const uint32_t r = wave * 32u + (uint32_t)__builtin_ctz(left);
-    grad_kv_row<T, D>(p, kv, h0, h1, tile * ROWS + r, seen.lo[r], seen.hi[r], part_k, part_v);
+    grad_kv_row<T, D>(p, kv, h0, h1, tile * kRows + r, seen.lo[r], seen.hi[r], part_k, part_v);
   }
 }
 
@@ -837,21 +935,27 @@ __global__ __launch_bounds__(256) void k_attend_join(const Attention p) {
     for (int e = 0; e < 4; ++e) x[e] += a[e], x[4 + e] += b[e];
   }
   const Heads& to = key / p.rows < p.kv_heads ? p.grad_k : p.grad_v;
-  T* row = const_cast<T*>(row_of(head_of<T>(to, (uint32_t)kv), to, (uint32_t)j)) + piece * 8u;
+  T* row = const_cast<T*>(row_of(head_of<T>(to, (uint32_t)kv), to, (uint32_t)j));
   Vec<T, 8> v;
   v.set(x);
-  if (piece * 8u + 8u <= p.size) store<false>(row, v);
-  else store_end(row, v, p.size - piece * 8u);
+  store_piece(row, piece, v, p.size);
 }
 
-constexpr int kWaves = 4;
-
+// Whether rows of two tensors can go to LDS by themselves: on 16 bytes, and 64 rows within what 32 bits count.
+bool direct(const Attention& p, const Heads& a, const Heads& b) {
+  const auto fits = [&](const Heads& x) { return ((uintptr_t)x.at & 15u) == 0 && x.row % 8 == 0 && x.head % 8 == 0 && x.row < (1u << 24); };
+  return p.size % 8 == 0 && fits(a) && fits(b);
+}
 template <typename F>
-hipError_t with_form(const Attention& p, int dtype, F f) {
+hipError_t with_form(const Attention& p, int dtype, bool straight, F f) {
   const bool plain = p.cap == 0.f && !p.slopes && p.scale > 0.f;
+  const auto staged = [&](auto t, auto wide, auto simple) {
+    if (straight) return f(t, wide, simple, std::true_type{});
+    return f(t, wide, simple, std::false_type{});
+  };
   const auto sized = [&](auto t, auto wide) {
-    if (plain) return f(t, wide, std::true_type{});
-    return f(t, wide, std::false_type{});
+    if (plain) return staged(t, wide, std::true_type{});
+    return staged(t, wide, std::false_type{});
   };
   const auto typed = [&](auto t) {
     if (p.size <= 64u) return sized(t, std::integral_constant<int, 64>{});
@@ -862,28 +966,35 @@ hipError_t with_form(const Attention& p, int dtype, F f) {
 
 }  // namespace
 
-uint32_t attention_parts(uint64_t, uint64_t, uint64_t, uint64_t) { return 1; }
+uint32_t attention_parts(uint64_t rows, uint64_t heads, uint64_t kv_heads, uint64_t) {
+  const uint64_t group = heads / kv_heads, there = ceil_div(rows, kRows) * kv_heads;
+  return (uint32_t)std::max<uint64_t>(1, std::min(group, 4 * kCus / there));
+}
 
 uint64_t attention_grad_workspace(uint64_t rows, uint64_t heads, uint64_t kv_heads, uint64_t size) {
   const uint64_t parts = attention_parts(rows, heads, kv_heads, size);
   return round_up(4 * rows * heads, 16) + (parts > 1 ? 8 * parts * kv_heads * rows * (size <= 64 ? 64 : 128) : 0);
 }
 
-uint64_t attention_launches(uint64_t rows, uint64_t heads) { return ceil_div(rows, 32 * kWaves) * heads; }
+uint64_t attention_launches(uint64_t rows, uint64_t heads) { return ceil_div(rows, kRows) * heads; }
 
 hipError_t launch_attention(const Attention& p, int dtype, hipStream_t s) {
-  return with_form(p, dtype, [&](auto t, auto d, auto plain) {
-    const uint32_t tiles = (uint32_t)ceil_div(p.rows, 32 * kWaves);
-    hipLaunchKernelGGL((k_attend<decltype(t), decltype(d)::value, decltype(plain)::value, kWaves>), dim3(tiles * p.heads), dim3(64 * kWaves), 0, s, p, tiles);
+  const uint32_t tiles = (uint32_t)ceil_div(p.rows, kRows);
+  return with_form(p, dtype, direct(p, p.k, p.v), [&](auto t, auto d, auto plain, auto straight) {
+    hipLaunchKernelGGL((k_attend<decltype(t), decltype(d)::value, decltype(plain)::value, decltype(straight)::value>), dim3(tiles * p.heads), dim3(kThreads), 0, s, p, tiles);
     return hipGetLastError();
   });
 }
 
 hipError_t launch_attention_grad(const Attention& p, int dtype, hipStream_t s) {
-  return with_form(p, dtype, [&](auto t, auto d, auto plain) {
-    const uint32_t tiles = (uint32_t)ceil_div(p.rows, 32 * kWaves);
-    hipLaunchKernelGGL((k_attend_grad_q<decltype(t), decltype(d)::value, decltype(plain)::value, kWaves>), dim3(tiles * p.heads), dim3(64 * kWaves), 0, s, p, tiles);
-    hipLaunchKernelGGL((k_attend_grad_kv<decltype(t), decltype(d)::value, decltype(plain)::value, kWaves>), dim3(tiles * p.kv_heads * p.parts), dim3(64 * kWaves), 0, s, p, tiles);
+  const uint32_t tiles = (uint32_t)ceil_div(p.rows, kRows);
+  const hipError_t e = with_form(p, dtype, direct(p, p.k, p.v), [&](auto t, auto d, auto plain, auto straight) {
+    hipLaunchKernelGGL((k_attend_grad_q<decltype(t), decltype(d)::value, decltype(plain)::value, decltype(straight)::value>), dim3(tiles * p.heads), dim3(kThreads), 0, s, p, tiles);
+    return hipGetLastError();
+  });
+  if (e != hipSuccess) return e;
+  return with_form(p, dtype, direct(p, p.q, p.grad_out), [&](auto t, auto d, auto plain, auto straight) {
+    hipLaunchKernelGGL((k_attend_grad_kv<decltype(t), decltype(d)::value, decltype(plain)::value, decltype(straight)::value>), dim3(tiles * p.kv_heads * p.parts), dim3(kThreads), 0, s, p, tiles);
     if (p.parts > 1u)
       hipLaunchKernelGGL((k_attend_join<decltype(t), decltype(d)::value>), dim3((uint32_t)ceil_div((uint64_t)2 * p.kv_heads * p.rows * (decltype(d)::value / 8), 256)), dim3(256), 0, s, p);
     return hipGetLastError();
