@@ -46,11 +46,18 @@ __device__ __forceinline__ float other_half(float x) {
   return __uint_as_float((threadIdx.x & 32u) ? r[0] : r[1]);
 }
 __device__ __forceinline__ bool any(bool x) { return __builtin_amdgcn_ballot_w64(x) != 0; }
-__device__ __forceinline__ int wave_min(int x) {
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) x = min(x, __shfl_xor(x, d));
-  return __builtin_amdgcn_readfirstlane(x);
+// The largest of the lanes up to this one, by moves between lanes: within rows of 16, then from the end of the rows in front.  -1 is the least.
+__device__ __forceinline__ int max_so_far(int x) {
+  x = max(x, __builtin_amdgcn_update_dpp(-1, x, 0x111, 0xf, 0xf, false));  // row_shr:1
+  x = max(x, __builtin_amdgcn_update_dpp(-1, x, 0x112, 0xf, 0xf, false));
+  x = max(x, __builtin_amdgcn_update_dpp(-1, x, 0x114, 0xf, 0xf, false));
+  x = max(x, __builtin_amdgcn_update_dpp(-1, x, 0x118, 0xf, 0xf, false));
+  x = max(x, __builtin_amdgcn_update_dpp(-1, x, 0x142, 0xa, 0xf, false));  // row_bcast:15, to the second and fourth row
+  return max(x, __builtin_amdgcn_update_dpp(-1, x, 0x143, 0xc, 0xf, false));  // row_bcast:31, to the upper half
 }
+// The largest and smallest of a wavefront's whole numbers of 0 and more.
+__device__ __forceinline__ int wave_max(int x) { return __builtin_amdgcn_readlane(max_so_far(x), 63); }
+__device__ __forceinline__ int wave_min(int x) { return 0x7fffffff - wave_max(0x7fffffff - x); }
 __device__ __forceinline__ float wave_max(float x) {
 #pragma unroll
   for (int d = 1; d < 64; d *= 2) x = fmaxf(x, __shfl_xor(x, d));
@@ -97,17 +104,10 @@ __device__ __forceinline__ void find_seen(const Attention& p, uint32_t block_row
     if (start < r1) atomicMax(&s.lo[start <= r0 ? 0 : start - r0], (int)q);
   }
   __syncthreads();
-  int of = -1, before = -1;
+  int of = -1;
   if (t < ROWS) {
-    of = s.lo[t];
-    if (t >= 64) before = s.lo[t - 64];
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-      const int x = __shfl_up(of, d);
-      if ((t & 63) >= d) of = max(of, x);
-      before = max(before, __shfl_xor(before, d));
-    }
-    of = max(of, before);
+    of = max_so_far(s.lo[t]);
+    if (ROWS > 64 && t >= 64) of = max(of, wave_max(s.lo[t - 64]));
   }
   __syncthreads();
   if (t < ROWS) {
@@ -122,10 +122,11 @@ __device__ __forceinline__ void find_seen(const Attention& p, uint32_t block_row
         const int prefix = p.causal && p.prefixes ? start + min(max(((const LMT_GLOBAL int32_t*)p.prefixes)[of], 0), length) : start;
         if constexpr (KEYS) lo = p.causal && i >= prefix ? i : start, hi = stop;
         else lo = start, hi = p.causal ? max(i + 1, prefix) : stop;
-        atomicMin(&s.first, lo), atomicMax(&s.last, hi);
       }
     }
     s.lo[t] = lo, s.hi[t] = hi;
+    const int first = wave_min(lo < hi ? lo : 0x7fffffff), last = wave_max(hi);
+    if ((t & 63) == 0) atomicMin(&s.first, first), atomicMax(&s.last, last);
   }
   __syncthreads();
 }
@@ -155,8 +156,8 @@ struct Span {
   __device__ __forceinline__ void read(const Seen<ROWS>& s, uint32_t row) {
     lo = s.lo[row], hi = s.hi[row];
     const bool some = lo < hi;
-    any_lo = wave_min(some ? lo : 0x7fffffff), any_hi = -wave_min(some ? -hi : 0);
-    all_lo = -wave_min(some ? -lo : 0), all_hi = wave_min(some ? hi : 0x7fffffff);
+    any_lo = wave_min(some ? lo : 0x7fffffff), any_hi = wave_max(hi);
+    all_lo = wave_max(lo), all_hi = wave_min(some ? hi : 0x7fffffff);
   }
   __device__ __forceinline__ bool touches(int at, int n) const { return at < any_hi && at + n > any_lo; }
   __device__ __forceinline__ bool inside(int at, int n) const { return at >= all_lo && at + n <= all_hi; }
@@ -193,7 +194,7 @@ __device__ __forceinline__ const T* row_of(const T* head, const Heads& x, uint32
 
 // kTile rows of D elements in LDS.  The 16-byte pieces of a row change places by the row's number: reads of one piece of 16 rows and
 // transposing reads of four rows then meet every bank once.
-constexpr int kTile = 64;
+constexpr int kTile = 64, kAhead = 4;  // kAhead: operands on their way from LDS
 template <int D>
 __device__ __forceinline__ uint32_t turn(uint32_t row) {
   if constexpr (D == 64) return (row >> 1 & 1u) << 2 | (row >> 2 & 1u) << 1 | (row >> 3 & 1u);
@@ -213,7 +214,7 @@ struct Stage {
       const uint8_t* base = reinterpret_cast<const uint8_t*>(row_of(head, x, first));
       const uint32_t last = rows - 1u - first;
 #pragma unroll
-      for (int j = 0; j < loads; ++j) load_to_lds(base, min(r + j * step, last) * row + at, 0, tile + (j * THREADS + wave * 64u) * 16u);
+      for (int j = 0; j < loads; ++j) send_to_lds(base, min(r + j * step, last) * row + at, 0, tile + (j * THREADS + wave * 64u) * 16u);
     } else {
 #pragma unroll
       for (int j = 0; j < loads; ++j) w[j] = load_piece(row_of(head, x, min(first + r + j * step, rows - 1u)), slot, size);
@@ -464,7 +465,7 @@ __device__ __forceinline__ void attend_row(const Attention& p, uint32_t head, ui
 // The scores of the next tile are made while those of this one go through exp2: matrix instructions and the others take turns in the
 // instruction stream, as one wavefront's do not overlap unless they are side by side in it.
 template <typename T, int D, bool PLAIN, bool DIRECT>
-__global__ __launch_bounds__(kThreads, 2) void k_attend(const Attention p, uint32_t tiles) {
+__global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void k_attend(const Attention p, uint32_t tiles) {
   __shared__ __align__(16) uint8_t keys[2][kTile * D * 2], values[2][kTile * D * 2];
   __shared__ Seen<kRows> seen;
   uint32_t tile, head;
@@ -483,7 +484,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_attend(const Attention p, uint3
   Along<D> along;
   Across<D> across;
   along.set(), across.set();
-  float m = -kInf, l = 0;
+  float m = -kInf, sum[4] = {};
   f32x16 o[D / 32] = {}, s[2] = {};
   Stage<T, D, kThreads, DIRECT> next_k, next_v;
   if (first < last) {
@@ -521,7 +522,9 @@ __global__ __launch_bounds__(kThreads, 2) void k_attend(const Attention p, uint3
       if constexpr (PLAIN) top *= score.by;
       if (any(top > m + kSlack)) {
         const float up = fmaxf(m, top), by = m == -kInf ? 0.f : exp2_of(m - up);
-        m = up, l *= by;
+        m = up;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sum[e] *= by;
 #pragma unroll
         for (int d = 0; d < D / 32; ++d)
 #pragma unroll
@@ -529,24 +532,33 @@ __global__ __launch_bounds__(kThreads, 2) void k_attend(const Attention p, uint3
       }
       const float base = (m == -kInf ? 0.f : m) - kShift<T>;
       f32x16 next[2] = {};
-      u32x4 w[2][2];
-      constexpr int kSteps = 2 * (D / 16), kEach = 32 / kSteps;  // scores' instructions, elements behind each of them
+      u32x4 w[2][2], ahead[kAhead];
+      constexpr int kSteps = 2 * (D / 16), kEach = 32 / kSteps;  // instructions of either kind; elements between two
+      // operand t: of the next scores, then of this tile's values
+      const auto operand = [&](int t) {
+        if (t < kSteps) return along.read(keys[now ^ 1u], t % 2, t / 2);  // behind the last tile: of no concern
+        const int u = t - kSteps, of = u / (D / 32);
+        return across.read(values[now], of / 2, of % 2, u % (D / 32));
+      };
 #pragma unroll
-      for (int t = 0; t < kSteps; ++t) {
-        next[t % 2] = mma(T{}, along.read(keys[now ^ 1u], t % 2, t / 2), q.w[t / 2], next[t % 2]);  // behind the last tile: of no concern
+      for (int t = 0; t < kAhead - 1; ++t) ahead[t] = operand(t);
 #pragma unroll
-        for (int e = t * kEach; e < (t + 1) * kEach; ++e) {
-          const float x = exp2_of(PLAIN ? __builtin_fmaf(s[e / 16][e % 16], score.by, -base) : s[e / 16][e % 16] - base);
-          s[e / 16][e % 16] = x, l += x;
+      for (int t = 0; t < 2 * kSteps; ++t) {
+        if (t + kAhead - 1 < 2 * kSteps) ahead[(t + kAhead - 1) % kAhead] = operand(t + kAhead - 1);
+        if (t < kSteps) {
+          next[t % 2] = mma(T{}, ahead[t % kAhead], q.w[t / 2], next[t % 2]);
+#pragma unroll
+          for (int e = t * kEach; e < (t + 1) * kEach; ++e) {
+            const float x = exp2_of(PLAIN ? __builtin_fmaf(s[e / 16][e % 16], score.by, -base) : s[e / 16][e % 16] - base);
+            s[e / 16][e % 16] = x, sum[e % 4] += x;
+          }
+          if ((t + 1) * kEach % 8 == 0) w[((t + 1) * kEach - 8) / 16][((t + 1) * kEach - 8) / 8 % 2] = packed<T>(s[((t + 1) * kEach - 8) / 16], ((t + 1) * kEach - 8) / 8 % 2);
+        } else {
+          const int u = t - kSteps, of = u / (D / 32), d = u % (D / 32);
+          o[d] = mma(T{}, ahead[t % kAhead], w[of / 2][of % 2], o[d]);
         }
-        if ((t + 1) * kEach % 8 == 0) w[((t + 1) * kEach - 8) / 16][((t + 1) * kEach - 8) / 8 % 2] = packed<T>(s[((t + 1) * kEach - 8) / 16], ((t + 1) * kEach - 8) / 8 % 2);
+        __builtin_amdgcn_sched_barrier(0);
       }
-#pragma unroll
-      for (int b = 0; b < 2; ++b)
-#pragma unroll
-        for (int c = 0; c < 2; ++c)
-#pragma unroll
-          for (int d = 0; d < D / 32; ++d) o[d] = mma(T{}, across.read(values[now], b, c, d), w[b][c], o[d]);
 #pragma unroll
       for (int b = 0; b < 2; ++b) s[b] = next[b];
     } else if (more && span.touches(at + kTile, kTile)) {
@@ -561,6 +573,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_attend(const Attention p, uint3
     if (more) next_v.put(values[now ^ 1u]);
     arrived();
   }
+  float l = (sum[0] + sum[1]) + (sum[2] + sum[3]);
   l += other_half(l);
   const bool some = span.lo < span.hi, here = i < p.rows;
   const bool again = some && !(finite<D>(o) && finite(l));

@@ -164,7 +164,7 @@ __global__ __launch_bounds__(S::threads, 2) void k_linear(const Product p) {
   const auto fetch = [&](uint32_t block, uint32_t at) {
 #pragma unroll
     for (int j = 0; j < S::loads; ++j)
-      load_to_lds(j * S::waves * 8 < S::rows_m ? a0 : b0, from[j], block * 128u, stage + at + (j * S::waves + wave) * 1024u);
+      send_to_lds(j * S::waves * 8 < S::rows_m ? a0 : b0, from[j], block * 128u, stage + at + (j * S::waves + wave) * 1024u);
   };
   uint32_t at[2][2];
 #pragma unroll
