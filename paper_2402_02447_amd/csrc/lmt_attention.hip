@@ -12,6 +12,8 @@
 // l % 32 of the result, rows 8 g + 4 (l / 32) + r in element 4 g + r.  Scores are made as K Q^T, so that a lane has those of one query;
 // what it has of them after exp2 is, in its order, an operand of V^T P^T again: no lane needs another one's.  V^T comes from
 // LDS through the transposing read: 16 lanes read 4 rows of 16 elements, and get 4 rows' elements of a column each.
+#include <utility>
+
 #include "lmt_device.h"
 #include "lmt_internal.h"
 #include "lmt_tiles.h"
@@ -39,11 +41,25 @@ __device__ __forceinline__ f32x16 mma(_Float16, const u32x4& a, const u32x4& b, 
 __device__ __forceinline__ uint32_t pack2(bf16_t, float x, float y) { return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{x, y}, bf16x2)); }
 __device__ __forceinline__ uint32_t pack2(_Float16, float x, float y) { return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{x, y}, f16x2)); }
 
+// f(0), f(1), ... f(N - 1), each with a number that is known when it is compiled: registers are not indexed.
+template <typename F, int... I>
+__device__ __forceinline__ void each_of(std::integer_sequence<int, I...>, F f) {
+  (f(std::integral_constant<int, I>{}), ...);
+}
+template <int N, typename F>
+__device__ __forceinline__ void each(F f) {
+  each_of(std::make_integer_sequence<int, N>{}, f);
+}
+
 __device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
-// The other half's value of the lane 32 further, or back.
-__device__ __forceinline__ float other_half(float x) {
+// A lane's value and that of the lane 32 further or back, joined.
+__device__ __forceinline__ float halves_max(float x) {
   const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  return __uint_as_float((threadIdx.x & 32u) ? r[0] : r[1]);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float halves_sum(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 __device__ __forceinline__ bool any(bool x) { return __builtin_amdgcn_ballot_w64(x) != 0; }
 // The largest of the lanes up to this one, by moves between lanes: within rows of 16, then from the end of the rows in front.  -1 is the least.
@@ -207,14 +223,23 @@ struct Stage {
   static constexpr int pieces = D / 8, loads = kTile * pieces / THREADS, step = THREADS / pieces;
   static_assert(step % 16 == 0, "rows that a thread loads turn their pieces alike");
   u32x4 w[DIRECT ? 1 : loads];
+  uint32_t at;  // DIRECT: of this thread's first piece, in bytes behind the tile's first row
+  __device__ __forceinline__ void set(const Heads& x, uint32_t size) {
+    if constexpr (DIRECT) at = threadIdx.x / pieces * (uint32_t)x.row * 2u + piece_at(threadIdx.x % pieces ^ turn<D>(threadIdx.x / pieces), size) * 2u;
+  }
   __device__ __forceinline__ void fetch(const T* head, const Heads& x, uint32_t first, uint32_t rows, uint32_t size, uint8_t* tile) {
     const uint32_t r = threadIdx.x / pieces, slot = threadIdx.x % pieces;
     if constexpr (DIRECT) {
-      const uint32_t row = (uint32_t)x.row * 2u, at = piece_at(slot ^ turn<D>(r), size) * 2u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+      const uint32_t row = (uint32_t)x.row * 2u, last = rows - 1u - first;
+      uint8_t* to = tile + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * 1024u;
       const uint8_t* base = reinterpret_cast<const uint8_t*>(row_of(head, x, first));
-      const uint32_t last = rows - 1u - first;
+      if (last >= kTile - 1u) {
 #pragma unroll
-      for (int j = 0; j < loads; ++j) send_to_lds(base, min(r + j * step, last) * row + at, 0, tile + (j * THREADS + wave * 64u) * 16u);
+        for (uint32_t j = 0; j < loads; ++j) send_to_lds(base, at, j * step * row, to + j * THREADS * 16u);
+      } else {
+#pragma unroll
+        for (uint32_t j = 0; j < loads; ++j) send_to_lds(base, at - r * row + min(r + j * step, last) * row, 0, to + j * THREADS * 16u);
+      }
     } else {
 #pragma unroll
       for (int j = 0; j < loads; ++j) w[j] = load_piece(row_of(head, x, min(first + r + j * step, rows - 1u)), slot, size);
@@ -465,7 +490,7 @@ __device__ __forceinline__ void attend_row(const Attention& p, uint32_t head, ui
 // The scores of the next tile are made while those of this one go through exp2: matrix instructions and the others take turns in the
 // instruction stream, as one wavefront's do not overlap unless they are side by side in it.
 template <typename T, int D, bool PLAIN, bool DIRECT>
-__global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void k_attend(const Attention p, uint32_t tiles) {
+__global__ __launch_bounds__(kThreads, D == 64 && DIRECT ? 3 : 2) void k_attend(const Attention p, uint32_t tiles) {
   __shared__ __align__(16) uint8_t keys[2][kTile * D * 2], values[2][kTile * D * 2];
   __shared__ Seen<kRows> seen;
   uint32_t tile, head;
@@ -487,6 +512,7 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void k_attend(const Atte
   float m = -kInf, sum[4] = {};
   f32x16 o[D / 32] = {}, s[2] = {};
   Stage<T, D, kThreads, DIRECT> next_k, next_v;
+  next_k.set(p.k, p.size), next_v.set(p.v, p.size);
   if (first < last) {
     next_k.fetch(k, p.k, (uint32_t)first, p.rows, p.size, keys[0]), next_v.fetch(v, p.v, (uint32_t)first, p.rows, p.size, values[0]);
     next_k.put(keys[0]), next_v.put(values[0]);
@@ -518,7 +544,7 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void k_attend(const Atte
       float top = s[0][0];
 #pragma unroll
       for (int e = 1; e < 32; ++e) top = fmaxf(top, s[e / 16][e % 16]);
-      top = fmaxf(top, other_half(top));
+      top = halves_max(top);
       if constexpr (PLAIN) top *= score.by;
       if (any(top > m + kSlack)) {
         const float up = fmaxf(m, top), by = m == -kInf ? 0.f : exp2_of(m - up);
@@ -542,23 +568,23 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void k_attend(const Atte
       };
 #pragma unroll
       for (int t = 0; t < kAhead - 1; ++t) ahead[t] = operand(t);
-#pragma unroll
-      for (int t = 0; t < 2 * kSteps; ++t) {
+      each<2 * kSteps>([&](auto number) {
+        constexpr int t = decltype(number)::value;
         if (t + kAhead - 1 < 2 * kSteps) ahead[(t + kAhead - 1) % kAhead] = operand(t + kAhead - 1);
-        if (t < kSteps) {
+        if constexpr (t < kSteps) {
           next[t % 2] = mma(T{}, ahead[t % kAhead], q.w[t / 2], next[t % 2]);
 #pragma unroll
           for (int e = t * kEach; e < (t + 1) * kEach; ++e) {
             const float x = exp2_of(PLAIN ? __builtin_fmaf(s[e / 16][e % 16], score.by, -base) : s[e / 16][e % 16] - base);
             s[e / 16][e % 16] = x, sum[e % 4] += x;
           }
-          if ((t + 1) * kEach % 8 == 0) w[((t + 1) * kEach - 8) / 16][((t + 1) * kEach - 8) / 8 % 2] = packed<T>(s[((t + 1) * kEach - 8) / 16], ((t + 1) * kEach - 8) / 8 % 2);
+          if constexpr ((t + 1) * kEach % 8 == 0) w[((t + 1) * kEach - 8) / 16][((t + 1) * kEach - 8) / 8 % 2] = packed<T>(s[((t + 1) * kEach - 8) / 16], ((t + 1) * kEach - 8) / 8 % 2);
         } else {
-          const int u = t - kSteps, of = u / (D / 32), d = u % (D / 32);
+          constexpr int u = t - kSteps, of = u / (D / 32), d = u % (D / 32);
           o[d] = mma(T{}, ahead[t % kAhead], w[of / 2][of % 2], o[d]);
         }
         __builtin_amdgcn_sched_barrier(0);
-      }
+      });
 #pragma unroll
       for (int b = 0; b < 2; ++b) s[b] = next[b];
     } else if (more && span.touches(at + kTile, kTile)) {
@@ -574,7 +600,7 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void k_attend(const Atte
     arrived();
   }
   float l = (sum[0] + sum[1]) + (sum[2] + sum[3]);
-  l += other_half(l);
+  l = halves_sum(l);
   const bool some = span.lo < span.hi, here = i < p.rows;
   const bool again = some && !(finite<D>(o) && finite(l));
   const uint64_t rows_again = __builtin_amdgcn_ballot_w64(again);
@@ -656,6 +682,12 @@ __device__ __forceinline__ void grad_q_row(const Attention& p, uint32_t head, ui
     if (lane + 64u * e < p.size) store1(to + lane + 64u * e, from_f32<T>(sum[e] * p.scale));
 }
 
+// Scores that the column's row does not see, its first element `from` places into what it sees: none.  Their weights are 0, and so are
+// weights times what is finite; what is not shows in the sums.
+__device__ __forceinline__ void hide(f32x16& s, uint32_t from, uint32_t n) {
+#pragma unroll
+  for (int e = 0; e < 16; ++e) s[e] = from + (uint32_t)(8 * (e / 4) + e % 4) < n ? s[e] : -kInf;
+}
 // lse in units of log 2, as what is subtracted from scores: a row without weights has none.
 __device__ __forceinline__ float subtracted(float lse) { return lse == -kInf ? kInf : lse * kLog2e; }
 
@@ -682,7 +714,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_attend_grad_q(const Attention p
 #pragma unroll
       for (int e = 0; e < 8; ++e) delta = __builtin_fmaf(a.get(e), b.get(e), delta);
     }
-    delta += other_half(delta);
+    delta = halves_sum(delta);
   }
   const float lse = subtracted(load1(p.lse + (uint64_t)head * p.rows + held));
   find_seen<kRows, kThreads, false>(p, tile * kRows, seen);
@@ -700,6 +732,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_attend_grad_q(const Attention p
   range.begin();
   f32x16 sum[D / 32] = {};
   Stage<T, D, kThreads, DIRECT> next_k, next_v;
+  next_k.set(p.k, p.size), next_v.set(p.v, p.size);
   if (first < last) {
     next_k.fetch(k, p.k, (uint32_t)first, p.rows, p.size, keys[0]), next_v.fetch(v, p.v, (uint32_t)first, p.rows, p.size, values[0]);
     next_k.put(keys[0]), next_v.put(values[0]);
@@ -709,38 +742,56 @@ __global__ __launch_bounds__(kThreads, 2) void k_attend_grad_q(const Attention p
   for (int at = first; at < last; at += kTile, now ^= 1u) {
     const bool more = at + kTile < last;
     if (more) next_k.fetch(k, p.k, (uint32_t)(at + kTile), p.rows, p.size, keys[now ^ 1u]), next_v.fetch(v, p.v, (uint32_t)(at + kTile), p.rows, p.size, values[now ^ 1u]);
+    if (span.touches(at, kTile)) {
+      {
+        constexpr int kHalf = D / 16, kSteps = 6 * kHalf;  // of k; of matrix instructions: scores and products with v of either half, then sums of either
+        f32x16 s[2][1] = {}, dp[2] = {}, bend[2][1];
+        u32x4 w[2][2], ahead[kAhead];
+        const auto operand = [&](int t) {
+          if (t < 4 * kHalf) return along.read(t % 2 ? values[now] : keys[now], t / (2 * kHalf), t / 2 % kHalf);
+          const int u = t - 4 * kHalf, b = u / kHalf, of = u % kHalf;
+          return across.read(keys[now], b, of / (D / 32), of % (D / 32));
+        };
+        const uint32_t from = (uint32_t)(at + 4 * (int)(lane >> 5) - span.lo), n = (uint32_t)(span.hi - span.lo);
+        const bool inside = span.inside(at, kTile);
+        const auto element = [&](int b, int e) {
+          const float x = exp2_of(PLAIN ? __builtin_fmaf(s[b][0][e], score.by, -lse) : s[b][0][e] - lse);
+          float d = __builtin_fmaf(dp[b][e], range.by, -delta * range.by) * x;
+          if constexpr (!PLAIN) d *= bend[b][0][e];
+          s[b][0][e] = d;
+        };
 #pragma unroll
-    for (int b = 0; b < 2; ++b) {
-      const int at_b = at + 32 * b;
-      if (!span.touches(at_b, 32)) continue;
-      f32x16 s[1] = {}, dp = {};
+        for (int t = 0; t < kAhead - 1; ++t) ahead[t] = operand(t);
+        each<kSteps>([&](auto number) {
+          constexpr int t = decltype(number)::value;
+          if (t + kAhead - 1 < kSteps) ahead[(t + kAhead - 1) % kAhead] = operand(t + kAhead - 1);
+          if constexpr (t < 4 * kHalf) {
+            constexpr int b = t / (2 * kHalf), c = t / 2 % kHalf;
+            if (t % 2) dp[b] = mma(T{}, ahead[t % kAhead], go.w[c], dp[b]);
+            else s[b][0] = mma(T{}, ahead[t % kAhead], q.w[c], s[b][0]);
+          } else {
+            constexpr int u = t - 4 * kHalf, b = u / kHalf, of = u % kHalf, d = of % (D / 32);
+            sum[d] = mma(T{}, ahead[t % kAhead], w[b][of / (D / 32)], sum[d]);
+          }
+          // the first half's elements beside the second half's scores, the second half's beside the first one's sums
+          if constexpr (!PLAIN) {
+            if constexpr (t == 2 * kHalf) score.of<1, true>(s[0], (float)(at + 4 * (int)(lane >> 5) - (int)i), bend[0]);
+            if constexpr (t == 4 * kHalf) score.of<1, true>(s[1], (float)(at + 32 + 4 * (int)(lane >> 5) - (int)i), bend[1]);
+          }
+          if constexpr (t == 2 * kHalf || t == 4 * kHalf) {
+            if (!inside) hide(s[t / (2 * kHalf) - 1][0], from + (t == 4 * kHalf ? 32u : 0u), n);
+          }
+          if constexpr (t >= 2 * kHalf && t < 5 * kHalf) {
+            constexpr int b = t >= 4 * kHalf, n_steps = b ? kHalf : 2 * kHalf, step = b ? t - 4 * kHalf : t - 2 * kHalf;
 #pragma unroll
-      for (int c = 0; c < D / 16; ++c) {
-        s[0] = mma(T{}, along.read(keys[now], b, c), q.w[c], s[0]);
-        dp = mma(T{}, along.read(values[now], b, c), go.w[c], dp);
-      }
-      const int j0 = at_b + 4 * (int)(lane >> 5);
-      const bool inside = span.inside(at_b, 32);
-      const uint32_t from = (uint32_t)(j0 - span.lo), n = (uint32_t)(span.hi - span.lo);
-      const float less = delta * range.by;
-      f32x16 bend[1];
-      if constexpr (!PLAIN) score.of<1, true>(s, (float)(j0 - (int)i), bend);
-#pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const float w = exp2_of(PLAIN ? __builtin_fmaf(s[0][e], score.by, -lse) : s[0][e] - lse);
-        s[0][e] = __builtin_fmaf(dp[e], range.by, -less) * w;
-        if constexpr (!PLAIN) s[0][e] *= bend[0][e];
-      }
-      if (!inside) {
-#pragma unroll
-        for (int e = 0; e < 16; ++e) s[0][e] = from + (uint32_t)(8 * (e / 4) + e % 4) < n ? s[0][e] : 0.f;
-      }
-      range.fit(s, sum);
-#pragma unroll
-      for (int c = 0; c < 2; ++c) {
-        const u32x4 w = packed<T>(s[0], c);
-#pragma unroll
-        for (int d = 0; d < D / 32; ++d) sum[d] = mma(T{}, across.read(keys[now], b, c, d), w, sum[d]);
+            for (int e = step * 16 / n_steps; e < (step + 1) * 16 / n_steps; ++e) element(b, e);
+            if constexpr (step + 1 == n_steps) {
+              range.fit(s[b], sum);
+              w[b][0] = packed<T>(s[b][0], 0), w[b][1] = packed<T>(s[b][0], 1);
+            }
+          }
+          __builtin_amdgcn_sched_barrier(0);
+        });
       }
     }
     if (more) next_k.put(keys[now ^ 1u]), next_v.put(values[now ^ 1u]);
@@ -858,6 +909,7 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 2 : 1) void k_attend_grad_kv(co
     next_q.put(queries[to]), next_go.put(grads[to]);
     if (threadIdx.x < kTile) lse[to][threadIdx.x] = subtracted(next_lse), delta[to][threadIdx.x] = next_delta;
   };
+  next_q.set(p.q, p.size), next_go.set(p.grad_out, p.size);
   if (first < last) fetch(h0, first, 0), put(0);
   arrived();
   uint32_t now = 0;
@@ -867,48 +919,69 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 2 : 1) void k_attend_grad_kv(co
     for (int at = first; at < last; at += kTile, now ^= 1u) {
       const bool wrap = at + kTile >= last, more = !wrap || head + 1u < h1;
       if (more) fetch(wrap ? head + 1u : head, wrap ? first : at + kTile, now ^ 1u);
+      if (span.touches(at, kTile)) {
+        {
+          constexpr int kHalf = D / 16, kSteps = 8 * kHalf;
+          f32x16 s[2][1] = {}, d[2][1] = {}, bend[2][1];
+          u32x4 w[2][2], x[2][2], ahead[kAhead];
+          f32x4 less[2], dots[2];  // of four rows, and of the next four
+          const int half = 4 * (int)(lane >> 5);
+          const auto rows = [&](int b, int g) {
+            less[g % 2] = *reinterpret_cast<const f32x4*>(&lse[now][32 * b + 8 * g + half]), dots[g % 2] = *reinterpret_cast<const f32x4*>(&delta[now][32 * b + 8 * g + half]);
+          };
+          const auto operand = [&](int t) {
+            if (t < 4 * kHalf) return along.read(t % 2 ? grads[now] : queries[now], t / (2 * kHalf), t / 2 % kHalf);
+            const int u = t - 4 * kHalf, b = u / (2 * kHalf), of = u / 2 % kHalf;
+            return across.read(u % 2 ? queries[now] : grads[now], b, of / (D / 32), of % (D / 32));
+          };
+          const uint32_t from = (uint32_t)(at + half - span.lo), n = (uint32_t)(span.hi - span.lo);
+          const bool inside = span.inside(at, kTile);
+          const auto element = [&](int b, int e) {
+            const int g = e / 4;
+            float p_ = exp2_of(PLAIN ? __builtin_fmaf(s[b][0][e], score.by, -less[g % 2][e % 4]) : s[b][0][e] - less[g % 2][e % 4]);
+            float d_ = __builtin_fmaf(d[b][0][e], range.by, -dots[g % 2][e % 4] * range.by) * p_;
+            if constexpr (!PLAIN) d_ *= bend[b][0][e];
+            if constexpr (kShift<T> != 0.f) p_ *= 0x1p14f;  // weights are at most 1
+            s[b][0][e] = p_, d[b][0][e] = d_;
+          };
 #pragma unroll
-      for (int b = 0; b < 2; ++b) {
-        const int at_b = at + 32 * b;
-        if (!span.touches(at_b, 32)) continue;
-        f32x16 s[1] = {}, d[1] = {}, bend[1];
-#pragma unroll
-        for (int c = 0; c < D / 16; ++c) {
-          s[0] = mma(T{}, along.read(queries[now], b, c), k.w[c], s[0]);
-          d[0] = mma(T{}, along.read(grads[now], b, c), v.w[c], d[0]);
-        }
-        const int half = 4 * (int)(lane >> 5), i0 = at_b + half;
-        const bool inside = span.inside(at_b, 32);
-        const uint32_t from = (uint32_t)(i0 - span.lo), n = (uint32_t)(span.hi - span.lo);
-        if constexpr (!PLAIN) score.of<1, true>(s, (float)(i0 - (int)j), bend);
-#pragma unroll
-        for (int g = 0; g < 4; ++g) {
-          const f32x4 less = *reinterpret_cast<const f32x4*>(&lse[now][32 * b + 8 * g + half]), dot_out = *reinterpret_cast<const f32x4*>(&delta[now][32 * b + 8 * g + half]);
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const int e = 4 * g + r;
-            const float w = exp2_of(PLAIN ? __builtin_fmaf(s[0][e], score.by, -less[r]) : s[0][e] - less[r]);
-            s[0][e] = w, d[0][e] = __builtin_fmaf(d[0][e], range.by, -dot_out[r] * range.by) * w;
-            if constexpr (!PLAIN) d[0][e] *= bend[0][e];
+          for (int t = 0; t < kAhead - 1; ++t) ahead[t] = operand(t);
+          each<kSteps>([&](auto number) {
+            constexpr int t = decltype(number)::value;
+            if (t + kAhead - 1 < kSteps) ahead[(t + kAhead - 1) % kAhead] = operand(t + kAhead - 1);
+            if constexpr (t < 4 * kHalf) {
+              constexpr int b = t / (2 * kHalf), c = t / 2 % kHalf;
+              if (t % 2) d[b][0] = mma(T{}, ahead[t % kAhead], v.w[c], d[b][0]);
+              else s[b][0] = mma(T{}, ahead[t % kAhead], k.w[c], s[b][0]);
+            } else {
+              constexpr int u = t - 4 * kHalf, b = u / (2 * kHalf), of = u / 2 % kHalf, e = of % (D / 32);
+              if (u % 2) dk[e] = mma(T{}, ahead[t % kAhead], x[b][of / (D / 32)], dk[e]);
+              else dv[e] = mma(T{}, ahead[t % kAhead], w[b][of / (D / 32)], dv[e]);
+            }
+            if constexpr (!PLAIN) {
+              if constexpr (t == 2 * kHalf) score.of<1, true>(s[0], (float)(at + half - (int)j), bend[0]);
+              if constexpr (t == 4 * kHalf) score.of<1, true>(s[1], (float)(at + 32 + half - (int)j), bend[1]);
+            }
+            if constexpr (t == 2 * kHalf || t == 4 * kHalf) {
+            if (!inside) hide(s[t / (2 * kHalf) - 1][0], from + (t == 4 * kHalf ? 32u : 0u), n);
           }
-        }
-        if (!inside) {
+            if constexpr (t == 2 * kHalf - 1) rows(0, 0);
+            if constexpr (t >= 2 * kHalf && t < 6 * kHalf) {
+              constexpr int b = t >= 4 * kHalf, step = t - (b ? 4 : 2) * kHalf;
 #pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            const bool in = from + (uint32_t)(8 * (e / 4) + e % 4) < n;
-            s[0][e] = in ? s[0][e] : 0.f, d[0][e] = in ? d[0][e] : 0.f;
-          }
-        }
-        range.fit(d, dk);
-        if constexpr (kShift<T> != 0.f) s[0] *= 0x1p14f;  // weights are at most 1
+              for (int e = step * 8 / kHalf; e < (step + 1) * 8 / kHalf; ++e) {
+                if (e % 4 == 0 && e < 12) rows(b, e / 4 + 1);
+                element(b, e);
+              }
+              if constexpr (step + 1 == 2 * kHalf) {
+                if constexpr (b == 0) rows(1, 0);
+                range.fit(d[b], dk);
 #pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          const u32x4 w = packed<T>(s[0], c), x = packed<T>(d[0], c);
-#pragma unroll
-          for (int e = 0; e < D / 32; ++e) {
-            dv[e] = mma(T{}, across.read(grads[now], b, c, e), w, dv[e]);
-            dk[e] = mma(T{}, across.read(queries[now], b, c, e), x, dk[e]);
-          }
+                for (int c = 0; c < 2; ++c) w[b][c] = packed<T>(s[b][0], c), x[b][c] = packed<T>(d[b][0], c);
+              }
+            }
+            __builtin_amdgcn_sched_barrier(0);
+          });
         }
       }
       if (more) put(now ^ 1u);
