@@ -447,12 +447,22 @@ constexpr float kShift = 0.f;
 template <>
 constexpr float kShift<_Float16> = 7.f;
 
-// Which head and block of rows a workgroup has: an XCD has one head after the other, so that its L2 sees the same keys again and again; causal: long
-// rows first.
-__device__ __forceinline__ void place(uint32_t tiles, uint32_t lists, bool backwards, uint32_t* tile, uint32_t* list) {
-  const uint32_t id = (uint32_t)neighbours(blockIdx.x, tiles * lists);
-  *list = id / tiles, *tile = id % tiles;
-  if (backwards) *tile = tiles - 1u - *tile;
+// Which head and block of rows a workgroup has.  An XCD, which takes every eighth workgroup, has one head after the other, so that its L2 sees the
+// same keys again and again.  CAUSAL, where blocks are from 1 to `tiles` long: the longest of all heads that an XCD has come first (kFirst or kLast says
+// which end that is), since those that come last decide when it ends; heads that do not divide by XCDs go over all of them.
+// 16 heads of 8 192 rows of 64: one head after the other 213 us, longest first 183.
+enum Order { kAny, kFirst, kLast };
+__device__ __forceinline__ void place(uint32_t tiles, uint32_t lists, Order longest, uint32_t* tile, uint32_t* list) {
+  constexpr uint32_t kXcds = 8;
+  if (longest == kAny) {
+    const uint32_t id = (uint32_t)neighbours(blockIdx.x, tiles * lists);
+    *list = id / tiles, *tile = id % tiles;
+    return;
+  }
+  const uint32_t of_xcd = lists / kXcds;
+  if (lists % kXcds == 0) *list = blockIdx.x % kXcds * of_xcd + blockIdx.x / kXcds % of_xcd, *tile = blockIdx.x / kXcds / of_xcd;
+  else *list = blockIdx.x % lists, *tile = blockIdx.x / lists;
+  if (longest == kLast) *tile = tiles - 1u - *tile;
 }
 
 // ---- forward ------------------------------------------------------------------------------------
@@ -494,7 +504,7 @@ __global__ __launch_bounds__(kThreads, D == 64 && DIRECT ? 3 : 2) void k_attend(
   __shared__ __align__(16) uint8_t keys[2][kTile * D * 2], values[2][kTile * D * 2];
   __shared__ Seen<kRows> seen;
   uint32_t tile, head;
-  place(tiles, p.heads, p.causal, &tile, &head);
+  place(tiles, p.heads, p.causal ? kLast : kAny, &tile, &head);
   const uint32_t kv = head / p.group, wave = threadIdx.x >> 6, lane = threadIdx.x & 63u, row = wave * 32u + (lane & 31u), i = tile * kRows + row;
   const T *k = head_of<T>(p.k, kv), *v = head_of<T>(p.v, kv);
   check_sequences(p);
@@ -698,7 +708,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_attend_grad_q(const Attention p
   __shared__ __align__(16) uint8_t keys[2][kTile * D * 2], values[2][kTile * D * 2];
   __shared__ Seen<kRows> seen;
   uint32_t tile, head;
-  place(tiles, p.heads, p.causal, &tile, &head);
+  place(tiles, p.heads, p.causal ? kLast : kAny, &tile, &head);
   const uint32_t kv = head / p.group, wave = threadIdx.x >> 6, lane = threadIdx.x & 63u, row = wave * 32u + (lane & 31u), i = tile * kRows + row, held = min(i, p.rows - 1u);
   const T *k = head_of<T>(p.k, kv), *v = head_of<T>(p.v, kv);
   check_sequences(p);
@@ -881,7 +891,7 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 2 : 1) void k_attend_grad_kv(co
   __shared__ __align__(16) float lse[2][kTile], delta[2][kTile];
   __shared__ Seen<kRows> seen;
   uint32_t tile, list;
-  place(tiles, p.kv_heads * p.parts, false, &tile, &list);
+  place(tiles, p.kv_heads * p.parts, p.causal ? kFirst : kAny, &tile, &list);
   const uint32_t kv = list / p.parts, part = list % p.parts, h0 = kv * p.group + part * p.group / p.parts, h1 = kv * p.group + (part + 1u) * p.group / p.parts;
   const uint32_t wave = threadIdx.x >> 6, lane = threadIdx.x & 63u, row = wave * 32u + (lane & 31u), j = tile * kRows + row, held = min(j, p.rows - 1u);
   Row<T, D> k, v;
