@@ -21,6 +21,11 @@ __device__ __forceinline__ f32x16 mma(bf16_t, const u32x4& a, const u32x4& b, co
 __device__ __forceinline__ f32x16 mma(_Float16, const u32x4& a, const u32x4& b, const f32x16& c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
 }
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t pack2(bf16_t, float x, float y) { return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{x, y}, bf16x2)); }
+__device__ __forceinline__ uint32_t pack2(_Float16, float x, float y) { return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{x, y}, f16x2)); }
 __device__ __forceinline__ float other_half(float x) {
   const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
   return __uint_as_float((threadIdx.x & 32u) ? r[0] : r[1]);
@@ -272,10 +277,73 @@ __global__ __launch_bounds__(S::threads, 2) void k_linear(const Product p) {
     }
     return;
   }
+  if constexpr (MODE == kGrad) {
+    // 64 rows of 64 classes at a time through the wavefront's part of LDS, in 16 bits: g as it is, which goes out by rows, and times its row's weight, which the
+    // transposing reads give by classes.  16-byte pieces of a row change places by its number, so that both meet every bank once.
+    uint8_t *plain = stage + wave * 16384u, *weighted = plain + 8192u;
+    const float columns = column_scale<T>(load1(p.largest));
+    const auto turn = [](uint32_t r) { return (r >> 1 & 1u) << 2 | (r >> 3 & 1u) << 1 | (r >> 2 & 1u); };
+    const uint32_t c0 = n0 + wn * 64u, half = lane >> 5;
+    const bool all_classes = p.first_class + c0 + 64u <= p.classes;
+#pragma unroll
+    for (int two = 0; two < S::TM / 2; ++two) {
+      const uint32_t r0 = (wm * S::TM + 2 * two) * 32u;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const uint32_t r = i * 32u + (lane & 31u);
+        const RowOf of = row_of[r0 + r];
+        const float by = of.weight * columns;
+        const uint32_t hit = (uint32_t)of.target - p.first_class - c0 - 4u * half;  // the target among this lane's classes
+        const bool none = of.target < 0;
+#pragma unroll
+        for (int j = 0; j < S::TN; ++j)
+#pragma unroll
+          for (uint32_t g = 0; g < 4; ++g) {
+            float f[4];
+#pragma unroll
+            for (uint32_t e = 0; e < 4; ++e) {
+              const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(acc[2 * two + i][j][4 * g + e] - of.top, kLog2e, -of.log_sum));
+              f[e] = none ? 0.f : hit == 32u * j + 8u * g + e ? w - 1.f : w;
+              if (!all_classes) f[e] = p.first_class + c0 + 4u * half + 32u * j + 8u * g + e < p.classes ? f[e] : 0.f;
+            }
+            const uint32_t at = r * 128u + ((j * 4u + g) ^ turn(r)) * 16u + half * 8u;
+            if (p.g) *reinterpret_cast<u32x2*>(plain + at) = u32x2{pack2(T{}, f[0] * kRowScale<T>, f[1] * kRowScale<T>), pack2(T{}, f[2] * kRowScale<T>, f[3] * kRowScale<T>)};
+            if (p.gt) *reinterpret_cast<u32x2*>(weighted + at) = none ? u32x2{0, 0} : u32x2{pack2(T{}, f[0] * by, f[1] * by), pack2(T{}, f[2] * by, f[3] * by)};
+          }
+      }
+      __builtin_amdgcn_wave_barrier();
+      if (p.g) {
+#pragma unroll
+        for (uint32_t it = 0; it < 8; ++it) {
+          const uint32_t r = it * 8u + lane / 8u, piece = lane & 7u, i = m0 + r0 + r, j = c0 + piece * 8u;
+          const u32x4 v = *reinterpret_cast<const u32x4*>(plain + r * 128u + (piece ^ turn(r)) * 16u);
+          if (i < p.m && j < p.cols) *(LMT_GLOBAL u32x4*)(static_cast<T*>(p.g) + (uint64_t)i * p.g_ld + j) = v;
+        }
+      }
+      if (p.gt) {
+        const uint32_t q = lane >> 4, l = lane & 15u;
+#pragma unroll
+        for (uint32_t it = 0; it < 2; ++it)  // 8 rows of every class: pieces 4 it + q of 64 rows
+#pragma unroll
+          for (uint32_t b = 0; b < 4; ++b) {  // 16 classes
+            u32x2 v[2];
+#pragma unroll
+            for (uint32_t e = 0; e < 2; ++e) {
+              const uint32_t r = (4u * it + q) * 8u + 4u * e + l / 4u;
+              v[e] = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(weighted + r * 128u + ((2u * b + (l >> 1 & 1u)) ^ turn(r)) * 16u + (l & 1u) * 8u)));
+            }
+            const uint32_t j = c0 + 16u * b + l, i = m0 + r0 + (4u * it + q) * 8u;
+            if (i < p.gt_ld && j < p.cols) *(LMT_GLOBAL u32x4*)(static_cast<T*>(p.gt) + (uint64_t)j * p.gt_ld + i) = u32x4{v[0].x, v[0].y, v[1].x, v[1].y};
+          }
+      }
+      __builtin_amdgcn_wave_barrier();
+    }
+    return;
+  }
   // 64 rows of 64 at a time through LDS, a wavefront in its own part of it
   float* mine = reinterpret_cast<float*>(stage) + wave * (64 * 64);
-  const float columns = MODE == kGrad ? column_scale<T>(load1(p.largest)) : MODE == kSum && p.largest ? 1.f / column_scale<T>(load1(p.largest)) : 1.f;
-  float* part = MODE == kSum && p.part ? p.part + (uint64_t)split * p.m * p.n : nullptr;
+  const float columns = p.largest ? 1.f / column_scale<T>(load1(p.largest)) : 1.f;
+  float* part = p.part ? p.part + (uint64_t)split * p.m * p.n : nullptr;
 #pragma unroll
   for (int half = 0; half < S::TM / 2; ++half) {
 #pragma unroll
@@ -290,7 +358,7 @@ __global__ __launch_bounds__(S::threads, 2) void k_linear(const Product p) {
         }
     __builtin_amdgcn_wave_barrier();
     const uint32_t r0 = (wm * S::TM + 2 * half) * 32u, c0 = n0 + wn * 64u;
-    constexpr int N = MODE == kGrad ? 8 : 16 / sizeof(TC);  // elements a lane writes
+    constexpr int N = 16 / sizeof(TC);  // elements a lane writes
 #pragma unroll
     for (uint32_t it = 0; it < 64u * 64u / (64u * N); ++it) {
       const uint32_t e = it * 64u + lane, r = e / (64u / N), col = e % (64u / N) * N;
@@ -301,55 +369,18 @@ __global__ __launch_bounds__(S::threads, 2) void k_linear(const Product p) {
         f[v] = d.x, f[v + 1] = d.y, f[v + 2] = d.z, f[v + 3] = d.w;
       }
       const uint32_t i = m0 + r0 + r, j = c0 + col;
-      if constexpr (MODE == kGrad) {
-        const RowOf of = row_of[r0 + r];
+      if (i >= p.m) continue;
+      if (part) {
+        put<float, N>(part + (uint64_t)i * p.n, j, p.n, f, false);
+      } else {
+        const float by = p.by_row ? p.rows[i].weight * (1.f / kRowScale<T>) : columns;
+        const bool none = p.by_row && p.rows[i].target < 0;
 #pragma unroll
-        for (int v = 0; v < N; ++v) {
-          const uint32_t c = p.first_class + j + v;
-          const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(f[v] - of.top, kLog2e, -of.log_sum)) - ((int)c == of.target ? 1.f : 0.f);
-          f[v] = of.target >= 0 && c < p.classes ? w : 0.f;
-        }
-#pragma unroll
-        for (uint32_t v = 0; v < N; v += 4) *reinterpret_cast<f32x4*>(mine + r * 64u + ((col / 4u + v / 4u) ^ (r & 15u)) * 4u) = f32x4{f[v], f[v + 1], f[v + 2], f[v + 3]};
-        if (p.g && i < p.m && j < p.cols) {
-          Vec<T, 8> out;
-#pragma unroll
-          for (int v = 0; v < N; ++v) f[v] *= kRowScale<T>;
-          out.set(f);
-          *(LMT_GLOBAL u32x4*)(static_cast<T*>(p.g) + (uint64_t)i * p.g_ld + j) = u32x4{out.w[0], out.w[1], out.w[2], out.w[3]};
-        }
-      } else if (i < p.m) {
-        if (part) {
-          put<float, N>(part + (uint64_t)i * p.n, j, p.n, f, false);
-        } else {
-          const float by = p.by_row ? p.rows[i].weight * (1.f / kRowScale<T>) : columns;
-          const bool none = p.by_row && p.rows[i].target < 0;
-#pragma unroll
-          for (int v = 0; v < N; ++v) f[v] = none ? 0.f : f[v] * by;
-          put<TC, N>(static_cast<TC*>(p.c) + (uint64_t)i * p.ldc, j, p.n, f, p.accumulate);
-        }
+        for (int v = 0; v < N; ++v) f[v] = none ? 0.f : f[v] * by;
+        put<TC, N>(static_cast<TC*>(p.c) + (uint64_t)i * p.ldc, j, p.n, f, p.accumulate);
       }
     }
     __builtin_amdgcn_wave_barrier();
-    if constexpr (MODE == kGrad) {
-      if (p.gt) {
-#pragma unroll
-        for (uint32_t it = 0; it < 8; ++it) {  // lane: a class; 8 rows
-          float f[8];
-#pragma unroll
-          for (uint32_t v = 0; v < 8; ++v) {
-            const uint32_t r = it * 8u + v;
-            f[v] = mine[r * 64u + ((lane / 4u) ^ (r & 15u)) * 4u + (lane & 3u)] * (row_of[r0 + r].weight * columns);
-            if (row_of[r0 + r].target < 0) f[v] = 0.f;
-          }
-          Vec<T, 8> out;
-          out.set(f);
-          const uint32_t i = m0 + r0 + it * 8u;
-          if (i < p.gt_ld && c0 + lane < p.cols) *(LMT_GLOBAL u32x4*)(static_cast<T*>(p.gt) + (uint64_t)(c0 + lane) * p.gt_ld + i) = u32x4{out.w[0], out.w[1], out.w[2], out.w[3]};
-        }
-        __builtin_amdgcn_wave_barrier();
-      }
-    }
   }
 }
 
@@ -388,32 +419,31 @@ __global__ __launch_bounds__(256) void k_linear_targets(const LinearLoss p, RowO
   if (bad && p.status) atomicOr(p.status, LMT_STATUS_BAD_TARGET);
   rows[i] = {0.f, 0.f, t < 0 ? 0.f : p.weights ? load1(p.weights + i) : 1.f, t};
 }
-// Behind it: the tiles' maxima and sums joined, the loss.
+// Behind it: the tiles' maxima and sums joined, the loss.  16 threads a row, each an equal part of the tiles, then two by two.
+__device__ __forceinline__ float2 joined(float2 a, float2 b) {
+  const float top = fmaxf(a.x, b.x);
+  return {top, (a.y == 0.f ? 0.f : a.y * __builtin_amdgcn_exp2f((a.x - top) * kLog2e)) + (b.y == 0.f ? 0.f : b.y * __builtin_amdgcn_exp2f((b.x - top) * kLog2e))};
+}
 __global__ __launch_bounds__(256) void k_linear_rows(const LinearLoss p, RowOf* rows, const float2* sums, const float* hit, uint32_t tiles, uint32_t* largest) {
-  const uint32_t i = blockIdx.x * 256u + threadIdx.x;
-  uint32_t size = 0;
-  if (i < p.rows) {
-    float top = -kInf, sum = 0;
-    for (uint32_t t = 0; t < tiles; ++t) {
-      const float2 x = sums[(uint64_t)t * p.rows + i];
-      const float up = fmaxf(top, x.x);
-      sum = (sum == 0.f ? 0.f : sum * __builtin_amdgcn_exp2f((top - up) * kLog2e)) + (x.y == 0.f ? 0.f : x.y * __builtin_amdgcn_exp2f((x.x - up) * kLog2e));
-      top = up;
-    }
-    RowOf r = rows[i];
-    const float log_sum = __builtin_amdgcn_logf(sum);
-    if (p.lse) store1(p.lse + i, __builtin_fmaf(log_sum, kLn2, top));
-    if (p.loss) store1(p.loss + i, r.target < 0 ? 0.f : r.weight * __builtin_fmaf(log_sum, kLn2, top - load1(hit + i)));
-    r.top = top, r.log_sum = log_sum;
-    rows[i] = r;
-    size = __float_as_uint(r.weight) & 0x7fffffffu;
-    if (size >= 0x7f800000u) size = 0;
-  }
-  if (largest) {
+  __shared__ float2 part[16][17];
+  const uint32_t of = threadIdx.x / 16u, row = threadIdx.x % 16u, i = blockIdx.x * 16u + row, each = (tiles + 15u) / 16u;
+  float2 x = {-kInf, 0.f};
+  if (i < p.rows)
+    for (uint32_t t = of * each; t < min(tiles, (of + 1u) * each); ++t) x = joined(x, sums[(uint64_t)t * p.rows + i]);
+  part[of][row] = x;
+  __syncthreads();
+  if (threadIdx.x >= 16u) return;
 #pragma unroll
-    for (int d = 1; d < 64; d *= 2) size = max(size, (uint32_t)__shfl_xor((int)size, d));
-    if ((threadIdx.x & 63u) == 0 && size) atomicMax(largest, size);
-  }
+  for (uint32_t t = 1; t < 16; ++t) x = joined(x, part[t][row]);
+  if (i >= p.rows) return;
+  RowOf r = rows[i];
+  const float log_sum = __builtin_amdgcn_logf(x.y);
+  if (p.lse) store1(p.lse + i, __builtin_fmaf(log_sum, kLn2, x.x));
+  if (p.loss) store1(p.loss + i, r.target < 0 ? 0.f : r.weight * __builtin_fmaf(log_sum, kLn2, x.x - load1(hit + i)));
+  r.top = x.x, r.log_sum = log_sum;
+  rows[i] = r;
+  const uint32_t size = __float_as_uint(r.weight) & 0x7fffffffu;
+  if (largest && size < 0x7f800000u) atomicMax(largest, size);
 }
 
 // ---- host ---------------------------------------------------------------------------------------
@@ -424,16 +454,22 @@ typedef Shape<2, 2, 2, 2> Medium;  // 128 x 128
 struct Choice {
   bool large;
   Tiles t;
-  uint32_t tiles() const { return t.across * t.down; }
 };
+// What a form takes, in thirds of a microsecond: a round of large tiles, one a compute unit, 5 a block of k, one of medium ones, two a unit, 3; parts of k
+// where `split`, each written and read once in fp32 at 5 TB/s.
 Choice choose(uint64_t m, uint64_t n, uint64_t blocks, bool split) {
-  const uint64_t large = ceil_div(m, Large::rows_m) * ceil_div(n, Large::rows_n), medium = ceil_div(m, Medium::rows_m) * ceil_div(n, Medium::rows_n);
-  const bool wide = medium > 2 * kCus && 5 * ceil_div(large, kCus) <= 3 * ceil_div(medium, 2 * kCus);
-  const uint64_t tile = wide ? 256 : 128, tiles = wide ? large : medium;
-  uint64_t splits = 1;
-  if (split) splits = std::max<uint64_t>(1, std::min<uint64_t>({(wide ? 1u : 2u) * kCus / tiles, blocks / 8, 16}));
-  const uint64_t per = std::max<uint64_t>(1, ceil_div(blocks, splits));
-  return {wide, {(uint32_t)ceil_div(n, tile), (uint32_t)ceil_div(m, tile), (uint32_t)std::max<uint64_t>(1, ceil_div(blocks, per)), (uint32_t)per}};
+  Choice best = {};
+  double least = 0;
+  for (const bool wide : {true, false}) {
+    const uint64_t tile = wide ? 256 : 128, across = ceil_div(n, tile), down = ceil_div(m, tile), slots = wide ? kCus : 2 * kCus;
+    for (uint64_t splits = 1; splits <= (split ? 16 : 1); ++splits) {
+      const uint64_t per = std::max<uint64_t>(1, ceil_div(blocks, splits));
+      if (splits > 1 && (per < 8 || ceil_div(blocks, per) != splits)) continue;
+      const double takes = (double)ceil_div(across * down * splits, slots) * (double)(per + 4) * (wide ? 5 : 3) + (splits > 1 ? (double)(splits * m * n) * 8 / 5e6 * 3 + 12 : 0);
+      if (least == 0 || takes < least) least = takes, best = {wide, {(uint32_t)across, (uint32_t)down, (uint32_t)splits, (uint32_t)per}};
+    }
+  }
+  return best;
 }
 
 // Where things lie in the workspace, in bytes.
@@ -501,7 +537,7 @@ hipError_t launch_typed(const LinearLoss& q, hipStream_t s) {
   p.sums = reinterpret_cast<float2*>(at(w.sums)), p.hit = reinterpret_cast<float*>(at(w.hit));
   p.classes = q.classes, p.largest = largest;
   launch<T, kStats, float>(p, w.stats.large, s);
-  hipLaunchKernelGGL(k_linear_rows, dim3((uint32_t)ceil_div(q.rows, 256)), dim3(256), 0, s, q, rows, p.sums, p.hit, w.stats.t.across, largest);
+  hipLaunchKernelGGL(k_linear_rows, dim3((uint32_t)ceil_div(q.rows, 16)), dim3(256), 0, s, q, rows, p.sums, p.hit, w.stats.t.across, largest);
   if (!gradients) return hipGetLastError();
   for (uint64_t piece = 0; piece < w.pieces; ++piece) {
     const uint32_t first = (uint32_t)(piece * w.piece), n = (uint32_t)std::min<uint64_t>(w.piece, q.classes - first);
