@@ -1,9 +1,9 @@
 // Cross entropy of x table^T without the logits, and the gradients of both (lmt.h).
 //
 // Logits are made twice.  The first time each tile leaves its rows' maxima and sums of exponentials, which are joined to a maximum and a sum a
-// row; the second time, a piece of the classes at a time, tiles become g = softmax - onehot in 16 bits, as rows and as columns, which are multiplied by
-// the transposed table (grad_x, summed over the pieces) and the transposed x (grad_table).  Four products where three would do with the logits
-// in memory; what is kept instead is one piece of g, 2 x 2 bytes an element.
+// row; the second time, a piece of the classes at a time, tiles become g = w (softmax - onehot) in 16 bits, which is multiplied by the table (grad_x,
+// summed over the pieces) and, as its columns, by x (grad_table).  Four products where three would do with the logits in memory; what is kept
+// instead is one piece of g, 2 bytes an element.
 #include "lmt_device.h"
 #include "lmt_internal.h"
 #include "lmt_tiles.h"
@@ -37,72 +37,60 @@ struct RowOf {
   int target;
 };
 
-// ---- transposes and padded copies ---------------------------------------------------------
+// ---- copies ---------------------------------------------------------------------------------
 
-// A matrix by squares of 64 x 64: its copy with rows of whole blocks of 64, zeros behind their end, its transpose likewise, or both.
-struct Lay {
-  const void* from;
-  uint64_t ld;
-  uint32_t rows, cols, tiles_across, tiles;
-  void *copy, *turned;  // either may be nullptr
-};
 __device__ __forceinline__ int target_of(const void* targets, bool wide, uint64_t i, int64_t ignore, uint32_t classes, bool* bad) {
   const int64_t t = wide ? id_at<int64_t>(targets, i) : id_at<int32_t>(targets, i);
   *bad = t != ignore && (t < 0 || t >= (int64_t)classes);
   return t == ignore || *bad ? -1 : (int)t;
 }
-// Rows of x that are not counted are zeros in its transpose.
+// A matrix with rows of whole blocks of 64, zeros behind their end: x and the table where they do not lie like that, and x with zeros in the rows that
+// are not counted, for the table's gradient.  A thread 8 elements.
+struct Copy {
+  const void* from;
+  uint64_t ld;
+  uint32_t rows, cols;
+  bool counted;  // only the counted rows
+  void* to;      // or nullptr
+};
 template <typename T>
-__global__ __launch_bounds__(256) void k_lay(const Lay x, const Lay table, const LinearLoss p, uint32_t* largest) {
-  __shared__ uint16_t square[64][66];
-  const bool of_x = blockIdx.x < x.tiles;
-  const Lay& a = of_x ? x : table;
-  if (blockIdx.x == 0 && threadIdx.x == 0) *largest = 0;
-  const uint32_t tile = of_x ? blockIdx.x : blockIdx.x - x.tiles, r0 = tile / a.tiles_across * 64u, c0 = tile % a.tiles_across * 64u;
-  const uint32_t r = threadIdx.x / 8u, c = c0 + threadIdx.x % 8u * 8u;
-  const uint64_t row_out = round_up(a.cols, 64), row_turned = round_up(a.rows, 64);
-#pragma unroll
-  for (uint32_t k = 0; k < 2; ++k) {
-    const uint32_t i = r0 + r + 32u * k;
-    Vec<T, 8> v;
-    v.w[0] = v.w[1] = v.w[2] = v.w[3] = 0;
-    if (i < a.rows && c < a.cols) {
-      const T* from = static_cast<const T*>(a.from) + (uint64_t)i * a.ld + c;
-      if (c + 8u <= a.cols) load<false>(v, from);
-      else load_end(v, from, a.cols - c, 0.f);
+__global__ __launch_bounds__(256) void k_linear_copy(const Copy a, const Copy b, const Copy c, const LinearLoss p, uint32_t* largest) {
+  if (largest && blockIdx.x == 0 && threadIdx.x == 0) *largest = 0;
+  const uint32_t pieces = (uint32_t)(round_up(p.width, 64) / 8);
+  for (int n = 0; n < 3; ++n) {
+    const Copy& m = n == 0 ? a : n == 1 ? b : c;
+    if (!m.to) continue;
+    const uint64_t all = (uint64_t)m.rows * pieces;
+    for (uint64_t of = (uint64_t)blockIdx.x * 256u + threadIdx.x; of < all; of += (uint64_t)gridDim.x * 256u) {
+      const uint64_t i = of / pieces;
+      const uint32_t j = (uint32_t)(of % pieces) * 8u;
+      bool bad;
+      Vec<T, 8> v;
+      v.w[0] = v.w[1] = v.w[2] = v.w[3] = 0;
+      if (j < m.cols && !(m.counted && target_of(p.targets, p.wide_targets, i, p.ignore, p.classes, &bad) < 0)) {
+        const T* from = static_cast<const T*>(m.from) + i * m.ld + j;
+        if (j + 8u <= m.cols) load<false>(v, from);
+        else load_end(v, from, m.cols - j, 0.f);
+      }
+      *(LMT_GLOBAL u32x4*)(static_cast<T*>(m.to) + of * 8u) = u32x4{v.w[0], v.w[1], v.w[2], v.w[3]};
     }
-    if (a.copy && i < a.rows) *(LMT_GLOBAL u32x4*)(static_cast<T*>(a.copy) + i * row_out + c) = u32x4{v.w[0], v.w[1], v.w[2], v.w[3]};
-    bool bad;
-    const bool none = of_x && i < a.rows && target_of(p.targets, p.wide_targets, i, p.ignore, p.classes, &bad) < 0;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) square[r + 32u * k][threadIdx.x % 8u * 8u + e] = none ? (uint16_t)0 : (uint16_t)(v.w[e / 2] >> (16 * (e & 1)));
-  }
-  if (!a.turned) return;
-  __syncthreads();
-#pragma unroll
-  for (uint32_t k = 0; k < 2; ++k) {
-    const uint32_t j = r + 32u * k;  // a column of the square
-    uint32_t w[4];
-#pragma unroll
-    for (uint32_t e = 0; e < 4; ++e) w[e] = (uint32_t)square[threadIdx.x % 8u * 8u + 2 * e][j] | (uint32_t)square[threadIdx.x % 8u * 8u + 2 * e + 1][j] << 16;
-    if (c0 + j < a.cols) *(LMT_GLOBAL u32x4*)(static_cast<T*>(a.turned) + (c0 + j) * row_turned + r0 + threadIdx.x % 8u * 8u) = u32x4{w[0], w[1], w[2], w[3]};
   }
 }
 
 // ---- products -------------------------------------------------------------------------------
 
-// c[i][j] = sum over k of a[i][k] b[j][k]: rows of both in whole blocks of 64 elements, 16-byte aligned.
+// c[i][j] = sum over k of a[i][k] b[j][k], or of operands that lie the other way, a[k][i] or b[k][j]: rows of whole blocks of 64 elements, 16-byte aligned.
 struct Product {
   const uint8_t *a, *b;
   uint32_t a_row, b_row;  // bytes from row to row
-  uint32_t m, n, blocks;
+  uint32_t m, n, k, blocks;  // k: rows of b where it lies the other way; a has whole blocks, zeros behind k
   Tiles t;
   // what becomes of it
   const RowOf* rows;
   float2* sums;      // kStats: [tile of n][m]: maximum and sum of exp(x - maximum)
   float* hit;        // kStats: logit of the row's target
-  void *g, *gt;      // kGrad: [m][g_ld] and [piece's class][gt_ld], columns up to `cols`
-  uint64_t g_ld, gt_ld;
+  void *g, *gw;      // kGrad: [rows in whole blocks][g_ld], columns up to `cols`: as it is, and times the row's weight
+  uint64_t g_ld;
   uint32_t first_class, cols, classes;
   const uint32_t* largest;  // kGrad: bits of the largest weight
   void* c;           // kSum
@@ -112,8 +100,8 @@ struct Product {
 };
 enum Mode { kStats, kGrad, kSum };
 
-// fp16: elements of g are multiplied by 2^14 as rows, where they are at most 1, and by a power of two that brings the largest weight to
-// 2^14 as columns.  bf16 has fp32's range.
+// bf16 has fp32's range: g has its row's weight in it, for both gradients.  In fp16 small weights would lose bits, so that there are two: without weights, times
+// 2^14 (it is at most 1), for grad_x, whose rows get theirs at the end, and with them, times a power of two that brings the largest to 2^14, for grad_table.
 template <typename T>
 constexpr bool kNarrow = false;
 template <>
@@ -146,7 +134,30 @@ __device__ __forceinline__ void put(TC* row, uint32_t j, uint32_t end, float (&f
 
 // The loop is that of 8-bit products (one block of k arrives while another is multiplied, two groups of wavefronts in turns where there are
 // eight), with 64 elements of 16 bits to a block.
-template <typename S, typename T, Mode MODE, typename TC>
+// Operands that lie the other way (TURN_A, TURN_B) are staged as 64 rows of k, as many elements as the tile has rows, and read with the transposing
+// read: 16 lanes read 4 rows of k of 16 elements, and get 4 k of an element each.  Their 64-byte parts change places by the row of k.
+template <int ROWS>  // of the tile
+struct Turned {
+  static constexpr uint32_t pieces = ROWS / 8, row = ROWS * 2;
+  // What thread `chunk` of a block's 16-byte pieces stages: row of k, and element.
+  static __device__ __forceinline__ void place(uint32_t chunk, uint32_t* k, uint32_t* element) {
+    *k = chunk / pieces, *element = (chunk % pieces ^ (*k & 3u) << 2) * 8u;
+  }
+  // Where a lane reads from for 32 elements from `first` on, k from 0 on.
+  static __device__ __forceinline__ uint32_t at(uint32_t first, uint32_t lane) {
+    const uint32_t k = 8u * (lane >> 5) + (lane >> 2 & 3u), element = first + 16u * (lane >> 4 & 1u) + 4u * (lane & 3u);
+    return k * row + (element / 8u ^ (k & 3u) << 2) * 16u + (lane & 1u) * 8u;
+  }
+  // 16 k from 16 c on.
+  static __device__ __forceinline__ u32x4 read(const uint8_t* from, int c) {
+    typedef __attribute__((address_space(3))) s16x4* At;
+    const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((At)(from + c * 16 * row)));
+    const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((At)(from + c * 16 * row + 4 * row)));
+    return u32x4{lo.x, lo.y, hi.x, hi.y};
+  }
+};
+
+template <typename S, typename T, Mode MODE, typename TC, bool TURN_A, bool TURN_B>
 __global__ __launch_bounds__(S::threads, 2) void k_linear(const Product p) {
   __shared__ __align__(16) uint8_t stage[S::lds];
   __shared__ RowOf row_of[S::rows_m];
@@ -157,25 +168,49 @@ __global__ __launch_bounds__(S::threads, 2) void k_linear(const Product p) {
   tile_of(p.t, blockIdx.x - split * n_tiles, &tile_m, &tile_n);
   const uint32_t m0 = tile_m * S::rows_m, n0 = tile_n * S::rows_n;
   const uint32_t first = split * p.t.split_blocks, end = min(p.blocks, first + p.t.split_blocks);
-  const uint8_t *a0 = p.a + (uint64_t)m0 * p.a_row, *b0 = p.b + (uint64_t)n0 * p.b_row;
+  typedef Turned<S::rows_m> TurnedA;
+  typedef Turned<S::rows_n> TurnedB;
+  const uint8_t *a0 = p.a + (TURN_A ? 2ull * m0 : (uint64_t)m0 * p.a_row), *b0 = p.b + (TURN_B ? 2ull * n0 : (uint64_t)n0 * p.b_row);
   const uint32_t last_m = p.m - 1u - m0, last_n = p.n - 1u - n0;
+  constexpr int kLoadsA = S::rows_m / (8 * S::waves);  // of 16 bytes per thread and block; the rest are b's
   uint32_t from[S::loads];
 #pragma unroll
   for (int j = 0; j < S::loads; ++j) {
-    const uint32_t r = (j * S::waves + wave) * 8u + lane / 8u;
-    const uint32_t piece = ((lane & 7u) ^ (r >> 1 & 7u)) * 16u;
-    from[j] = (j * S::waves * 8 < S::rows_m ? min(r, last_m) * p.a_row : min(r - S::rows_m, last_n) * p.b_row) + piece;
+    const bool of_a = j < kLoadsA;
+    if (of_a ? TURN_A : TURN_B) {
+      uint32_t k, element;
+      if (of_a) TurnedA::place((j * S::waves + wave) * 64u + lane, &k, &element), element = min(element, last_m & ~7u);
+      else TurnedB::place(((j - kLoadsA) * S::waves + wave) * 64u + lane, &k, &element), element = min(element, last_n & ~7u);
+      from[j] = k * (of_a ? p.a_row : p.b_row) + element * 2u;
+    } else {
+      const uint32_t r = (j * S::waves + wave) * 8u + lane / 8u;
+      const uint32_t piece = ((lane & 7u) ^ (r >> 1 & 7u)) * 16u;
+      from[j] = (of_a ? min(r, last_m) * p.a_row : min(r - S::rows_m, last_n) * p.b_row) + piece;
+    }
   }
   const auto fetch = [&](uint32_t block, uint32_t at) {
+    const uint8_t *a = a0 + (TURN_A ? (uint64_t)block * 64u * p.a_row : block * 128ull), *b = b0 + (TURN_B ? (uint64_t)block * 64u * p.b_row : block * 128ull);
+    const bool end_b = TURN_B && block * 64u + 64u > p.k;  // b's rows of k behind the last one are the last one again, a has zeros there
 #pragma unroll
-    for (int j = 0; j < S::loads; ++j)
-      send_to_lds(j * S::waves * 8 < S::rows_m ? a0 : b0, from[j], block * 128u, stage + at + (j * S::waves + wave) * 1024u);
+    for (int j = 0; j < S::loads; ++j) {
+      const bool of_a = j < kLoadsA;
+      uint32_t offset = from[j];
+      if (!of_a && end_b) {
+        const uint32_t k = (((j - kLoadsA) * S::waves + wave) * 64u + lane) / TurnedB::pieces;
+        offset -= (k - min(k, p.k - 1u - block * 64u)) * p.b_row;
+      }
+      send_to_lds(of_a ? a : b, offset, 0, stage + at + (j * S::waves + wave) * 1024u);
+    }
   };
-  uint32_t at[2][2];
+  uint32_t at[2][2], turned_a[S::TM], turned_b[S::TN];
 #pragma unroll
   for (uint32_t h = 0; h < 2; ++h)
 #pragma unroll
     for (uint32_t q = 0; q < 2; ++q) at[h][q] = (lane & 31u) * 128u + ((4u * h + 2u * q + (lane >> 5)) ^ (lane >> 1 & 7u)) * 16u;
+#pragma unroll
+  for (uint32_t f = 0; f < S::TM; ++f) turned_a[f] = TurnedA::at((wm * S::TM + f) * 32u, lane);
+#pragma unroll
+  for (uint32_t f = 0; f < S::TN; ++f) turned_b[f] = S::rows_m * 128u + TurnedB::at((wn * S::TN + f) * 32u, lane);
   const uint32_t a_at = wm * S::TM * 4096u, b_at = S::rows_m * 128u + wn * S::TN * 4096u;
   if constexpr (MODE == kStats || MODE == kGrad) {
     if (threadIdx.x < S::rows_m) {
@@ -200,11 +235,11 @@ __global__ __launch_bounds__(S::threads, 2) void k_linear(const Product p) {
 #pragma unroll
       for (int f = 0; f < S::TN; ++f)
 #pragma unroll
-        for (int q = 0; q < 2; ++q) x[f][q] = *reinterpret_cast<const u32x4*>(stage + now + b_at + f * 4096 + at[h][q]);
+        for (int q = 0; q < 2; ++q) x[f][q] = TURN_B ? TurnedB::read(stage + now + turned_b[f], 2 * h + q) : *reinterpret_cast<const u32x4*>(stage + now + b_at + f * 4096 + at[h][q]);
 #pragma unroll
       for (int f = 0; f < S::TM; ++f)
 #pragma unroll
-        for (int q = 0; q < 2; ++q) y[f][q] = *reinterpret_cast<const u32x4*>(stage + now + a_at + f * 4096 + at[h][q]);
+        for (int q = 0; q < 2; ++q) y[f][q] = TURN_A ? TurnedA::read(stage + now + turned_a[f], 2 * h + q) : *reinterpret_cast<const u32x4*>(stage + now + a_at + f * 4096 + at[h][q]);
       if constexpr (S::turns) {
         if (h == 0) reads_done_and_meet();
         else wait_and_meet<0>();
@@ -278,11 +313,11 @@ __global__ __launch_bounds__(S::threads, 2) void k_linear(const Product p) {
     return;
   }
   if constexpr (MODE == kGrad) {
-    // 64 rows of 64 classes at a time through the wavefront's part of LDS, in 16 bits: g as it is, which goes out by rows, and times its row's weight, which the
-    // transposing reads give by classes.  16-byte pieces of a row change places by its number, so that both meet every bank once.
+    // 64 rows of 64 classes at a time through the wavefront's part of LDS, in 16 bits, so that they leave by whole lines; 16-byte pieces of a row change
+    // places by its number
     uint8_t *plain = stage + wave * 16384u, *weighted = plain + 8192u;
     const float columns = column_scale<T>(load1(p.largest));
-    const auto turn = [](uint32_t r) { return (r >> 1 & 1u) << 2 | (r >> 3 & 1u) << 1 | (r >> 2 & 1u); };
+    const auto turn = [](uint32_t r) { return r >> 1 & 7u; };
     const uint32_t c0 = n0 + wn * 64u, half = lane >> 5;
     const bool all_classes = p.first_class + c0 + 64u <= p.classes;
 #pragma unroll
@@ -303,38 +338,25 @@ __global__ __launch_bounds__(S::threads, 2) void k_linear(const Product p) {
 #pragma unroll
             for (uint32_t e = 0; e < 4; ++e) {
               const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(acc[2 * two + i][j][4 * g + e] - of.top, kLog2e, -of.log_sum));
-              f[e] = none ? 0.f : hit == 32u * j + 8u * g + e ? w - 1.f : w;
+              f[e] = hit == 32u * j + 8u * g + e ? w - 1.f : w;
               if (!all_classes) f[e] = p.first_class + c0 + 4u * half + 32u * j + 8u * g + e < p.classes ? f[e] : 0.f;
             }
             const uint32_t at = r * 128u + ((j * 4u + g) ^ turn(r)) * 16u + half * 8u;
-            if (p.g) *reinterpret_cast<u32x2*>(plain + at) = u32x2{pack2(T{}, f[0] * kRowScale<T>, f[1] * kRowScale<T>), pack2(T{}, f[2] * kRowScale<T>, f[3] * kRowScale<T>)};
-            if (p.gt) *reinterpret_cast<u32x2*>(weighted + at) = none ? u32x2{0, 0} : u32x2{pack2(T{}, f[0] * by, f[1] * by), pack2(T{}, f[2] * by, f[3] * by)};
+            if (p.g) *reinterpret_cast<u32x2*>(plain + at) = none ? u32x2{0, 0} : u32x2{pack2(T{}, f[0] * kRowScale<T>, f[1] * kRowScale<T>), pack2(T{}, f[2] * kRowScale<T>, f[3] * kRowScale<T>)};
+            if (p.gw) *reinterpret_cast<u32x2*>(weighted + at) = none ? u32x2{0, 0} : u32x2{pack2(T{}, f[0] * by, f[1] * by), pack2(T{}, f[2] * by, f[3] * by)};
           }
       }
       __builtin_amdgcn_wave_barrier();
-      if (p.g) {
+#pragma unroll
+      for (int which = 0; which < 2; ++which) {
+        T* to = static_cast<T*>(which ? p.gw : p.g);
+        if (!to) continue;
 #pragma unroll
         for (uint32_t it = 0; it < 8; ++it) {
           const uint32_t r = it * 8u + lane / 8u, piece = lane & 7u, i = m0 + r0 + r, j = c0 + piece * 8u;
-          const u32x4 v = *reinterpret_cast<const u32x4*>(plain + r * 128u + (piece ^ turn(r)) * 16u);
-          if (i < p.m && j < p.cols) *(LMT_GLOBAL u32x4*)(static_cast<T*>(p.g) + (uint64_t)i * p.g_ld + j) = v;
+          const u32x4 v = *reinterpret_cast<const u32x4*>((which ? weighted : plain) + r * 128u + (piece ^ turn(r)) * 16u);
+          if (i < round_up(p.m, 64) && j < p.cols) *(LMT_GLOBAL u32x4*)(to + (uint64_t)i * p.g_ld + j) = v;
         }
-      }
-      if (p.gt) {
-        const uint32_t q = lane >> 4, l = lane & 15u;
-#pragma unroll
-        for (uint32_t it = 0; it < 2; ++it)  // 8 rows of every class: pieces 4 it + q of 64 rows
-#pragma unroll
-          for (uint32_t b = 0; b < 4; ++b) {  // 16 classes
-            u32x2 v[2];
-#pragma unroll
-            for (uint32_t e = 0; e < 2; ++e) {
-              const uint32_t r = (4u * it + q) * 8u + 4u * e + l / 4u;
-              v[e] = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(weighted + r * 128u + ((2u * b + (l >> 1 & 1u)) ^ turn(r)) * 16u + (l & 1u) * 8u)));
-            }
-            const uint32_t j = c0 + 16u * b + l, i = m0 + r0 + (4u * it + q) * 8u;
-            if (i < p.gt_ld && j < p.cols) *(LMT_GLOBAL u32x4*)(static_cast<T*>(p.gt) + (uint64_t)j * p.gt_ld + i) = u32x4{v[0].x, v[0].y, v[1].x, v[1].y};
-          }
       }
       __builtin_amdgcn_wave_barrier();
     }
@@ -400,7 +422,7 @@ __global__ __launch_bounds__(256) void k_linear_join(const Product p, uint32_t p
 #pragma unroll
       for (int e = 0; e < 4; ++e) f[e] += v.get(e);
     }
-    const float by = p.by_row ? p.rows[i].weight * (1.f / kRowScale<T>) : 1.f / column_scale<T>(load1(p.largest));
+    const float by = p.by_row ? p.rows[i].weight * (1.f / kRowScale<T>) : p.largest ? 1.f / column_scale<T>(load1(p.largest)) : 1.f;
     const bool none = p.by_row && p.rows[i].target < 0;
 #pragma unroll
     for (int e = 0; e < 4; ++e) f[e] = none ? 0.f : f[e] * by;
@@ -475,20 +497,20 @@ Choice choose(uint64_t m, uint64_t n, uint64_t blocks, bool split) {
 // Where things lie in the workspace, in bytes.
 struct Plan {
   uint64_t piece, pieces;             // classes of a piece, a multiple of 256
-  uint64_t x_row, rows_row, t_row;    // elements of padded rows: of x and table, of x's transpose and g's, of the table's
+  uint64_t x_row;                     // elements of padded rows of x and the table
   Choice stats, grad_x, grad_t;
-  uint64_t rows, sums, hit, largest, x, table, xt, tt, g, gt, part_x, part_t, end;
+  uint64_t rows, sums, hit, largest, x, table, counted, g, gw, part_x, part_t, end;
 };
-constexpr uint64_t kPiece = 1ull << 27;  // elements of g at a time: 256 MB, twice
-Plan plan_of(uint64_t n, uint64_t classes, uint64_t width, bool gradients) {
+constexpr uint64_t kPiece = 1ull << 27;  // elements of g at a time: 256 MB
+Plan plan_of(uint64_t n, uint64_t classes, uint64_t width, bool gradients, bool narrow) {
   Plan w = {};
-  w.x_row = round_up(width, 64), w.rows_row = round_up(n, 64), w.t_row = round_up(classes, 64);
+  w.x_row = round_up(width, 64);
   w.pieces = std::max<uint64_t>(1, ceil_div(n * classes, kPiece));
   w.piece = std::min(round_up(ceil_div(classes, w.pieces), 256), round_up(classes, 256));
   w.pieces = ceil_div(classes, w.piece);
   w.stats = choose(n, classes, w.x_row / 64, false);
   w.grad_x = choose(n, width, w.piece / 64, true);
-  w.grad_t = choose(w.piece, width, w.rows_row / 64, true);
+  w.grad_t = choose(w.piece, width, ceil_div(n, 64), true);
   const auto take = [&](uint64_t bytes) {
     const uint64_t at = w.end;
     w.end += round_up(bytes, 256);
@@ -497,81 +519,80 @@ Plan plan_of(uint64_t n, uint64_t classes, uint64_t width, bool gradients) {
   w.rows = take(n * sizeof(RowOf)), w.sums = take(w.stats.t.across * n * sizeof(float2)), w.hit = take(n * 4), w.largest = take(4);
   w.x = take(n * w.x_row * 2), w.table = take(classes * w.x_row * 2);
   if (gradients) {
-    w.xt = take(width * w.rows_row * 2), w.tt = take(width * w.t_row * 2);
-    w.g = take(n * w.piece * 2), w.gt = take(w.piece * w.rows_row * 2);
+    w.counted = take(n * w.x_row * 2);
+    w.g = take(round_up(n, 64) * w.piece * 2), w.gw = narrow ? take(round_up(n, 64) * w.piece * 2) : w.g;
     if (w.pieces * w.grad_x.t.splits > 1) w.part_x = take(w.pieces * w.grad_x.t.splits * n * width * 4);
     if (w.grad_t.t.splits > 1) w.part_t = take(w.grad_t.t.splits * w.piece * width * 4);
   }
   return w;
 }
 
-template <typename T, Mode MODE, typename TC>
+template <typename T, Mode MODE, typename TC, bool TURN_A, bool TURN_B>
 void launch(const Product& p, bool large, hipStream_t s) {
   const uint32_t grid = p.t.across * p.t.down * p.t.splits;
-  if (large) hipLaunchKernelGGL((k_linear<Large, T, MODE, TC>), dim3(grid), dim3(Large::threads), 0, s, p);
-  else hipLaunchKernelGGL((k_linear<Medium, T, MODE, TC>), dim3(grid), dim3(Medium::threads), 0, s, p);
+  if (large) hipLaunchKernelGGL((k_linear<Large, T, MODE, TC, TURN_A, TURN_B>), dim3(grid), dim3(Large::threads), 0, s, p);
+  else hipLaunchKernelGGL((k_linear<Medium, T, MODE, TC, TURN_A, TURN_B>), dim3(grid), dim3(Medium::threads), 0, s, p);
+}
+template <typename T, typename TC>
+void join(const Product& p, uint32_t parts, hipStream_t s) {
+  hipLaunchKernelGGL((k_linear_join<T, TC>), dim3((uint32_t)std::min<uint64_t>(ceil_div((uint64_t)p.m * ceil_div(p.n, 4), 256), 1u << 16)), dim3(256), 0, s, p, parts);
 }
 
 template <typename T>
 hipError_t launch_typed(const LinearLoss& q, hipStream_t s) {
   const bool gradients = q.grad_x || q.grad_table;
-  const Plan w = plan_of(q.rows, q.classes, q.width, gradients);
+  const Plan w = plan_of(q.rows, q.classes, q.width, gradients, kNarrow<T>);
   uint8_t* base = static_cast<uint8_t*>(q.workspace);
   const auto at = [&](uint64_t offset) { return base + offset; };
   RowOf* rows = reinterpret_cast<RowOf*>(at(w.rows));
   uint32_t* largest = gradients ? reinterpret_cast<uint32_t*>(at(w.largest)) : nullptr;
-  const auto as_it_is = [&](const void* x, uint64_t ld) { return q.width % 64 == 0 && ld % 8 == 0 && ((uintptr_t)x & 15u) == 0 && ld * 2 * 256 < 0xffffffffull; };
+  const auto as_it_is = [&](const void* x, uint64_t ld) { return q.width % 64 == 0 && ld % 8 == 0 && ((uintptr_t)x & 15u) == 0 && ld <= LMT_MAX_WIDTH; };
   const bool x_copy = !as_it_is(q.x, q.x_ld), table_copy = !as_it_is(q.table, q.table_ld);
-  const auto lay = [&](const void* from, uint64_t ld, uint32_t n, bool copy, uint64_t copy_at, bool turn, uint64_t turn_at) {
-    const uint32_t across = (uint32_t)ceil_div(q.width, 64);
-    return Lay{from, ld, n, q.width, across, copy || turn ? across * (uint32_t)ceil_div(n, 64) : 0u, copy ? at(copy_at) : nullptr, turn ? at(turn_at) : nullptr};
-  };
-  const Lay x = lay(q.x, q.x_ld, q.rows, x_copy, w.x, q.grad_table != nullptr, w.xt);
-  const Lay table = lay(q.table, q.table_ld, q.classes, table_copy, w.table, q.grad_x != nullptr, w.tt);
+  const Copy x{q.x, q.x_ld, q.rows, q.width, false, x_copy ? at(w.x) : nullptr}, table{q.table, q.table_ld, q.classes, q.width, false, table_copy ? at(w.table) : nullptr};
+  const Copy counted{q.x, q.x_ld, q.rows, q.width, true, q.grad_table ? at(w.counted) : nullptr};
   hipLaunchKernelGGL(k_linear_targets, dim3((uint32_t)ceil_div(q.rows, 256)), dim3(256), 0, s, q, rows);
-  if (x.tiles + table.tiles) hipLaunchKernelGGL((k_lay<T>), dim3(x.tiles + table.tiles), dim3(256), 0, s, x, table, q, reinterpret_cast<uint32_t*>(at(w.largest)));
+  if (x_copy || table_copy || gradients) {
+    const uint64_t most = std::max<uint64_t>((uint64_t)q.rows * w.x_row, table_copy ? (uint64_t)q.classes * w.x_row : 0);
+    hipLaunchKernelGGL((k_linear_copy<T>), dim3((uint32_t)std::min<uint64_t>(ceil_div(most, 2048), 1u << 16)), dim3(256), 0, s, x, table, counted, q, largest);
+  }
   Product p = {};
   p.a = x_copy ? at(w.x) : static_cast<const uint8_t*>(q.x), p.a_row = (uint32_t)(2 * (x_copy ? w.x_row : q.x_ld));
   p.b = table_copy ? at(w.table) : static_cast<const uint8_t*>(q.table), p.b_row = (uint32_t)(2 * (table_copy ? w.x_row : q.table_ld));
   p.m = q.rows, p.n = q.classes, p.blocks = (uint32_t)(w.x_row / 64), p.t = w.stats.t, p.rows = rows;
   p.sums = reinterpret_cast<float2*>(at(w.sums)), p.hit = reinterpret_cast<float*>(at(w.hit));
   p.classes = q.classes, p.largest = largest;
-  launch<T, kStats, float>(p, w.stats.large, s);
+  launch<T, kStats, float, false, false>(p, w.stats.large, s);
   hipLaunchKernelGGL(k_linear_rows, dim3((uint32_t)ceil_div(q.rows, 16)), dim3(256), 0, s, q, rows, p.sums, p.hit, w.stats.t.across, largest);
-  if (!gradients) return hipGetLastError();
-  for (uint64_t piece = 0; piece < w.pieces; ++piece) {
+  for (uint64_t piece = 0; gradients && piece < w.pieces; ++piece) {
     const uint32_t first = (uint32_t)(piece * w.piece), n = (uint32_t)std::min<uint64_t>(w.piece, q.classes - first);
     Product g = p;
-    g.b = p.b + (uint64_t)first * p.b_row, g.n = n, g.first_class = first, g.cols = (uint32_t)round_up(n, 64);
+    g.b = p.b + (uint64_t)first * p.b_row, g.n = n, g.first_class = first, g.cols = (uint32_t)round_up(n, 64), g.g_ld = w.piece;
     const Choice c = choose(q.rows, n, p.blocks, false);
-    g.t = c.t, g.g = q.grad_x ? at(w.g) : nullptr, g.g_ld = w.piece, g.gt = q.grad_table ? at(w.gt) : nullptr, g.gt_ld = w.rows_row;
-    launch<T, kGrad, T>(g, c.large, s);
-    if (q.grad_x) {
+    g.t = c.t, g.g = kNarrow<T> && q.grad_x ? at(w.g) : nullptr, g.gw = kNarrow<T> && !q.grad_table ? nullptr : at(w.gw);
+    launch<T, kGrad, T, false, false>(g, c.large, s);
+    if (q.grad_x) {  // g by the table's rows
       Product d = {};
-      d.a = at(w.g), d.a_row = (uint32_t)(2 * w.piece), d.b = at(w.tt) + 2ull * first, d.b_row = (uint32_t)(2 * w.t_row);
-      d.m = q.rows, d.n = q.width, d.blocks = g.cols / 64, d.t = w.grad_x.t, d.rows = rows, d.by_row = true;
+      d.a = at(w.g), d.a_row = (uint32_t)(2 * w.piece), d.b = g.b, d.b_row = p.b_row;
+      d.m = q.rows, d.n = q.width, d.k = n, d.blocks = g.cols / 64, d.t = w.grad_x.t, d.rows = rows, d.by_row = kNarrow<T>;
       d.c = q.grad_x, d.ldc = q.grad_x_ld;
       const uint32_t parts = (uint32_t)w.pieces * d.t.splits;
       float* sums = reinterpret_cast<float*>(at(w.part_x));
       if (parts > 1) d.part = sums + piece * d.t.splits * (uint64_t)q.rows * q.width;
-      launch<T, kSum, T>(d, w.grad_x.large, s);
-      if (parts > 1 && piece + 1 == w.pieces) {
-        d.part = sums;
-        hipLaunchKernelGGL((k_linear_join<T, T>), dim3((uint32_t)std::min<uint64_t>(ceil_div((uint64_t)d.m * ceil_div(d.n, 4), 256), 1u << 16)), dim3(256), 0, s, d, parts);
-      }
+      launch<T, kSum, T, false, true>(d, w.grad_x.large, s);
+      d.part = sums;
+      if (parts > 1 && piece + 1 == w.pieces) join<T, T>(d, parts, s);
     }
-    if (q.grad_table) {
+    if (q.grad_table) {  // g's columns by x's
       const auto typed = [&](auto tc) {
         typedef decltype(tc) TC;
         Product d = {};
-        d.a = at(w.gt), d.a_row = (uint32_t)(2 * w.rows_row), d.b = at(w.xt), d.b_row = (uint32_t)(2 * w.rows_row);
-        d.m = n, d.n = q.width, d.blocks = (uint32_t)(w.rows_row / 64), d.rows = rows, d.largest = largest, d.accumulate = q.accumulate;
+        d.a = at(w.gw), d.a_row = (uint32_t)(2 * w.piece), d.b = at(w.counted), d.b_row = (uint32_t)(2 * w.x_row);
+        d.m = n, d.n = q.width, d.k = q.rows, d.blocks = (uint32_t)ceil_div(q.rows, 64), d.largest = largest, d.accumulate = q.accumulate;
         d.t = w.grad_t.t, d.t.down = (uint32_t)ceil_div(n, w.grad_t.large ? Large::rows_m : Medium::rows_m);
         d.c = static_cast<TC*>(q.grad_table) + (uint64_t)first * q.grad_table_ld, d.ldc = q.grad_table_ld;
         if (d.t.splits > 1) d.part = reinterpret_cast<float*>(at(w.part_t));
-        launch<T, kSum, TC>(d, w.grad_t.large, s);
-        if (d.t.splits > 1)
-          hipLaunchKernelGGL((k_linear_join<T, TC>), dim3((uint32_t)std::min<uint64_t>(ceil_div((uint64_t)d.m * ceil_div(d.n, 4), 256), 1u << 16)), dim3(256), 0, s, d, d.t.splits);
+        launch<T, kSum, TC, true, true>(d, w.grad_t.large, s);
+        if (d.t.splits > 1) join<T, TC>(d, d.t.splits, s);
       };
       if (q.grad_table_f32) typed(float{});
       else typed(T{});
@@ -583,7 +604,7 @@ hipError_t launch_typed(const LinearLoss& q, hipStream_t s) {
 }  // namespace
 
 uint64_t linear_loss_workspace(uint64_t rows, uint64_t classes, uint64_t width, bool gradients) {
-  return rows && classes ? plan_of(rows, classes, width, gradients).end : 0;
+  return rows && classes ? plan_of(rows, classes, width, gradients, true).end : 0;
 }
 hipError_t launch_linear_loss(const LinearLoss& p, int dtype, hipStream_t s) {
   return dtype == LMT_F16 ? launch_typed<_Float16>(p, s) : launch_typed<bf16_t>(p, s);
