@@ -45,7 +45,7 @@ __device__ __forceinline__ int target_of(const void* targets, bool wide, uint64_
   return t == ignore || *bad ? -1 : (int)t;
 }
 // A matrix with rows of whole blocks of 64, zeros behind their end: x and the table where they do not lie like that, and x with zeros in the rows that
-// are not counted, for the table's gradient.  A thread 8 elements.
+// are not counted, for the table's gradient.  A thread 8 elements.  And what rows' targets and weights are.
 struct Copy {
   const void* from;
   uint64_t ld;
@@ -54,8 +54,14 @@ struct Copy {
   void* to;      // or nullptr
 };
 template <typename T>
-__global__ __launch_bounds__(256) void k_linear_copy(const Copy a, const Copy b, const Copy c, const LinearLoss p, uint32_t* largest) {
+__global__ __launch_bounds__(256) void k_linear_begin(const Copy a, const Copy b, const Copy c, const LinearLoss p, RowOf* rows, uint32_t* largest) {
   if (largest && blockIdx.x == 0 && threadIdx.x == 0) *largest = 0;
+  for (uint32_t i = blockIdx.x * 256u + threadIdx.x; i < p.rows; i += gridDim.x * 256u) {
+    bool bad;
+    const int t = target_of(p.targets, p.wide_targets, i, p.ignore, p.classes, &bad);
+    if (bad && p.status) atomicOr(p.status, LMT_STATUS_BAD_TARGET);
+    rows[i] = {0.f, 0.f, t < 0 ? 0.f : p.weights ? load1(p.weights + i) : 1.f, t};
+  }
   const uint32_t pieces = (uint32_t)(round_up(p.width, 64) / 8);
   for (int n = 0; n < 3; ++n) {
     const Copy& m = n == 0 ? a : n == 1 ? b : c;
@@ -85,11 +91,13 @@ struct Product {
   uint32_t a_row, b_row;  // bytes from row to row
   uint32_t m, n, k, blocks;  // k: rows of b where it lies the other way; a has whole blocks, zeros behind k
   Tiles t;
+  uint32_t wrap;    // where a is twice as long, its rounding errors behind it: blocks of either part; b begins again there
+  uint64_t a_more;  // bytes from one part of a to the other
   // what becomes of it
   const RowOf* rows;
   float2* sums;      // kStats: [tile of n][m]: maximum and sum of exp(x - maximum)
   float* hit;        // kStats: logit of the row's target
-  void *g, *gw;      // kGrad: [rows in whole blocks][g_ld], columns up to `cols`: as it is, and times the row's weight
+  void *gw, *left, *g;  // kGrad: [rows in whole blocks][g_ld], columns up to `cols`: times the row's weight; what rounding that leaves, or as it is; or nullptr
   uint64_t g_ld;
   uint32_t first_class, cols, classes;
   const uint32_t* largest;  // kGrad: bits of the largest weight
@@ -102,6 +110,8 @@ enum Mode { kStats, kGrad, kSum };
 
 // bf16 has fp32's range: g has its row's weight in it, for both gradients.  In fp16 small weights would lose bits, so that there are two: without weights, times
 // 2^14 (it is at most 1), for grad_x, whose rows get theirs at the end, and with them, times a power of two that brings the largest to 2^14, for grad_table.
+// With few rows the rounding of g's few large elements is not averaged away, and the products are small: what it leaves is kept and multiplied too, in
+// which fp16 has bits enough.
 template <typename T>
 constexpr bool kNarrow = false;
 template <>
@@ -189,15 +199,16 @@ __global__ __launch_bounds__(S::threads, 2) void k_linear(const Product p) {
     }
   }
   const auto fetch = [&](uint32_t block, uint32_t at) {
-    const uint8_t *a = a0 + (TURN_A ? (uint64_t)block * 64u * p.a_row : block * 128ull), *b = b0 + (TURN_B ? (uint64_t)block * 64u * p.b_row : block * 128ull);
-    const bool end_b = TURN_B && block * 64u + 64u > p.k;  // b's rows of k behind the last one are the last one again, a has zeros there
+    const uint32_t again = block >= p.wrap ? p.wrap : 0u, of_b = block - again;
+    const uint8_t *a = a0 + (again ? p.a_more : 0ull) + (uint64_t)of_b * (TURN_A ? 64ull * p.a_row : 128ull), *b = b0 + (uint64_t)of_b * (TURN_B ? 64ull * p.b_row : 128ull);
+    const bool end_b = TURN_B && of_b * 64u + 64u > p.k;  // b's rows of k behind the last one are the last one again, a has zeros there
 #pragma unroll
     for (int j = 0; j < S::loads; ++j) {
       const bool of_a = j < kLoadsA;
       uint32_t offset = from[j];
       if (!of_a && end_b) {
         const uint32_t k = (((j - kLoadsA) * S::waves + wave) * 64u + lane) / TurnedB::pieces;
-        offset -= (k - min(k, p.k - 1u - block * 64u)) * p.b_row;
+        offset -= (k - min(k, p.k - 1u - of_b * 64u)) * p.b_row;
       }
       send_to_lds(of_a ? a : b, offset, 0, stage + at + (j * S::waves + wave) * 1024u);
     }
@@ -315,9 +326,10 @@ __global__ __launch_bounds__(S::threads, 2) void k_linear(const Product p) {
   if constexpr (MODE == kGrad) {
     // 64 rows of 64 classes at a time through the wavefront's part of LDS, in 16 bits, so that they leave by whole lines; 16-byte pieces of a row change
     // places by its number
-    uint8_t *plain = stage + wave * 16384u, *weighted = plain + 8192u;
+    uint8_t *weighted = stage + wave * 16384u, *other = weighted + 8192u;
     const float columns = column_scale<T>(load1(p.largest));
     const auto turn = [](uint32_t r) { return r >> 1 & 7u; };
+    const auto left = [](uint32_t w, float a, float b) { return pack2(T{}, a - to_f32(__builtin_bit_cast(T, (uint16_t)w)), b - to_f32(__builtin_bit_cast(T, (uint16_t)(w >> 16)))); };
     const uint32_t c0 = n0 + wn * 64u, half = lane >> 5;
     const bool all_classes = p.first_class + c0 + 64u <= p.classes;
 #pragma unroll
@@ -342,19 +354,21 @@ __global__ __launch_bounds__(S::threads, 2) void k_linear(const Product p) {
               if (!all_classes) f[e] = p.first_class + c0 + 4u * half + 32u * j + 8u * g + e < p.classes ? f[e] : 0.f;
             }
             const uint32_t at = r * 128u + ((j * 4u + g) ^ turn(r)) * 16u + half * 8u;
-            if (p.g) *reinterpret_cast<u32x2*>(plain + at) = none ? u32x2{0, 0} : u32x2{pack2(T{}, f[0] * kRowScale<T>, f[1] * kRowScale<T>), pack2(T{}, f[2] * kRowScale<T>, f[3] * kRowScale<T>)};
-            if (p.gw) *reinterpret_cast<u32x2*>(weighted + at) = none ? u32x2{0, 0} : u32x2{pack2(T{}, f[0] * by, f[1] * by), pack2(T{}, f[2] * by, f[3] * by)};
+            const u32x2 v = none ? u32x2{0, 0} : u32x2{pack2(T{}, f[0] * by, f[1] * by), pack2(T{}, f[2] * by, f[3] * by)};
+            *reinterpret_cast<u32x2*>(weighted + at) = v;
+            if (p.left) *reinterpret_cast<u32x2*>(other + at) = none ? u32x2{0, 0} : u32x2{left(v.x, f[0] * by, f[1] * by), left(v.y, f[2] * by, f[3] * by)};
+            else if (p.g) *reinterpret_cast<u32x2*>(other + at) = none ? u32x2{0, 0} : u32x2{pack2(T{}, f[0] * kRowScale<T>, f[1] * kRowScale<T>), pack2(T{}, f[2] * kRowScale<T>, f[3] * kRowScale<T>)};
           }
       }
       __builtin_amdgcn_wave_barrier();
 #pragma unroll
       for (int which = 0; which < 2; ++which) {
-        T* to = static_cast<T*>(which ? p.gw : p.g);
+        T* to = static_cast<T*>(which == 0 ? p.gw : p.left ? p.left : p.g);
         if (!to) continue;
 #pragma unroll
         for (uint32_t it = 0; it < 8; ++it) {
           const uint32_t r = it * 8u + lane / 8u, piece = lane & 7u, i = m0 + r0 + r, j = c0 + piece * 8u;
-          const u32x4 v = *reinterpret_cast<const u32x4*>((which ? weighted : plain) + r * 128u + (piece ^ turn(r)) * 16u);
+          const u32x4 v = *reinterpret_cast<const u32x4*>((which == 0 ? weighted : other) + r * 128u + (piece ^ turn(r)) * 16u);
           if (i < round_up(p.m, 64) && j < p.cols) *(LMT_GLOBAL u32x4*)(to + (uint64_t)i * p.g_ld + j) = v;
         }
       }
@@ -432,16 +446,7 @@ __global__ __launch_bounds__(256) void k_linear_join(const Product p, uint32_t p
 
 // ---- rows ---------------------------------------------------------------------------------------
 
-// In front of the first pass: what a row's target and weight are.
-__global__ __launch_bounds__(256) void k_linear_targets(const LinearLoss p, RowOf* rows) {
-  const uint32_t i = blockIdx.x * 256u + threadIdx.x;
-  if (i >= p.rows) return;
-  bool bad;
-  const int t = target_of(p.targets, p.wide_targets, i, p.ignore, p.classes, &bad);
-  if (bad && p.status) atomicOr(p.status, LMT_STATUS_BAD_TARGET);
-  rows[i] = {0.f, 0.f, t < 0 ? 0.f : p.weights ? load1(p.weights + i) : 1.f, t};
-}
-// Behind it: the tiles' maxima and sums joined, the loss.  16 threads a row, each an equal part of the tiles, then two by two.
+// Behind the first pass: the tiles' maxima and sums joined, the loss.  16 threads a row, each an equal part of the tiles, then two by two.
 __device__ __forceinline__ float2 joined(float2 a, float2 b) {
   const float top = fmaxf(a.x, b.x);
   return {top, (a.y == 0.f ? 0.f : a.y * __builtin_amdgcn_exp2f((a.x - top) * kLog2e)) + (b.y == 0.f ? 0.f : b.y * __builtin_amdgcn_exp2f((b.x - top) * kLog2e))};
@@ -478,7 +483,7 @@ struct Choice {
   Tiles t;
 };
 // What a form takes, in thirds of a microsecond: a round of large tiles, one a compute unit, 5 a block of k, one of medium ones, two a unit, 3; parts of k
-// where `split`, each written and read once in fp32 at 5 TB/s.
+// where `split`, each written and read once in fp32 at 5 TB/s.  (Four stages instead of two for few medium tiles: 76 x 2 003 x 257 10.4 us and 11.9.)
 Choice choose(uint64_t m, uint64_t n, uint64_t blocks, bool split) {
   Choice best = {};
   double least = 0;
@@ -497,10 +502,12 @@ Choice choose(uint64_t m, uint64_t n, uint64_t blocks, bool split) {
 // Where things lie in the workspace, in bytes.
 struct Plan {
   uint64_t piece, pieces;             // classes of a piece, a multiple of 256
+  uint64_t parts;                     // of g: 2 with what rounding leaves
   uint64_t x_row;                     // elements of padded rows of x and the table
   Choice stats, grad_x, grad_t;
   uint64_t rows, sums, hit, largest, x, table, counted, g, gw, part_x, part_t, end;
 };
+constexpr uint64_t kFewRows = 256;  // up to which what rounding g leaves is multiplied too
 constexpr uint64_t kPiece = 1ull << 27;  // elements of g at a time: 256 MB
 Plan plan_of(uint64_t n, uint64_t classes, uint64_t width, bool gradients, bool narrow) {
   Plan w = {};
@@ -509,8 +516,9 @@ Plan plan_of(uint64_t n, uint64_t classes, uint64_t width, bool gradients, bool 
   w.piece = std::min(round_up(ceil_div(classes, w.pieces), 256), round_up(classes, 256));
   w.pieces = ceil_div(classes, w.piece);
   w.stats = choose(n, classes, w.x_row / 64, false);
-  w.grad_x = choose(n, width, w.piece / 64, true);
-  w.grad_t = choose(w.piece, width, ceil_div(n, 64), true);
+  w.parts = n <= kFewRows ? 2 : 1;
+  w.grad_x = choose(n, width, w.parts * w.piece / 64, true);
+  w.grad_t = choose(w.piece, width, w.parts * ceil_div(n, 64), true);
   const auto take = [&](uint64_t bytes) {
     const uint64_t at = w.end;
     w.end += round_up(bytes, 256);
@@ -520,7 +528,7 @@ Plan plan_of(uint64_t n, uint64_t classes, uint64_t width, bool gradients, bool 
   w.x = take(n * w.x_row * 2), w.table = take(classes * w.x_row * 2);
   if (gradients) {
     w.counted = take(n * w.x_row * 2);
-    w.g = take(round_up(n, 64) * w.piece * 2), w.gw = narrow ? take(round_up(n, 64) * w.piece * 2) : w.g;
+    w.gw = take(round_up(n, 64) * w.piece * 2), w.g = w.parts > 1 || narrow ? take(round_up(n, 64) * w.piece * 2) : 0;
     if (w.pieces * w.grad_x.t.splits > 1) w.part_x = take(w.pieces * w.grad_x.t.splits * n * width * 4);
     if (w.grad_t.t.splits > 1) w.part_t = take(w.grad_t.t.splits * w.piece * width * 4);
   }
@@ -528,9 +536,10 @@ Plan plan_of(uint64_t n, uint64_t classes, uint64_t width, bool gradients, bool 
 }
 
 template <typename T, Mode MODE, typename TC, bool TURN_A, bool TURN_B>
-void launch(const Product& p, bool large, hipStream_t s) {
+void launch(Product p, Choice c, hipStream_t s) {
+  if (p.wrap == 0) p.wrap = ~0u;
   const uint32_t grid = p.t.across * p.t.down * p.t.splits;
-  if (large) hipLaunchKernelGGL((k_linear<Large, T, MODE, TC, TURN_A, TURN_B>), dim3(grid), dim3(Large::threads), 0, s, p);
+  if (c.large) hipLaunchKernelGGL((k_linear<Large, T, MODE, TC, TURN_A, TURN_B>), dim3(grid), dim3(Large::threads), 0, s, p);
   else hipLaunchKernelGGL((k_linear<Medium, T, MODE, TC, TURN_A, TURN_B>), dim3(grid), dim3(Medium::threads), 0, s, p);
 }
 template <typename T, typename TC>
@@ -550,35 +559,34 @@ hipError_t launch_typed(const LinearLoss& q, hipStream_t s) {
   const bool x_copy = !as_it_is(q.x, q.x_ld), table_copy = !as_it_is(q.table, q.table_ld);
   const Copy x{q.x, q.x_ld, q.rows, q.width, false, x_copy ? at(w.x) : nullptr}, table{q.table, q.table_ld, q.classes, q.width, false, table_copy ? at(w.table) : nullptr};
   const Copy counted{q.x, q.x_ld, q.rows, q.width, true, q.grad_table ? at(w.counted) : nullptr};
-  hipLaunchKernelGGL(k_linear_targets, dim3((uint32_t)ceil_div(q.rows, 256)), dim3(256), 0, s, q, rows);
-  if (x_copy || table_copy || gradients) {
-    const uint64_t most = std::max<uint64_t>((uint64_t)q.rows * w.x_row, table_copy ? (uint64_t)q.classes * w.x_row : 0);
-    hipLaunchKernelGGL((k_linear_copy<T>), dim3((uint32_t)std::min<uint64_t>(ceil_div(most, 2048), 1u << 16)), dim3(256), 0, s, x, table, counted, q, largest);
-  }
+  const uint64_t most = std::max<uint64_t>({x_copy || q.grad_table ? (uint64_t)q.rows * w.x_row : 0, table_copy ? (uint64_t)q.classes * w.x_row : 0, 8ull * q.rows});
+  hipLaunchKernelGGL((k_linear_begin<T>), dim3((uint32_t)std::min<uint64_t>(ceil_div(most, 2048), 1u << 16)), dim3(256), 0, s, x, table, counted, q, rows, largest);
   Product p = {};
   p.a = x_copy ? at(w.x) : static_cast<const uint8_t*>(q.x), p.a_row = (uint32_t)(2 * (x_copy ? w.x_row : q.x_ld));
   p.b = table_copy ? at(w.table) : static_cast<const uint8_t*>(q.table), p.b_row = (uint32_t)(2 * (table_copy ? w.x_row : q.table_ld));
   p.m = q.rows, p.n = q.classes, p.blocks = (uint32_t)(w.x_row / 64), p.t = w.stats.t, p.rows = rows;
   p.sums = reinterpret_cast<float2*>(at(w.sums)), p.hit = reinterpret_cast<float*>(at(w.hit));
   p.classes = q.classes, p.largest = largest;
-  launch<T, kStats, float, false, false>(p, w.stats.large, s);
+  launch<T, kStats, float, false, false>(p, w.stats, s);
   hipLaunchKernelGGL(k_linear_rows, dim3((uint32_t)ceil_div(q.rows, 16)), dim3(256), 0, s, q, rows, p.sums, p.hit, w.stats.t.across, largest);
   for (uint64_t piece = 0; gradients && piece < w.pieces; ++piece) {
     const uint32_t first = (uint32_t)(piece * w.piece), n = (uint32_t)std::min<uint64_t>(w.piece, q.classes - first);
     Product g = p;
     g.b = p.b + (uint64_t)first * p.b_row, g.n = n, g.first_class = first, g.cols = (uint32_t)round_up(n, 64), g.g_ld = w.piece;
+    const uint64_t part = w.g - w.gw;  // bytes
     const Choice c = choose(q.rows, n, p.blocks, false);
-    g.t = c.t, g.g = kNarrow<T> && q.grad_x ? at(w.g) : nullptr, g.gw = kNarrow<T> && !q.grad_table ? nullptr : at(w.gw);
-    launch<T, kGrad, T, false, false>(g, c.large, s);
+    const bool unweighted = kNarrow<T> && w.parts == 1;  // grad_x from g without weights
+    g.t = c.t, g.gw = unweighted && !q.grad_table ? nullptr : at(w.gw), g.left = w.parts > 1 ? at(w.g) : nullptr, g.g = unweighted && q.grad_x ? at(w.g) : nullptr;
+    launch<T, kGrad, T, false, false>(g, c, s);
     if (q.grad_x) {  // g by the table's rows
       Product d = {};
-      d.a = at(w.g), d.a_row = (uint32_t)(2 * w.piece), d.b = g.b, d.b_row = p.b_row;
-      d.m = q.rows, d.n = q.width, d.k = n, d.blocks = g.cols / 64, d.t = w.grad_x.t, d.rows = rows, d.by_row = kNarrow<T>;
+      d.a = at(unweighted ? w.g : w.gw), d.a_row = (uint32_t)(2 * w.piece), d.b = g.b, d.b_row = p.b_row;
+      d.m = q.rows, d.n = q.width, d.k = n, d.blocks = (uint32_t)w.parts * g.cols / 64, d.wrap = g.cols / 64, d.a_more = part, d.t = w.grad_x.t, d.rows = rows, d.by_row = unweighted, d.largest = unweighted ? nullptr : largest;
       d.c = q.grad_x, d.ldc = q.grad_x_ld;
       const uint32_t parts = (uint32_t)w.pieces * d.t.splits;
       float* sums = reinterpret_cast<float*>(at(w.part_x));
       if (parts > 1) d.part = sums + piece * d.t.splits * (uint64_t)q.rows * q.width;
-      launch<T, kSum, T, false, true>(d, w.grad_x.large, s);
+      launch<T, kSum, T, false, true>(d, w.grad_x, s);
       d.part = sums;
       if (parts > 1 && piece + 1 == w.pieces) join<T, T>(d, parts, s);
     }
@@ -587,11 +595,11 @@ hipError_t launch_typed(const LinearLoss& q, hipStream_t s) {
         typedef decltype(tc) TC;
         Product d = {};
         d.a = at(w.gw), d.a_row = (uint32_t)(2 * w.piece), d.b = at(w.counted), d.b_row = (uint32_t)(2 * w.x_row);
-        d.m = n, d.n = q.width, d.k = q.rows, d.blocks = (uint32_t)ceil_div(q.rows, 64), d.largest = largest, d.accumulate = q.accumulate;
+        d.m = n, d.n = q.width, d.k = q.rows, d.wrap = (uint32_t)ceil_div(q.rows, 64), d.blocks = (uint32_t)w.parts * d.wrap, d.a_more = part, d.largest = largest, d.accumulate = q.accumulate;
         d.t = w.grad_t.t, d.t.down = (uint32_t)ceil_div(n, w.grad_t.large ? Large::rows_m : Medium::rows_m);
         d.c = static_cast<TC*>(q.grad_table) + (uint64_t)first * q.grad_table_ld, d.ldc = q.grad_table_ld;
         if (d.t.splits > 1) d.part = reinterpret_cast<float*>(at(w.part_t));
-        launch<T, kSum, TC, true, true>(d, w.grad_t.large, s);
+        launch<T, kSum, TC, true, true>(d, w.grad_t, s);
         if (d.t.splits > 1) join<T, TC>(d, d.t.splits, s);
       };
       if (q.grad_table_f32) typed(float{});

@@ -270,7 +270,7 @@ for size in (1, 64, 65, 128):
 assert names(lambda: attend(0, 4, 4, 64)) == names(lambda: attend(0, 4, 4, 64, True)) == names(lambda: loss(0, 9, 9, gt=None)) == []
 assert names(lambda: loss(100, 500, 64, None, None))[-2:] == ["k_linear", "k_linear_rows"]
 both = names(lambda: loss(8192, 30522, 1024))
-assert both.count("k_linear") == 1 + 3 * 2 and "k_linear_copy" in both, both        # two pieces of the classes, three products each
+assert both.count("k_linear") == 1 + 3 * 2 and both[0] == "k_linear_begin", both        # two pieces of the classes, three products each
 assert names(lambda: loss(100, 500, 64, gt=None)).count("k_linear") == 3 and names(lambda: loss(100, 500, 64, gx=None)).count("k_linear") == 3
 assert fake.fake_device_allocations() == before
 """)
