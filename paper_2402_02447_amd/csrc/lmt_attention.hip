@@ -223,27 +223,30 @@ struct Stage {
   static constexpr int pieces = D / 8, loads = kTile * pieces / THREADS, step = THREADS / pieces;
   static_assert(step % 16 == 0, "rows that a thread loads turn their pieces alike");
   u32x4 w[DIRECT ? 1 : loads];
-  uint32_t at;  // DIRECT: of this thread's first piece, in bytes behind the tile's first row
-  __device__ __forceinline__ void set(const Heads& x, uint32_t size) {
-    if constexpr (DIRECT) at = threadIdx.x / pieces * (uint32_t)x.row * 2u + piece_at(threadIdx.x % pieces ^ turn<D>(threadIdx.x / pieces), size) * 2u;
+  uint32_t at, row;     // DIRECT: this thread's first piece, in bytes behind the tile's first row, and from row to row
+  const uint8_t* base;  // the next tile's first row, and how many are behind it
+  uint32_t behind;
+  // Tiles from row `first` on, one behind the other.
+  __device__ __forceinline__ void set(const T* head, const Heads& x, uint32_t first, uint32_t rows, uint32_t size) {
+    row = (uint32_t)x.row * 2u, base = reinterpret_cast<const uint8_t*>(row_of(head, x, first)), behind = rows - 1u - first;
+    if constexpr (DIRECT) at = threadIdx.x / pieces * row + piece_at(threadIdx.x % pieces ^ turn<D>(threadIdx.x / pieces), size) * 2u;
   }
-  __device__ __forceinline__ void fetch(const T* head, const Heads& x, uint32_t first, uint32_t rows, uint32_t size, uint8_t* tile) {
-    const uint32_t r = threadIdx.x / pieces, slot = threadIdx.x % pieces;
+  __device__ __forceinline__ void fetch(uint8_t* tile, uint32_t size) {
+    const uint32_t r = threadIdx.x / pieces;
     if constexpr (DIRECT) {
-      const uint32_t row = (uint32_t)x.row * 2u, last = rows - 1u - first;
       uint8_t* to = tile + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * 1024u;
-      const uint8_t* base = reinterpret_cast<const uint8_t*>(row_of(head, x, first));
-      if (last >= kTile - 1u) {
+      if (behind >= kTile - 1u) {
 #pragma unroll
         for (uint32_t j = 0; j < loads; ++j) send_to_lds(base, at, j * step * row, to + j * THREADS * 16u);
       } else {
 #pragma unroll
-        for (uint32_t j = 0; j < loads; ++j) send_to_lds(base, at - r * row + min(r + j * step, last) * row, 0, to + j * THREADS * 16u);
+        for (uint32_t j = 0; j < loads; ++j) send_to_lds(base, at - r * row + min(r + j * step, behind) * row, 0, to + j * THREADS * 16u);
       }
     } else {
 #pragma unroll
-      for (int j = 0; j < loads; ++j) w[j] = load_piece(row_of(head, x, min(first + r + j * step, rows - 1u)), slot, size);
+      for (int j = 0; j < loads; ++j) w[j] = load_piece(reinterpret_cast<const T*>(base + (uint64_t)min(r + j * step, behind) * row), threadIdx.x % pieces, size);
     }
+    base += (uint64_t)row * kTile, behind -= kTile;  // behind the last tile: of no concern
   }
   __device__ __forceinline__ void put(uint8_t* tile) const {
     if constexpr (!DIRECT) {
@@ -465,6 +468,19 @@ __device__ __forceinline__ void place(uint32_t tiles, uint32_t lists, Order long
   if (longest == kLast) *tile = tiles - 1u - *tile;
 }
 
+// Scores that the column's row does not see, its first element `from` places into what it sees: none.  Their weights are 0, and so are
+// weights times what is finite; what is not shows in the sums.
+__device__ __forceinline__ void hide(f32x16& s, uint32_t from, uint32_t n) {
+#pragma unroll
+  for (int e = 0; e < 16; ++e) s[e] = from + (uint32_t)(8 * (e / 4) + e % 4) < n ? s[e] : -kInf;
+}
+__device__ __forceinline__ float largest(const f32x16 (&s)[2]) {
+  float top[2] = {s[0][0], s[1][0]};
+#pragma unroll
+  for (int e = 1; e < 16; ++e) top[0] = fmaxf(top[0], s[0][e]), top[1] = fmaxf(top[1], s[1][e]);
+  return fmaxf(top[0], top[1]);
+}
+
 // ---- forward ------------------------------------------------------------------------------------
 
 // One row, a wavefront: only of what the row sees, so that infinities and NaN elsewhere stay there.
@@ -519,45 +535,27 @@ __global__ __launch_bounds__(kThreads, D == 64 && DIRECT ? 3 : 2) void k_attend(
   Along<D> along;
   Across<D> across;
   along.set(), across.set();
-  float m = -kInf, sum[4] = {};
-  f32x16 o[D / 32] = {}, s[2] = {};
+  float m = -kInf, top = -kInf, sum[4] = {};
+  f32x16 o[D / 32] = {}, s[2];
   Stage<T, D, kThreads, DIRECT> next_k, next_v;
-  next_k.set(p.k, p.size), next_v.set(p.v, p.size);
-  if (first < last) {
-    next_k.fetch(k, p.k, (uint32_t)first, p.rows, p.size, keys[0]), next_v.fetch(v, p.v, (uint32_t)first, p.rows, p.size, values[0]);
-    next_k.put(keys[0]), next_v.put(values[0]);
-    arrived();
-    const bool more = first + kTile < last;
-    if (more) next_k.fetch(k, p.k, (uint32_t)(first + kTile), p.rows, p.size, keys[1]);
-#pragma unroll
-    for (int c = 0; c < D / 16; ++c)
-#pragma unroll
-      for (int b = 0; b < 2; ++b) s[b] = mma(T{}, along.read(keys[0], b, c), q.w[c], s[b]);
-    if (more) next_k.put(keys[1]);
-    arrived();
-  }
-  uint32_t now = 0;
-  for (int at = first; at < last; at += kTile, now ^= 1u) {
+  // The scores of tile `at`, in buffer `now`, become weights, and those of the tile behind it are made.
+  const auto pass = [&](int at, uint32_t now) {
     const bool more = at + kTile < last, more_keys = at + 2 * kTile < last;
-    if (more_keys) next_k.fetch(k, p.k, (uint32_t)(at + 2 * kTile), p.rows, p.size, keys[now]);
-    if (more) next_v.fetch(v, p.v, (uint32_t)(at + kTile), p.rows, p.size, values[now ^ 1u]);
+    if (more_keys) next_k.fetch(keys[now], p.size);
+    if (more) next_v.fetch(values[now ^ 1u], p.size);
     if (span.touches(at, kTile)) {
       const int j0 = at + 4 * (int)(lane >> 5);
+      const bool inside = span.inside(at, kTile);
       if constexpr (!PLAIN) score.of<2, false>(s, (float)(j0 - (int)i), s);
-      if (!span.inside(at, kTile)) {
+      if (!inside) {
         const uint32_t from = (uint32_t)(j0 - span.lo), n = (uint32_t)(span.hi - span.lo);
-#pragma unroll
-        for (int b = 0; b < 2; ++b)
-#pragma unroll
-          for (int e = 0; e < 16; ++e) s[b][e] = from + (uint32_t)(32 * b + 8 * (e / 4) + e % 4) < n ? s[b][e] : -kInf;
+        hide(s[0], from, n), hide(s[1], from + 32u, n);
       }
-      float top = s[0][0];
-#pragma unroll
-      for (int e = 1; e < 32; ++e) top = fmaxf(top, s[e / 16][e % 16]);
-      top = halves_max(top);
-      if constexpr (PLAIN) top *= score.by;
-      if (any(top > m + kSlack)) {
-        const float up = fmaxf(m, top), by = m == -kInf ? 0.f : exp2_of(m - up);
+      if (!PLAIN || !inside) top = largest(s);
+      float most = halves_max(top);
+      if constexpr (PLAIN) most *= score.by;
+      if (any(most > m + kSlack)) {
+        const float up = fmaxf(m, most), by = m == -kInf ? 0.f : exp2_of(m - up);
         m = up;
 #pragma unroll
         for (int e = 0; e < 4; ++e) sum[e] *= by;
@@ -567,7 +565,6 @@ __global__ __launch_bounds__(kThreads, D == 64 && DIRECT ? 3 : 2) void k_attend(
           for (int e = 0; e < 16; ++e) o[d][e] *= by;
       }
       const float base = (m == -kInf ? 0.f : m) - kShift<T>;
-      f32x16 next[2] = {};
       u32x4 w[2][2], ahead[kAhead];
       constexpr int kSteps = 2 * (D / 16), kEach = 32 / kSteps;  // instructions of either kind; elements between two
       // operand t: of the next scores, then of this tile's values
@@ -576,6 +573,8 @@ __global__ __launch_bounds__(kThreads, D == 64 && DIRECT ? 3 : 2) void k_attend(
         const int u = t - kSteps, of = u / (D / 32);
         return across.read(values[now], of / 2, of % 2, u % (D / 32));
       };
+      f32x16 next[2] = {};
+      float tops[2];
 #pragma unroll
       for (int t = 0; t < kAhead - 1; ++t) ahead[t] = operand(t);
       each<2 * kSteps>([&](auto number) {
@@ -592,30 +591,56 @@ __global__ __launch_bounds__(kThreads, D == 64 && DIRECT ? 3 : 2) void k_attend(
         } else {
           constexpr int u = t - kSteps, of = u / (D / 32), d = u % (D / 32);
           o[d] = mma(T{}, ahead[t % kAhead], w[of / 2][of % 2], o[d]);
+          if constexpr (u >= kSteps / 2) {  // the next scores, which are there by now, move, and the largest is found
+            constexpr int b = (u - kSteps / 2) * 64 / kSteps / 16, n = 64 / kSteps, e0 = (u - kSteps / 2) * n % 16;
+#pragma unroll
+            for (int e = e0; e < e0 + n; ++e) {
+              float x = next[b][e];
+              asm volatile("" : "+v"(x));  // here, and not behind the last product
+              s[b][e] = x, tops[b] = e == 0 ? x : fmaxf(tops[b], x);
+            }
+          }
         }
         __builtin_amdgcn_sched_barrier(0);
       });
-#pragma unroll
-      for (int b = 0; b < 2; ++b) s[b] = next[b];
+      if constexpr (PLAIN) top = fmaxf(tops[0], tops[1]);
     } else if (more && span.touches(at + kTile, kTile)) {
-#pragma unroll
-      for (int b = 0; b < 2; ++b) s[b] = f32x16{};
+      s[0] = s[1] = f32x16{};
 #pragma unroll
       for (int c = 0; c < D / 16; ++c)
 #pragma unroll
         for (int b = 0; b < 2; ++b) s[b] = mma(T{}, along.read(keys[now ^ 1u], b, c), q.w[c], s[b]);
+      if constexpr (PLAIN) top = largest(s);
     }
     if (more_keys) next_k.put(keys[now]);
     if (more) next_v.put(values[now ^ 1u]);
     arrived();
+  };
+  if (first < last) {
+    next_k.set(k, p.k, (uint32_t)first, p.rows, p.size), next_v.set(v, p.v, (uint32_t)first, p.rows, p.size);
+    next_k.fetch(keys[0], p.size), next_v.fetch(values[0], p.size);
+    next_k.put(keys[0]), next_v.put(values[0]);
+    arrived();
+    const bool more = first + kTile < last;
+    if (more) next_k.fetch(keys[1], p.size);
+    s[0] = s[1] = f32x16{};
+#pragma unroll
+    for (int c = 0; c < D / 16; ++c)
+#pragma unroll
+      for (int b = 0; b < 2; ++b) s[b] = mma(T{}, along.read(keys[0], b, c), q.w[c], s[b]);
+    if constexpr (PLAIN) top = largest(s);
+    if (more) next_k.put(keys[1]);
+    arrived();
+    uint32_t now = 0;
+    for (int at = first; at < last; at += kTile, now ^= 1u) pass(at, now);
   }
   float l = (sum[0] + sum[1]) + (sum[2] + sum[3]);
   l = halves_sum(l);
-  const bool some = span.lo < span.hi, here = i < p.rows;
+  const bool some = span.lo < span.hi;
   const bool again = some && !(finite<D>(o) && finite(l));
   const uint64_t rows_again = __builtin_amdgcn_ballot_w64(again);
   const uint32_t redo = (uint32_t)rows_again | (uint32_t)(rows_again >> 32);
-  const bool mine = here && !(redo >> (lane & 31u) & 1u);
+  const bool mine = i < p.rows && !(redo >> (lane & 31u) & 1u);
   if (!some || l == 0.f) {
 #pragma unroll
     for (int d = 0; d < D / 32; ++d) o[d] = f32x16{};
@@ -692,12 +717,6 @@ __device__ __forceinline__ void grad_q_row(const Attention& p, uint32_t head, ui
     if (lane + 64u * e < p.size) store1(to + lane + 64u * e, from_f32<T>(sum[e] * p.scale));
 }
 
-// Scores that the column's row does not see, its first element `from` places into what it sees: none.  Their weights are 0, and so are
-// weights times what is finite; what is not shows in the sums.
-__device__ __forceinline__ void hide(f32x16& s, uint32_t from, uint32_t n) {
-#pragma unroll
-  for (int e = 0; e < 16; ++e) s[e] = from + (uint32_t)(8 * (e / 4) + e % 4) < n ? s[e] : -kInf;
-}
 // lse in units of log 2, as what is subtracted from scores: a row without weights has none.
 __device__ __forceinline__ float subtracted(float lse) { return lse == -kInf ? kInf : lse * kLog2e; }
 
@@ -742,16 +761,16 @@ __global__ __launch_bounds__(kThreads, 2) void k_attend_grad_q(const Attention p
   range.begin();
   f32x16 sum[D / 32] = {};
   Stage<T, D, kThreads, DIRECT> next_k, next_v;
-  next_k.set(p.k, p.size), next_v.set(p.v, p.size);
   if (first < last) {
-    next_k.fetch(k, p.k, (uint32_t)first, p.rows, p.size, keys[0]), next_v.fetch(v, p.v, (uint32_t)first, p.rows, p.size, values[0]);
+    next_k.set(k, p.k, (uint32_t)first, p.rows, p.size), next_v.set(v, p.v, (uint32_t)first, p.rows, p.size);
+    next_k.fetch(keys[0], p.size), next_v.fetch(values[0], p.size);
     next_k.put(keys[0]), next_v.put(values[0]);
   }
   arrived();
   uint32_t now = 0;
   for (int at = first; at < last; at += kTile, now ^= 1u) {
     const bool more = at + kTile < last;
-    if (more) next_k.fetch(k, p.k, (uint32_t)(at + kTile), p.rows, p.size, keys[now ^ 1u]), next_v.fetch(v, p.v, (uint32_t)(at + kTile), p.rows, p.size, values[now ^ 1u]);
+    if (more) next_k.fetch(keys[now ^ 1u], p.size), next_v.fetch(values[now ^ 1u], p.size);
     if (span.touches(at, kTile)) {
       {
         constexpr int kHalf = D / 16, kSteps = 6 * kHalf;  // of k; of matrix instructions: scores and products with v of either half, then sums of either
@@ -909,7 +928,8 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 2 : 1) void k_attend_grad_kv(co
   Stage<T, D, kThreads, DIRECT> next_q, next_go;
   float next_lse = 0, next_delta = 0;
   const auto fetch = [&](uint32_t head, int at, uint32_t to) {
-    next_q.fetch(head_of<T>(p.q, head), p.q, (uint32_t)at, p.rows, p.size, queries[to]), next_go.fetch(head_of<T>(p.grad_out, head), p.grad_out, (uint32_t)at, p.rows, p.size, grads[to]);
+    if (at == first) next_q.set(head_of<T>(p.q, head), p.q, (uint32_t)first, p.rows, p.size), next_go.set(head_of<T>(p.grad_out, head), p.grad_out, (uint32_t)first, p.rows, p.size);
+    next_q.fetch(queries[to], p.size), next_go.fetch(grads[to], p.size);
     if (threadIdx.x < kTile) {
       const uint64_t from = (uint64_t)head * p.rows + min((uint32_t)at + threadIdx.x, p.rows - 1u);
       next_lse = load1(p.lse + from), next_delta = load1(p.delta + from);
@@ -919,7 +939,6 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 2 : 1) void k_attend_grad_kv(co
     next_q.put(queries[to]), next_go.put(grads[to]);
     if (threadIdx.x < kTile) lse[to][threadIdx.x] = subtracted(next_lse), delta[to][threadIdx.x] = next_delta;
   };
-  next_q.set(p.q, p.size), next_go.set(p.grad_out, p.size);
   if (first < last) fetch(h0, first, 0), put(0);
   arrived();
   uint32_t now = 0;
