@@ -380,9 +380,9 @@ struct Score {
     const float e = exp2_of(__builtin_fabsf(x) * (2.f * kLog2e)), t = 1.f - 2.f * __builtin_amdgcn_rcpf(e + 1.f);
     return __builtin_fabsf(x) < 0.3f ? series(x) : __builtin_copysignf(t, x);
   }
-  // N elements of a lane's column, from distance `apart` (the column's own row subtracted) on; bend: what the cap multiplies derivatives by.
-  template <int N, bool BEND>
-  __device__ __forceinline__ void of(f32x16 (&s)[N], float apart, f32x16 (&bend)[N]) const {
+  // N elements of a lane's column, from distance `apart` (the column's own row subtracted) on.  GRAD: d is multiplied by what the cap does to derivatives.
+  template <int N, bool GRAD>
+  __device__ __forceinline__ void of(f32x16 (&s)[N], float apart, f32x16 (&d)[N]) const {
     if (cap != 0.f) {
       float top = 0;
 #pragma unroll
@@ -404,17 +404,14 @@ struct Score {
       for (int b = 0; b < N; ++b)
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
-          if constexpr (BEND) bend[b][e] = __builtin_fmaf(-s[b][e], s[b][e], 1.f);
+          if constexpr (GRAD) d[b][e] *= __builtin_fmaf(-s[b][e], s[b][e], 1.f);
           s[b][e] *= cap;
         }
     } else {
 #pragma unroll
       for (int b = 0; b < N; ++b)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          if constexpr (BEND) bend[b][e] = 1.f;
-          s[b][e] *= by;
-        }
+        for (int e = 0; e < 16; ++e) s[b][e] *= by;
     }
     if (slope != 0.f) {
 #pragma unroll
@@ -773,8 +770,8 @@ __global__ __launch_bounds__(kThreads, 2) void k_attend_grad_q(const Attention p
     if (more) next_k.fetch(keys[now ^ 1u], p.size), next_v.fetch(values[now ^ 1u], p.size);
     if (span.touches(at, kTile)) {
       {
-        constexpr int kHalf = D / 16, kSteps = 6 * kHalf;  // of k; of matrix instructions: scores and products with v of either half, then sums of either
-        f32x16 s[2][1] = {}, dp[2] = {}, bend[2][1];
+        constexpr int kHalf = D / 16, kSteps = 6 * kHalf, kAhead = 3;  // of k; of matrix instructions: scores and products with v of either half, then sums of either
+        f32x16 s[2][1] = {}, dp[2][1] = {};
         u32x4 w[2][2], ahead[kAhead];
         const auto operand = [&](int t) {
           if (t < 4 * kHalf) return along.read(t % 2 ? values[now] : keys[now], t / (2 * kHalf), t / 2 % kHalf);
@@ -785,9 +782,13 @@ __global__ __launch_bounds__(kThreads, 2) void k_attend_grad_q(const Attention p
         const bool inside = span.inside(at, kTile);
         const auto element = [&](int b, int e) {
           const float x = exp2_of(PLAIN ? __builtin_fmaf(s[b][0][e], score.by, -lse) : s[b][0][e] - lse);
-          float d = __builtin_fmaf(dp[b][e], range.by, -delta * range.by) * x;
-          if constexpr (!PLAIN) d *= bend[b][0][e];
-          s[b][0][e] = d;
+          s[b][0][e] = (PLAIN ? __builtin_fmaf(dp[b][0][e], range.by, -delta * range.by) : dp[b][0][e]) * x;
+        };
+        const auto general = [&](auto half_of) {  // what is not PLAIN's, for a whole half
+          constexpr int b = decltype(half_of)::value;
+#pragma unroll
+          for (int e = 0; e < 16; ++e) dp[b][0][e] = __builtin_fmaf(dp[b][0][e], range.by, -delta * range.by);
+          score.of<1, true>(s[b], (float)(at + 32 * b + 4 * (int)(lane >> 5) - (int)i), dp[b]);
         };
 #pragma unroll
         for (int t = 0; t < kAhead - 1; ++t) ahead[t] = operand(t);
@@ -796,7 +797,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_attend_grad_q(const Attention p
           if (t + kAhead - 1 < kSteps) ahead[(t + kAhead - 1) % kAhead] = operand(t + kAhead - 1);
           if constexpr (t < 4 * kHalf) {
             constexpr int b = t / (2 * kHalf), c = t / 2 % kHalf;
-            if (t % 2) dp[b] = mma(T{}, ahead[t % kAhead], go.w[c], dp[b]);
+            if (t % 2) dp[b][0] = mma(T{}, ahead[t % kAhead], go.w[c], dp[b][0]);
             else s[b][0] = mma(T{}, ahead[t % kAhead], q.w[c], s[b][0]);
           } else {
             constexpr int u = t - 4 * kHalf, b = u / kHalf, of = u % kHalf, d = of % (D / 32);
@@ -804,8 +805,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_attend_grad_q(const Attention p
           }
           // the first half's elements beside the second half's scores, the second half's beside the first one's sums
           if constexpr (!PLAIN) {
-            if constexpr (t == 2 * kHalf) score.of<1, true>(s[0], (float)(at + 4 * (int)(lane >> 5) - (int)i), bend[0]);
-            if constexpr (t == 4 * kHalf) score.of<1, true>(s[1], (float)(at + 32 + 4 * (int)(lane >> 5) - (int)i), bend[1]);
+            if constexpr (t == 2 * kHalf || t == 4 * kHalf) general(std::integral_constant<int, t / (2 * kHalf) - 1>{});
           }
           if constexpr (t == 2 * kHalf || t == 4 * kHalf) {
             if (!inside) hide(s[t / (2 * kHalf) - 1][0], from + (t == 4 * kHalf ? 32u : 0u), n);
@@ -950,8 +950,8 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 2 : 1) void k_attend_grad_kv(co
       if (more) fetch(wrap ? head + 1u : head, wrap ? first : at + kTile, now ^ 1u);
       if (span.touches(at, kTile)) {
         {
-          constexpr int kHalf = D / 16, kSteps = 8 * kHalf;
-          f32x16 s[2][1] = {}, d[2][1] = {}, bend[2][1];
+          constexpr int kHalf = D / 16, kSteps = 8 * kHalf, kAhead = D == 64 ? 3 : 4;
+          f32x16 s[2][1] = {}, d[2][1] = {};
           u32x4 w[2][2], x[2][2], ahead[kAhead];
           f32x4 less[2], dots[2];  // of four rows, and of the next four
           const int half = 4 * (int)(lane >> 5);
@@ -968,10 +968,19 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 2 : 1) void k_attend_grad_kv(co
           const auto element = [&](int b, int e) {
             const int g = e / 4;
             float p_ = exp2_of(PLAIN ? __builtin_fmaf(s[b][0][e], score.by, -less[g % 2][e % 4]) : s[b][0][e] - less[g % 2][e % 4]);
-            float d_ = __builtin_fmaf(d[b][0][e], range.by, -dots[g % 2][e % 4] * range.by) * p_;
-            if constexpr (!PLAIN) d_ *= bend[b][0][e];
+            const float d_ = (PLAIN ? __builtin_fmaf(d[b][0][e], range.by, -dots[g % 2][e % 4] * range.by) : d[b][0][e]) * p_;
             if constexpr (kShift<T> != 0.f) p_ *= 0x1p14f;  // weights are at most 1
             s[b][0][e] = p_, d[b][0][e] = d_;
+          };
+          const auto general = [&](auto half_of) {  // what is not PLAIN's, for a whole half
+          constexpr int b = decltype(half_of)::value;
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+              const f32x4 x = *reinterpret_cast<const f32x4*>(&delta[now][32 * b + 8 * g + half]);
+#pragma unroll
+              for (int r = 0; r < 4; ++r) d[b][0][4 * g + r] = __builtin_fmaf(d[b][0][4 * g + r], range.by, -x[r] * range.by);
+            }
+            score.of<1, true>(s[b], (float)(at + 32 * b + half - (int)j), d[b]);
           };
 #pragma unroll
           for (int t = 0; t < kAhead - 1; ++t) ahead[t] = operand(t);
@@ -988,8 +997,7 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 2 : 1) void k_attend_grad_kv(co
               else dv[e] = mma(T{}, ahead[t % kAhead], w[b][of / (D / 32)], dv[e]);
             }
             if constexpr (!PLAIN) {
-              if constexpr (t == 2 * kHalf) score.of<1, true>(s[0], (float)(at + half - (int)j), bend[0]);
-              if constexpr (t == 4 * kHalf) score.of<1, true>(s[1], (float)(at + 32 + half - (int)j), bend[1]);
+              if constexpr (t == 2 * kHalf || t == 4 * kHalf) general(std::integral_constant<int, t / (2 * kHalf) - 1>{});
             }
             if constexpr (t == 2 * kHalf || t == 4 * kHalf) {
             if (!inside) hide(s[t / (2 * kHalf) - 1][0], from + (t == 4 * kHalf ? 32u : 0u), n);
