@@ -9,6 +9,12 @@ and output).  One step is
     bucket_clip_adam                               the parameters' update, bucket by bucket
 with nothing but these calls on the stream: every buffer is allocated beforehand.
 
+With heads, the tokens are sequences of unlike lengths, one behind the other, and an attention layer comes before the projection:
+h = x + attention(x Q^T) P^T, Q giving queries, keys and values in one, queries and keys turned by their positions.  The step then has
+    matmul, rotary, attention                      in front of the projection, whose product is added to x
+    attention_grad, rotary, quantize, matmul       behind it, the input's gradient added to that of h
+With logits=False the logits are never kept: h and the table go into linear_cross_entropy in 16 bits, which gives both their gradients.
+
 Run as ``python -m paper_2402_02447_amd.lm_step`` (needs a GPU): prints the loss of some steps on a made-up language."""
 from __future__ import annotations
 
@@ -50,7 +56,8 @@ class _Fp8:
 class TiedLm:
     """The model, its gradients, moments and everything a step works in, for `tokens` positions a step."""
 
-    def __init__(self, vocab: int, width: int, tokens: int, seed: int = 0, clip: float = 1.0, hyper: AdamHyper = AdamHyper(lr=3e-3)):
+    def __init__(self, vocab: int, width: int, tokens: int, seed: int = 0, clip: float = 1.0, hyper: AdamHyper = AdamHyper(lr=3e-3), heads: int = 0, causal: bool = True,
+                 logits: bool = True):
         g = torch.Generator(device="cuda")
         g.manual_seed(seed)
         self.scale, self.hyper, self.step_count = math.sqrt(width), hyper, 0
@@ -61,43 +68,108 @@ class TiedLm:
         def bf16(rows, cols):
             return torch.empty(rows, cols, dtype=torch.bfloat16, device="cuda")
         e4m3, e5m2 = torch.float8_e4m3fn, torch.float8_e5m2
-        self.x, self.h, self.dh, self.dx, self.logits = (bf16(tokens, n) for n in (width, width, width, width, vocab))
-        self.x8, self.h8 = _Fp8(tokens, width, e4m3), _Fp8(tokens, width, e4m3)
-        self.table8, self.proj8 = _Fp8(vocab, width, e4m3, tile=True), _Fp8(width, width, e4m3, tile=True)
-        self.dlogits8, self.dh8 = _Fp8(tokens, vocab, e5m2), _Fp8(tokens, width, e5m2)
+        self.x, self.h, self.dh, self.dx = (bf16(tokens, width) for _ in range(4))
+        self.x8, self.dh8 = _Fp8(tokens, width, e4m3), _Fp8(tokens, width, e5m2)
+        self.proj8 = _Fp8(width, width, e4m3, tile=True)
         self.loss = torch.empty(tokens, device="cuda")
         self.status = torch.zeros(1, dtype=torch.int32, device="cuda")
         need = [lmt.embed_grad_workspace(tokens, vocab, width)]
-        need += [lmt.matmul_workspace(*mnk) for mnk in ((tokens, width, width), (tokens, vocab, width), (tokens, width, vocab), (vocab, width, tokens), (width, width, tokens))]
+        need += [lmt.matmul_workspace(*mnk) for mnk in ((tokens, width, width), (width, width, tokens))]
+        self.keeps_logits = logits
+        if logits:
+            self.logits, self.h8 = bf16(tokens, vocab), _Fp8(tokens, width, e4m3)
+            self.table8, self.dlogits8 = _Fp8(vocab, width, e4m3, tile=True), _Fp8(tokens, vocab, e5m2)
+            need += [lmt.matmul_workspace(*mnk) for mnk in ((tokens, vocab, width), (tokens, width, vocab), (vocab, width, tokens))]
+        else:
+            self.table16, self.every_token = bf16(vocab, width), torch.arange(vocab, device="cuda")
+            need += [lmt.linear_cross_entropy_workspace(tokens, vocab, width)]
+        self.heads, self.causal = heads, causal
+        if heads:
+            if width % (2 * heads):
+                raise ValueError("width is no multiple of twice the heads")
+            size = width // heads
+            self.attend_scale, self.frequencies = 1 / math.sqrt(size), lmt.rotary_frequencies(size // 2).cuda()
+            self.qkv = torch.randn(3 * width, width, generator=g, device="cuda") / math.sqrt(width)
+            self.grad_qkv, self.qkv8 = torch.empty_like(self.qkv), _Fp8(3 * width, width, e4m3, tile=True)
+            self.mix, self.dmix = (bf16(tokens, width) for _ in range(2))
+            self.mix8, self.parts, self.dparts, self.dparts8 = _Fp8(tokens, width, e4m3), bf16(tokens, 3 * width), bf16(tokens, 3 * width), _Fp8(tokens, 3 * width, e5m2)
+            self.lse = torch.empty(heads, tokens, device="cuda")
+            need += [lmt.attention_grad_workspace(tokens, heads, heads, size)]
+            need += [lmt.matmul_workspace(*mnk) for mnk in ((tokens, 3 * width, width), (tokens, width, 3 * width), (3 * width, width, tokens))]
         self.workspace = torch.empty(max(need), dtype=torch.uint8, device="cuda")   # one call after the other on one stream: they share it
 
-        tensors: List[torch.Tensor] = [self.table, self.proj]
+        tensors: List[torch.Tensor] = [self.table, self.proj] + ([self.qkv] if heads else [])
+        grads = [self.grad_table, self.grad_proj] + ([self.grad_qkv] if heads else [])
         layout = whole_tensors([t.numel() for t in tensors], 1)                     # a bucket per tensor, the last one first
         self.moments = [[torch.zeros_like(t).view(-1) for t in tensors] for _ in range(2)]
         self.plan = Plan.from_layout(layout, BCA_GRAD_F32, device=torch.cuda.current_device())
-        self.plan.bind([self.grad_table.view(-1), self.grad_proj.view(-1)], [t.view(-1) for t in tensors], *self.moments)
+        self.plan.bind([t.view(-1) for t in grads], [t.view(-1) for t in tensors], *self.moments)
         self.thresholds = torch.from_numpy(alg1_thresholds(clip, layout.n_buckets)).cuda()
 
-    def gradients(self, tokens, targets, weights, stream=None) -> None:
-        """Loss (per position, weighted) and gradients of a batch.  tokens, targets: [tokens] int32 or int64; weights: [tokens]."""
+    def _heads(self, parts):
+        """Queries, keys and values of a [tokens, 3 * width] matrix, as heads, and the first two in one."""
+        n, x = self.heads, parts.view(parts.shape[0], 3 * self.heads, -1)
+        return x[:, :n], x[:, n:2 * n], x[:, 2 * n:], x[:, :2 * n]
+
+    def _attend(self, tokens, starts, positions, s) -> None:
+        """h = x + attention(x Q^T) P^T."""
+        T = self
+        T.qkv8.take(T.qkv, s)
+        lmt.matmul(*T.x8.rows, *T.qkv8.rows, T.parts, T.workspace, stream=s)
+        q, k, v, turned = T._heads(T.parts)
+        lmt.rotary(turned, positions, T.frequencies, turned, stream=s)
+        lmt.attention(q, k, v, T.mix.view(v.shape), T.lse, starts, scale=T.attend_scale, causal=T.causal, status=T.status, stream=s)
+        T.mix8.take(T.mix, s)
+        lmt.embed(T.table, tokens, T.h, T.scale, T.status, s)
+        lmt.matmul(*T.mix8.rows, *T.proj8.rows, T.h, T.workspace, accumulate=True, stream=s)
+
+    def _attend_grad(self, starts, positions, s) -> None:
+        """Gradients of P, Q and, in dh, of x, from that of h in dh8 and dh."""
+        T = self
+        lmt.matmul(*T.dh8.cols, *T.mix8.cols, T.grad_proj, T.workspace, stream=s)   # dP = dh^T mix
+        lmt.matmul(*T.dh8.rows, *T.proj8.cols, T.dmix, T.workspace, stream=s)       # dmix = dh P
+        q, k, v, _ = T._heads(T.parts)
+        dq, dk, dv, turned = T._heads(T.dparts)
+        lmt.attention_grad(T.dmix.view(v.shape), q, k, v, T.mix.view(v.shape), T.lse, dq, dk, dv, T.workspace, starts, scale=T.attend_scale, causal=T.causal, status=T.status, stream=s)
+        lmt.rotary(turned, positions, T.frequencies, turned, inverse=True, stream=s)
+        T.dparts8.take(T.dparts, s)
+        lmt.matmul(*T.dparts8.cols, *T.x8.cols, T.grad_qkv, T.workspace, stream=s)  # dQ = dparts^T x
+        lmt.matmul(*T.dparts8.rows, *T.qkv8.cols, T.dh, T.workspace, accumulate=True, stream=s)   # dx = dh + dparts Q
+
+    def gradients(self, tokens, targets, weights, stream=None, starts=None, positions=None) -> None:
+        """Loss (per position, weighted) and gradients of a batch.  tokens, targets: [tokens] int32 or int64; weights: [tokens]; with heads also
+        where sequences start (int32, one more than there are) and each token's position in its own."""
         T, s = self, stream
-        T.table8.take(T.table, s), T.proj8.take(T.proj, s)                          # weights as the last update left them
+        T.proj8.take(T.proj, s)                                                     # weights as the last update left them
         lmt.embed(T.table, tokens, T.x, T.scale, T.status, s)
         T.x8.take(T.x, s)
-        lmt.matmul(*T.x8.rows, *T.proj8.rows, T.h, T.workspace, stream=s)           # h = x P^T
-        T.h8.take(T.h, s)
-        lmt.matmul(*T.h8.rows, *T.table8.rows, T.logits, T.workspace, stream=s)     # logits = h table^T
-        lmt.cross_entropy(T.logits, targets, T.loss, None, T.logits, weights, IGNORE, T.status, s)
-        T.dlogits8.take(T.logits, s)
-        lmt.matmul(*T.dlogits8.rows, *T.table8.cols, T.dh, T.workspace, stream=s)   # dh = dlogits table
-        lmt.matmul(*T.dlogits8.cols, *T.h8.cols, T.grad_table, T.workspace, stream=s)   # dtable = dlogits^T h
+        if T.heads:
+            T._attend(tokens, starts, positions, s)
+        else:
+            lmt.matmul(*T.x8.rows, *T.proj8.rows, T.h, T.workspace, stream=s)       # h = x P^T
+        if T.keeps_logits:
+            T.table8.take(T.table, s)
+            T.h8.take(T.h, s)
+            lmt.matmul(*T.h8.rows, *T.table8.rows, T.logits, T.workspace, stream=s) # logits = h table^T
+            lmt.cross_entropy(T.logits, targets, T.loss, None, T.logits, weights, IGNORE, T.status, s)
+            T.dlogits8.take(T.logits, s)
+            lmt.matmul(*T.dlogits8.rows, *T.table8.cols, T.dh, T.workspace, stream=s)       # dh = dlogits table
+            lmt.matmul(*T.dlogits8.cols, *T.h8.cols, T.grad_table, T.workspace, stream=s)   # dtable = dlogits^T h
+        else:
+            lmt.embed(T.table, T.every_token, T.table16, stream=s)                  # the table in 16 bits
+            lmt.linear_cross_entropy(T.h, T.table16, targets, T.workspace, T.loss, None, T.dh, T.grad_table, weights, IGNORE, status=T.status, stream=s)
         T.dh8.take(T.dh, s)
-        lmt.matmul(*T.dh8.rows, *T.proj8.cols, T.dx, T.workspace, stream=s)         # dx = dh P
-        lmt.matmul(*T.dh8.cols, *T.x8.cols, T.grad_proj, T.workspace, stream=s)     # dP = dh^T x
-        lmt.embed_grad(T.dx, tokens, T.grad_table, T.workspace, T.scale, PADDING, True, T.status, s)
+        if T.heads:
+            T._attend_grad(starts, positions, s)
+            dx = T.dh
+        else:
+            lmt.matmul(*T.dh8.rows, *T.proj8.cols, T.dx, T.workspace, stream=s)     # dx = dh P
+            lmt.matmul(*T.dh8.cols, *T.x8.cols, T.grad_proj, T.workspace, stream=s) # dP = dh^T x
+            dx = T.dx
+        lmt.embed_grad(dx, tokens, T.grad_table, T.workspace, T.scale, PADDING, True, T.status, s)
 
-    def step(self, tokens, targets, weights, stream=None) -> None:
-        self.gradients(tokens, targets, weights, stream)
+    def step(self, tokens, targets, weights, stream=None, starts=None, positions=None) -> None:
+        self.gradients(tokens, targets, weights, stream, starts, positions)
         self.step_count += 1
         self.plan.bucket_clip_adam(self.thresholds, self.hyper, self.step_count, stream=stream)
 
@@ -113,18 +185,30 @@ def batch(vocab: int, tokens: int, generator):
     return torch.where(pad, PADDING, t), targets, weights
 
 
+def sequences(tokens: int, longest: int, generator):
+    """Where sequences of 1 to `longest` tokens start (int32; as many as `tokens` could ever need, the last ones empty), and every token's position in its own."""
+    lengths = torch.randint(1, longest + 1, (tokens,), generator=generator, device="cuda")
+    starts = torch.cat([torch.zeros_like(lengths[:1]), lengths.cumsum(0)]).clamp_(max=tokens)
+    at = torch.arange(tokens, device="cuda")
+    return starts.to(torch.int32), at - starts[torch.searchsorted(starts, at, right=True) - 1]
+
+
 def main() -> None:
     ap = argparse.ArgumentParser(description=__doc__, formatter_class=argparse.RawDescriptionHelpFormatter)
     ap.add_argument("--vocab", type=int, default=1000)
     ap.add_argument("--width", type=int, default=256)
     ap.add_argument("--tokens", type=int, default=4096)
     ap.add_argument("--steps", type=int, default=200)
+    ap.add_argument("--heads", type=int, default=0, help="with an attention layer of so many heads")
+    ap.add_argument("--longest", type=int, default=128, help="with heads: tokens of the longest sequence")
+    ap.add_argument("--no-logits", action="store_true", help="never keep the logits")
     a = ap.parse_args()
-    model = TiedLm(a.vocab, a.width, a.tokens)
+    model = TiedLm(a.vocab, a.width, a.tokens, heads=a.heads, logits=not a.no_logits)
     g = torch.Generator(device="cuda")
     g.manual_seed(1)
     for i in range(a.steps):
-        model.step(*batch(a.vocab, a.tokens, g))
+        more = dict(zip(("starts", "positions"), sequences(a.tokens, a.longest, g))) if a.heads else {}
+        model.step(*batch(a.vocab, a.tokens, g), **more)
         if i % 20 == 0 or i + 1 == a.steps:
             print(f"step {i:4d}  loss {float(model.loss.sum()):.4f}", flush=True)
     assert int(model.status.item()) == 0
