@@ -95,7 +95,7 @@ struct Attention {
   const int32_t *starts, *lengths, *prefixes;
   const float* slopes;
   int32_t* status;
-  uint32_t rows, heads, kv_heads, group, parts, size, sequences;  // group: query heads of a key head
+  uint32_t rows, heads, kv_heads, group, parts, size, sequences, cuts;  // group: query heads of a key head; cuts: sequences, where they cut blocks of rows
   float scale, cap;
   bool causal;
 };

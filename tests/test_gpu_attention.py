@@ -122,6 +122,17 @@ def test_many_short_sequences():
     check(at(*([0] * 1500 + [200] + [0] * 1500)), heads=1, kv_heads=1, size=64)
 
 
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("size", [40, 128])
+def test_long_sequences_whose_starts_cut_blocks(causal, size):
+    """Few and long ones: a block's rows go to more than one workgroup."""
+    prefixes = [5, 0, 300, 1] if causal else None
+    check([37, 300, 300, 1000, 1101], heads=2, kv_heads=1, size=size, rows=1400, causal=causal, prefixes=prefixes)          # rows in front and behind that are none's
+    check([0, 128, 384, 900], heads=1, kv_heads=1, size=size, causal=causal, kind="f16")                                    # some start with a block
+    check([0, 600, 601, 602, 1290], heads=1, kv_heads=1, size=size, causal=causal, slopes=[0.2])                            # three in a block
+    check([200, 900], heads=1, kv_heads=1, size=size, rows=1000, causal=causal, only_forward=True)
+
+
 @pytest.mark.parametrize("heads,kv_heads", [(1, 1), (2, 1), (3, 3), (8, 1), (12, 4), (16, 2)])
 @pytest.mark.parametrize("size", [64, 128])
 def test_shared_heads(heads, kv_heads, size):
@@ -261,6 +272,7 @@ def test_tables_that_are_wrong_are_reported_and_do_no_harm():
                             ([0, 100, 200], [101, 100]), ([0, 100, 200], [-1, 100]), ([0, 100, 200], [2 ** 31 - 1, 2 ** 31 - 1])):
         for causal in (False, True):
             status = torch.zeros(1, dtype=torch.int32, device="cuda")
+            out.fill_(float("nan"))                         # every row is written, whatever the table
             lmt.attention(q, q, q, out, lse, device(starts, torch.int32), lengths=device(lengths, torch.int32), scale=0.2, causal=causal, status=status)
             torch.cuda.synchronize()
             assert int(status.item()) == lmt.LMT_STATUS_BAD_SEQUENCE and bool(torch.isfinite(out).all())
@@ -268,6 +280,17 @@ def test_tables_that_are_wrong_are_reported_and_do_no_harm():
             lmt.attention_grad(q, q, q, q, out, lse, *g, ws, device(starts, torch.int32), lengths=device(lengths, torch.int32), scale=0.2, causal=causal, status=status)
             torch.cuda.synchronize()
             assert int(status.item()) == lmt.LMT_STATUS_BAD_SEQUENCE and all(bool(torch.isfinite(x).all()) for x in g)
+
+
+def test_wrong_tables_of_long_sequences_leave_no_row_out():
+    q = torch.randn(1500, 1, 32, device="cuda").bfloat16()
+    out, lse = torch.empty_like(q), torch.empty(1, 1500, device="cuda")
+    for starts in ([0, 1000, 500, 1500], [700, 300, 1400, 100], [-5, 700, 1501], [1500, 200, 0, 900], [0, 2 ** 31 - 1, 3, 1500], [-2 ** 31, 400, 90, 2 ** 31 - 1]):
+        status = torch.zeros(1, dtype=torch.int32, device="cuda")
+        out.fill_(float("nan")), lse.fill_(float("nan"))
+        lmt.attention(q, q, q, out, lse, device(starts, torch.int32), scale=0.2, status=status)
+        torch.cuda.synchronize()
+        assert int(status.item()) == lmt.LMT_STATUS_BAD_SEQUENCE and bool(torch.isfinite(out).all()) and not bool(torch.isnan(lse).any())
 
 
 def test_the_same_call_gives_the_same_bits_and_a_graph_follows_its_inputs():
