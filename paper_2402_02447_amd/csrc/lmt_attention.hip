@@ -252,13 +252,12 @@ __device__ __forceinline__ uint32_t turn(uint32_t row) {
   if constexpr (D == 64) return (row >> 1 & 1u) << 2 | (row >> 2 & 1u) << 1 | (row >> 3 & 1u);
   else return (row & 3u) << 2 | (row >> 2 & 3u);
 }
-// DIRECT: from memory to LDS without registers, where all rows start on 16 bytes; else through registers.  Rows behind the last one are the last
-// one again: nobody sees them.
+// DIRECT: from memory to LDS without registers, where all rows start on 16 bytes; else through registers, at once, since those that hold a tile on its way are
+// not to be had.  Rows behind the last one are the last one again: nobody sees them.
 template <typename T, int D, int THREADS, bool DIRECT>
 struct Stage {
   static constexpr int pieces = D / 8, loads = kTile * pieces / THREADS, step = THREADS / pieces;
   static_assert(step % 16 == 0, "rows that a thread loads turn their pieces alike");
-  u32x4 w[DIRECT ? 1 : loads];
   uint32_t at, row;     // DIRECT: this thread's first piece, in bytes behind the tile's first row, and from row to row
   const uint8_t* base;  // the next tile's first row, and how many are behind it
   uint32_t behind;
@@ -279,20 +278,17 @@ struct Stage {
         for (uint32_t j = 0; j < loads; ++j) send_to_lds(base, at - r * row + min(r + j * step, behind) * row, 0, to + j * THREADS * 16u);
       }
     } else {
+      u32x4 w[loads];
+      const uint32_t piece = threadIdx.x % pieces;
 #pragma unroll
-      for (int j = 0; j < loads; ++j) w[j] = load_piece(reinterpret_cast<const T*>(base + (uint64_t)min(r + j * step, behind) * row), threadIdx.x % pieces, size);
-    }
-    base += (uint64_t)row * kTile, behind -= kTile;  // behind the last tile: of no concern
-  }
-  __device__ __forceinline__ void put(uint8_t* tile) const {
-    if constexpr (!DIRECT) {
-      const uint32_t piece = threadIdx.x % pieces, r = threadIdx.x / pieces;
+      for (int j = 0; j < loads; ++j) w[j] = load_piece(reinterpret_cast<const T*>(base + (uint64_t)min(r + j * step, behind) * row), piece, size);
 #pragma unroll
       for (int j = 0; j < loads; ++j) *reinterpret_cast<u32x4*>(tile + (r + j * step) * (D * 2) + (piece ^ turn<D>(r)) * 16u) = w[j];
     }
+    base += (uint64_t)row * kTile, behind -= kTile;  // behind the last tile: of no concern
   }
 };
-// What this wavefront has fetched and put is in LDS, and everybody's is.
+// What this wavefront has fetched is in LDS, and everybody's is.
 __device__ __forceinline__ void arrived() { wait_and_meet<0>(); }
 // A lane's own row in registers, as an operand for all of k = 0 .. D - 1, zeros where there is no element.
 template <typename T, int D>
@@ -647,14 +643,11 @@ __global__ __launch_bounds__(kThreads, D == 64 && DIRECT ? 3 : 2) void k_attend(
         for (int b = 0; b < 2; ++b) s[b] = mma(T{}, along.read(keys[now ^ 1u], b, c), q.w[c], s[b]);
       if constexpr (PLAIN) top = largest(s);
     }
-    if (more_keys) next_k.put(keys[now]);
-    if (more) next_v.put(values[now ^ 1u]);
     arrived();
   };
   if (first < last) {
     next_k.set(k, p.k, (uint32_t)first, p.rows, p.size), next_v.set(v, p.v, (uint32_t)first, p.rows, p.size);
     next_k.fetch(keys[0], p.size), next_v.fetch(values[0], p.size);
-    next_k.put(keys[0]), next_v.put(values[0]);
     arrived();
     const bool more = first + kTile < last;
     if (more) next_k.fetch(keys[1], p.size);
@@ -664,7 +657,6 @@ __global__ __launch_bounds__(kThreads, D == 64 && DIRECT ? 3 : 2) void k_attend(
 #pragma unroll
       for (int b = 0; b < 2; ++b) s[b] = mma(T{}, along.read(keys[0], b, c), q.w[c], s[b]);
     if constexpr (PLAIN) top = largest(s);
-    if (more) next_k.put(keys[1]);
     arrived();
     uint32_t now = 0;
     for (int at = first; at < last; at += kTile, now ^= 1u) pass(at, now);
@@ -800,7 +792,6 @@ __global__ __launch_bounds__(kThreads, 2) void k_attend_grad_q(const Attention p
   if (first < last) {
     next_k.set(k, p.k, (uint32_t)first, p.rows, p.size), next_v.set(v, p.v, (uint32_t)first, p.rows, p.size);
     next_k.fetch(keys[0], p.size), next_v.fetch(values[0], p.size);
-    next_k.put(keys[0]), next_v.put(values[0]);
   }
   arrived();
   uint32_t now = 0;
@@ -809,7 +800,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_attend_grad_q(const Attention p
     if (more) next_k.fetch(keys[now ^ 1u], p.size), next_v.fetch(values[now ^ 1u], p.size);
     if (span.touches(at, kTile)) {
       {
-        constexpr int kHalf = D / 16, kSteps = 6 * kHalf, kAhead = 3;  // of k; of matrix instructions: scores and products with v of either half, then sums of either
+        constexpr int kHalf = D / 16, kSteps = 6 * kHalf, kAhead = D == 128 && !PLAIN ? 2 : 3;  // of k; of matrix instructions: scores and products with v of either half, then sums of either
         f32x16 s[2][1] = {}, dp[2][1] = {};
         u32x4 w[2][2], ahead[kAhead];
         const auto operand = [&](int t) {
@@ -862,7 +853,6 @@ __global__ __launch_bounds__(kThreads, 2) void k_attend_grad_q(const Attention p
         });
       }
     }
-    if (more) next_k.put(keys[now ^ 1u]), next_v.put(values[now ^ 1u]);
     arrived();
   }
   const uint64_t rows_again = __builtin_amdgcn_ballot_w64(some && !finite<D>(sum));
@@ -976,7 +966,6 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 2 : 1) void k_attend_grad_kv(co
     }
   };
   const auto put = [&](uint32_t to) {
-    next_q.put(queries[to]), next_go.put(grads[to]);
     if (threadIdx.x < kTile) lse[to][threadIdx.x] = subtracted(next_lse), delta[to][threadIdx.x] = next_delta;
   };
   if (first < last) fetch(h0, first, 0), put(0);
@@ -990,13 +979,14 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 2 : 1) void k_attend_grad_kv(co
       if (more) fetch(wrap ? head + 1u : head, wrap ? first : at + kTile, now ^ 1u);
       if (span.touches(at, kTile)) {
         {
-          constexpr int kHalf = D / 16, kSteps = 8 * kHalf, kAhead = D == 64 ? 3 : 4;
+          constexpr int kHalf = D / 16, kSteps = 8 * kHalf, kAhead = D == 128 ? 4 : PLAIN ? 3 : 2;
           f32x16 s[2][1] = {}, d[2][1] = {};
           u32x4 w[2][2], x[2][2], ahead[kAhead];
-          f32x4 less[2], dots[2];  // of four rows, and of the next four
+          constexpr int kRowsAhead = D == 64 ? 1 : 2;  // registers are short
+          f32x4 less[kRowsAhead], dots[kRowsAhead];    // of four rows, and of the next four
           const int half = 4 * (int)(lane >> 5);
           const auto rows = [&](int b, int g) {
-            less[g % 2] = *reinterpret_cast<const f32x4*>(&lse[now][32 * b + 8 * g + half]), dots[g % 2] = *reinterpret_cast<const f32x4*>(&delta[now][32 * b + 8 * g + half]);
+            less[g % kRowsAhead] = *reinterpret_cast<const f32x4*>(&lse[now][32 * b + 8 * g + half]), dots[g % kRowsAhead] = *reinterpret_cast<const f32x4*>(&delta[now][32 * b + 8 * g + half]);
           };
           const auto operand = [&](int t) {
             if (t < 4 * kHalf) return along.read(t % 2 ? grads[now] : queries[now], t / (2 * kHalf), t / 2 % kHalf);
@@ -1007,8 +997,8 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 2 : 1) void k_attend_grad_kv(co
           const bool inside = span.inside(at, kTile);
           const auto element = [&](int b, int e) {
             const int g = e / 4;
-            float p_ = exp2_of(PLAIN ? __builtin_fmaf(s[b][0][e], score.by, -less[g % 2][e % 4]) : s[b][0][e] - less[g % 2][e % 4]);
-            const float d_ = (PLAIN ? __builtin_fmaf(d[b][0][e], range.by, -dots[g % 2][e % 4] * range.by) : d[b][0][e]) * p_;
+            float p_ = exp2_of(PLAIN ? __builtin_fmaf(s[b][0][e], score.by, -less[g % kRowsAhead][e % 4]) : s[b][0][e] - less[g % kRowsAhead][e % 4]);
+            const float d_ = (PLAIN ? __builtin_fmaf(d[b][0][e], range.by, -dots[g % kRowsAhead][e % 4] * range.by) : d[b][0][e]) * p_;
             if constexpr (kShift<T> != 0.f) p_ *= 0x1p14f;  // weights are at most 1
             s[b][0][e] = p_, d[b][0][e] = d_;
           };
@@ -1042,16 +1032,16 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 2 : 1) void k_attend_grad_kv(co
             if constexpr (t == 2 * kHalf || t == 4 * kHalf) {
             if (!inside) hide(s[t / (2 * kHalf) - 1][0], from + (t == 4 * kHalf ? 32u : 0u), n);
           }
-            if constexpr (t == 2 * kHalf - 1) rows(0, 0);
+            if constexpr (t == 2 * kHalf - 1 && kRowsAhead == 2) rows(0, 0);
             if constexpr (t >= 2 * kHalf && t < 6 * kHalf) {
               constexpr int b = t >= 4 * kHalf, step = t - (b ? 4 : 2) * kHalf;
 #pragma unroll
               for (int e = step * 8 / kHalf; e < (step + 1) * 8 / kHalf; ++e) {
-                if (e % 4 == 0 && e < 12) rows(b, e / 4 + 1);
+                if (kRowsAhead == 2 ? e % 4 == 0 && e < 12 : e % 4 == 0) rows(b, e / 4 + kRowsAhead - 1);
                 element(b, e);
               }
               if constexpr (step + 1 == 2 * kHalf) {
-                if constexpr (b == 0) rows(1, 0);
+                if constexpr (b == 0 && kRowsAhead == 2) rows(1, 0);
                 range.fit(d[b], dk);
 #pragma unroll
                 for (int c = 0; c < 2; ++c) w[b][c] = packed<T>(s[b][0], c), x[b][c] = packed<T>(d[b][0], c);
