@@ -145,7 +145,8 @@ int lmt_cross_entropy(const void* logits /*DEVICE*/, int dtype, uint64_t rows, u
  * x: [rows][x_ld], table: [classes][table_ld], both of `dtype`, LMT_F16 or LMT_BF16; rows, classes and width are up to LMT_MAX_WIDTH.  Logits, losses and
  * sums are in fp32; elements of g are rounded to `dtype` (fp16: scaled by powers of two, so that none gets lost below its range) before
  * they are multiplied.  loss, lse (DEVICE [rows], fp32), grad_x (of `dtype`, [rows][grad_x_ld]) and grad_table (of grad_table_dtype,
- * `dtype` or LMT_F32, [classes][grad_table_ld]) may each be NULL.  Ignored rows take no part, whatever they hold.
+ * `dtype` or LMT_F32, [classes][grad_table_ld]) may each be NULL.  Ignored rows have no loss, a grad_x of zeros and no part in grad_table, whatever they
+ * hold; their lse is that of any row.
  * Infinities and NaN in a row of x or in its weight are in that row's results and in grad_table; those in a row of the table are in everything.
  * workspace: DEVICE, 16-byte aligned, lmt_linear_cross_entropy_workspace bytes (with gradients != 0 if grad_x or grad_table is given),
  * contents of no concern; not shared by calls that overlap in time.  Without rows a grad_table that is not added to is refused. */
@@ -184,7 +185,7 @@ typedef struct lmt_attend {
   const int32_t *starts /*DEVICE [sequences + 1]*/, *lengths /*DEVICE [sequences] or NULL*/;
   const int32_t* prefixes;                /* DEVICE [sequences] or NULL, with LMT_CAUSAL: all of a sequence sees its first prefixes[s] positions */
   const float* slopes;                    /* DEVICE [heads] or NULL                                                        */
-  double scale, cap;                      /* cap: 0 for none                                                               */
+  double scale, cap;                      /* cap: 0 for none;  1.5 times either, and scale / cap, are finite in fp32       */
   int32_t* status;                        /* DEVICE or NULL                                                                */
 } lmt_attend;
 

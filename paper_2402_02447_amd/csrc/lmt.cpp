@@ -55,9 +55,11 @@ int attend_error(const lmt_attend* a) {
   if (a->prefixes && !(a->flags & LMT_CAUSAL)) return fail(LMT_ERR_ARG, "prefixes without LMT_CAUSAL");
   if (!std::isfinite((float)a->scale)) return fail(LMT_ERR_ARG, "scale is not a finite fp32 number");
   if (!std::isfinite((float)a->cap) || a->cap < 0 || (a->cap != 0 && (float)a->cap < 1e-30f)) return fail(LMT_ERR_ARG, "cap is neither 0 nor a positive fp32 number");
+  if (!std::isfinite((float)a->scale * 1.5f) || !std::isfinite((float)a->cap * 1.5f) || (a->cap != 0 && !std::isfinite((float)a->scale / (float)a->cap)))
+    return fail(LMT_ERR_ARG, "scale, cap or scale / cap in units of log 2 are beyond fp32");
   if (a->rows > LMT_MAX_ROWS || a->sequences > LMT_MAX_ROWS || a->heads > LMT_MAX_HEADS || a->kv_heads > LMT_MAX_HEADS || a->size > LMT_MAX_HEAD)
     return fail(LMT_ERR_LIMIT, "sizes exceed LMT_MAX_ROWS, LMT_MAX_HEADS or LMT_MAX_HEAD");
-  if (a->kv_heads == 0 ? a->heads != 0 : a->heads % a->kv_heads != 0) return fail(LMT_ERR_ARG, "the query heads are no multiple of the key heads");
+  if (a->kv_heads == 0 ? a->heads != 0 : a->heads == 0 || a->heads % a->kv_heads != 0) return fail(LMT_ERR_ARG, "the query heads are no multiple of the key heads");
   if (lmt::attention_launches(a->rows, a->heads) > lmt::kMaxWorkgroups) return fail(LMT_ERR_LIMIT, "rows times heads are more than a launch can have");
   if (a->sequences != 0 && !a->starts) return fail(LMT_ERR_NULL, "starts is NULL");
   if (off(a->starts, 4) || off(a->lengths, 4) || off(a->prefixes, 4) || off(a->slopes, 4) || off(a->status, 4)) return fail(LMT_ERR_ALIGN, "a pointer is not aligned to its element size");

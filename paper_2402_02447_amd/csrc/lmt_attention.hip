@@ -488,12 +488,16 @@ __device__ __forceinline__ void place(uint32_t tiles, uint32_t cuts, uint32_t li
   constexpr uint32_t kXcds = 8;
   if (longest == kAny) {
     const uint32_t id = (uint32_t)neighbours(blockIdx.x, tiles * lists);
-    *list = id / tiles, *tile = id % tiles;
+    *list = uniform(id / tiles), *tile = id - *list * tiles;
     return;
   }
   const uint32_t of_xcd = lists / kXcds;
-  if (lists % kXcds == 0) *list = blockIdx.x % kXcds * of_xcd + blockIdx.x / kXcds % of_xcd, *tile = blockIdx.x / kXcds / of_xcd;
-  else *list = blockIdx.x % lists, *tile = blockIdx.x / lists;
+  if (lists % kXcds == 0) {
+    const uint32_t in_xcd = blockIdx.x / kXcds;
+    *tile = uniform(in_xcd / of_xcd), *list = blockIdx.x % kXcds * of_xcd + in_xcd - *tile * of_xcd;
+  } else {
+    *tile = uniform(blockIdx.x / lists), *list = blockIdx.x - *tile * lists;
+  }
   if (longest == kLast && *tile >= cuts) *tile = tiles - 1u - (*tile - cuts);
 }
 
@@ -552,7 +556,7 @@ __global__ __launch_bounds__(kThreads, D == 64 && DIRECT ? 3 : 2) void k_attend(
   place(tiles, p.cuts, p.heads, p.causal ? kLast : kAny, &tile, &head);
   Block block;
   block.set(p, tile);
-  const uint32_t kv = head / p.group, wave = threadIdx.x >> 6, lane = threadIdx.x & 63u, row = wave * 32u + (lane & 31u), i = (uint32_t)block.first + row;
+  const uint32_t kv = uniform(head / p.group), wave = threadIdx.x >> 6, lane = threadIdx.x & 63u, row = wave * 32u + (lane & 31u), i = (uint32_t)block.first + row;
   const T *k = head_of<T>(p.k, kv), *v = head_of<T>(p.v, kv);
   check_sequences(p);
   Row<T, D> q;
@@ -756,7 +760,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_attend_grad_q(const Attention p
   uint32_t tile, head;
   place(tiles, 0u, p.heads, p.causal ? kLast : kAny, &tile, &head);
   const Block block{(int)(tile * kRows), -1};
-  const uint32_t kv = head / p.group, wave = threadIdx.x >> 6, lane = threadIdx.x & 63u, row = wave * 32u + (lane & 31u), i = (uint32_t)block.first + row, held = min(i, p.rows - 1u);
+  const uint32_t kv = uniform(head / p.group), wave = threadIdx.x >> 6, lane = threadIdx.x & 63u, row = wave * 32u + (lane & 31u), i = (uint32_t)block.first + row, held = min(i, p.rows - 1u);
   const T *k = head_of<T>(p.k, kv), *v = head_of<T>(p.v, kv);
   check_sequences(p);
   Row<T, D> q, go;
@@ -941,7 +945,7 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 2 : 1) void k_attend_grad_kv(co
   uint32_t tile, list;
   place(tiles, 0u, p.kv_heads * p.parts, p.causal ? kFirst : kAny, &tile, &list);
   const Block block{(int)(tile * kRows), -1};
-  const uint32_t kv = list / p.parts, part = list % p.parts, h0 = kv * p.group + part * p.group / p.parts, h1 = kv * p.group + (part + 1u) * p.group / p.parts;
+  const uint32_t kv = uniform(list / p.parts), part = list - kv * p.parts, h0 = kv * p.group + uniform(part * p.group / p.parts), h1 = kv * p.group + uniform((part + 1u) * p.group / p.parts);
   const uint32_t wave = threadIdx.x >> 6, lane = threadIdx.x & 63u, row = wave * 32u + (lane & 31u), j = (uint32_t)block.first + row, held = min(j, p.rows - 1u);
   Row<T, D> k, v;
   k.read(row_of(head_of<T>(p.k, kv), p.k, held), p.size), v.read(row_of(head_of<T>(p.v, kv), p.v, held), p.size);

@@ -62,14 +62,17 @@ __device__ __forceinline__ uint32_t load_word(const uint8_t* base, uint32_t offs
 __device__ __forceinline__ void load_to_lds(const uint8_t* base, uint32_t offset, uint32_t wave_offset, uint8_t* lds) {
   __builtin_amdgcn_raw_ptr_buffer_load_lds(__builtin_amdgcn_make_buffer_rsrc((void*)base, 0, -1, 0x27000), (__attribute__((address_space(3))) void*)lds, 16, (int)offset, (int)wave_offset, 0, 0);
 }
+// A number that is the same in all lanes, in a scalar register: what is made by a division, for one, is not there by itself.
+__device__ __forceinline__ uint32_t uniform(uint32_t x) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)x); }
 // The same, without the compiler's knowledge: it waits for every load to LDS in front of every read of LDS that could be of the same
 // place, and does not see that buffers take turns.  So whoever reads what was sent waits for it himself (wait_and_meet).  No register is written, and the
-// operands are read when the instruction is issued.
+// operands are read when the instruction is issued.  Scalar registers that a vector instruction wrote (a lane read into one) may be read by a load five
+// wait states later, which the compiler sees to for its own instructions alone: hence s_nop 4, which covers m0's one as well.
 __device__ __forceinline__ void send_to_lds(const uint8_t* base, uint32_t offset, uint32_t wave_offset, uint8_t* lds) {
   const uint64_t at = (uint64_t)(uintptr_t)base;
-  const u32x4 rsrc = {(uint32_t)at, (uint32_t)(at >> 32) & 0xffffu, 0xffffffffu, 0x27000u};
-  asm volatile("s_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"{m0}"((uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)lds), "v"(offset), "s"(rsrc),
-               "s"(wave_offset)
+  const u32x4 rsrc = {uniform((uint32_t)at), uniform((uint32_t)(at >> 32)) & 0xffffu, 0xffffffffu, 0x27000u};
+  asm volatile("s_nop 4\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"{m0}"((uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)lds), "v"(offset), "s"(rsrc),
+               "s"(uniform(wave_offset))
                : "memory");
 }
 // At most N of this wavefront's loads are in flight and none of its LDS reads; then a barrier.  (A barrier alone does not order memory

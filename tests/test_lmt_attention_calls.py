@@ -75,6 +75,9 @@ BAD += [(attention, dict(out=(P, 63, 16)), ARG), (attention, dict(out=(P, 64, 0)
         (loss, dict(width=0), ARG), (loss, dict(rows=0), ARG), (loss, dict(rows=1 << 23), LIMIT), (loss, dict(classes=1 << 23), LIMIT), (loss, dict(width=1 << 23, x_ld=1 << 23, table_ld=1 << 23, gx_ld=1 << 23, gt_ld=1 << 23), LIMIT),
         (loss, dict(rows=1 << 22, classes=1 << 22), LIMIT), (loss, dict(x=P + 1), ALIGN), (loss, dict(gt=P + 2, gt_dt=0), ALIGN), (loss, dict(loss=P + 2), ALIGN), (loss, dict(t=P + 4), ALIGN), (loss, dict(ws=P + 8), ALIGN),
         (loss, dict(ws_bytes=100), WORKSPACE)]
+for call in (attention, attention_grad):
+    BAD += [(call, dict(by=dict(scale=3e38)), ARG), (call, dict(by=dict(scale=-3e38)), ARG), (call, dict(by=dict(cap=3e38)), ARG), (call, dict(by=dict(scale=1e20, cap=1e-20)), ARG),
+            (call, dict(by=dict(heads=0)), ARG)]                                     # key heads that nobody asks would have gradients
 
 
 @pytest.mark.parametrize("call,changed,code", BAD, ids=lambda x: getattr(x, "__name__", str(x)))
