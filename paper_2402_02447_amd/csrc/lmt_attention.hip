@@ -804,7 +804,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_attend_grad_q(const Attention p
     if (more) next_k.fetch(keys[now ^ 1u], p.size), next_v.fetch(values[now ^ 1u], p.size);
     if (span.touches(at, kTile)) {
       {
-        constexpr int kHalf = D / 16, kSteps = 6 * kHalf, kAhead = D == 128 && !PLAIN ? 2 : 3;  // of k; of matrix instructions: scores and products with v of either half, then sums of either
+        constexpr int kHalf = D / 16, kSteps = 6 * kHalf, kAhead = 3;  // of k; of matrix instructions: scores and products with v of either half, then sums of either
         f32x16 s[2][1] = {}, dp[2][1] = {};
         u32x4 w[2][2], ahead[kAhead];
         const auto operand = [&](int t) {
