@@ -246,7 +246,7 @@ __device__ __forceinline__ const T* row_of(const T* head, const Heads& x, uint32
 
 // kTile rows of D elements in LDS.  The 16-byte pieces of a row change places by the row's number: reads of one piece of 16 rows and
 // transposing reads of four rows then meet every bank once.
-constexpr int kTile = 64, kAhead = 4;  // kAhead: operands on their way from LDS
+constexpr int kTile = 64, kAhead = 4;  // kAhead: operands that are held, of which kAhead - 1 are on their way from LDS
 template <int D>
 __device__ __forceinline__ uint32_t turn(uint32_t row) {
   if constexpr (D == 64) return (row >> 1 & 1u) << 2 | (row >> 2 & 1u) << 1 | (row >> 3 & 1u);
@@ -482,7 +482,7 @@ constexpr float kShift<_Float16> = 7.f;
 // Which head and block of rows a workgroup has.  An XCD, which takes every eighth workgroup, has one head after the other, so that its L2 sees the
 // same keys again and again.  CAUSAL, where blocks are from 1 to `tiles` long: the longest of all heads that an XCD has come first (kFirst or kLast says
 // which end that is), since those that come last decide when it ends; heads that do not divide by XCDs go over all of them.
-// 16 heads of 8 192 rows of 64: one head after the other 213 us, longest first 183.
+// 16 heads of 8 192 rows of 64: one head after the other 213 us, longest first 176.
 enum Order { kAny, kFirst, kLast };
 __device__ __forceinline__ void place(uint32_t tiles, uint32_t cuts, uint32_t lists, Order longest, uint32_t* tile, uint32_t* list) {
   constexpr uint32_t kXcds = 8;
@@ -547,7 +547,12 @@ __device__ __forceinline__ void attend_row(const Attention& p, uint32_t head, ui
 }
 
 // The scores of the next tile are made while those of this one go through exp2: matrix instructions and the others take turns in the
-// instruction stream, as one wavefront's do not overlap unless they are side by side in it.
+// instruction stream, as one wavefront's do not overlap unless they are side by side in it.  Operands are asked for kAhead - 1 instructions early.
+// A tile of 32 x 64 is 16 matrix instructions of 32 cycles with heads of 64 (32 with 128) and about 200 others, an exponential counting double, so that heads of 64 are
+// bound by vector issue (78 % of the busy cycles; matrix cores 45 %) and heads of 128 by the two together (53 and 56 %).  LDS has no bank conflicts.  bf16, 16 heads
+// of 8 192 rows: 64, causal 176 us, 0.78 PFLOP/s; 128 512 us, 1.07, causal 282, 0.97, with a cap 368 (its tanh is as many instructions again).  16 sequences of 512, heads of 64: 34 us.
+// One workgroup's 64 keys take 0.93 us (64) or 1.18 (128), which is what few rows wait for.  Three workgroups a compute unit with heads of 64: 118 us where two take 146
+// (128 sequences of up to 512, 16 heads).  Two tiles to a round instead of one: 1.18 -> 1.07 us, but registers spill and 16 of 512 take 39 us for 34.
 template <typename T, int D, bool PLAIN, bool DIRECT>
 __global__ __launch_bounds__(kThreads, D == 64 && DIRECT ? 3 : 2) void k_attend(const Attention p, uint32_t tiles) {
   __shared__ __align__(16) uint8_t keys[2][kTile * D * 2], values[2][kTile * D * 2];
@@ -752,7 +757,10 @@ __device__ __forceinline__ void grad_q_row(const Attention& p, uint32_t head, ui
 __device__ __forceinline__ float subtracted(float lse) { return lse == -kInf ? kInf : lse * kLog2e; }
 
 // Gradient of q and, for the next kernel, delta = grad_out . out of every row: as the forward pass, scores and products with v from a tile of each, d into the
-// sums with k across.
+// sums with k across.  One half tile's exponentials stand beside the other one's products.  Three products here and four in the next kernel instead of five in
+// one: sums of both kinds do not fit a wavefront's registers, and one kernel would have to add one of them to memory from many workgroups, in no order.  16 heads of 8 192 rows
+// of 128, causal: 392 us, matrix cores busy 67 % of the time; 128 sequences of up to 512, 16 heads of 64: 153.  (The general form of heads of 128 keeps 20 bytes in
+// scratch: with an operand less ahead it does not, and takes 297 us for 281.)
 template <typename T, int D, bool PLAIN, bool DIRECT>
 __global__ __launch_bounds__(kThreads, 2) void k_attend_grad_q(const Attention p, uint32_t tiles) {
   __shared__ __align__(16) uint8_t keys[2][kTile * D * 2], values[2][kTile * D * 2];
@@ -936,7 +944,9 @@ __device__ __forceinline__ void grad_kv_row(const Attention& p, uint32_t kv, uin
 }
 
 // Gradients of k and v: a lane has a key, the rows that see it come by in tiles, for one query head after the other.  Scores as Q K^T, so that
-// what a lane has of them is an operand of dO^T P and Q^T d.
+// what a lane has of them is an operand of dO^T P and Q^T d.  With heads of 128 the sums and the key's rows take more than half the registers: one wavefront a SIMD, and
+// what its instructions wait for each other is not filled by another's: 16 heads of 8 192 rows of 128, causal 610 us, matrix cores busy 38 % of the time, vector issue 28 %, 41 % waiting
+// (operands 5 or 7 instructions early instead of 3: no difference).  Heads of 64, two wavefronts: 128 sequences of up to 512, 16 heads 212 us.
 template <typename T, int D, bool PLAIN, bool DIRECT>
 __global__ __launch_bounds__(kThreads, D == 64 ? 2 : 1) void k_attend_grad_kv(const Attention p, uint32_t tiles) {
   __shared__ __align__(16) uint8_t queries[2][kTile * D * 2], grads[2][kTile * D * 2];
@@ -1007,7 +1017,7 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 2 : 1) void k_attend_grad_kv(co
             s[b][0][e] = p_, d[b][0][e] = d_;
           };
           const auto general = [&](auto half_of) {  // what is not PLAIN's, for a whole half
-          constexpr int b = decltype(half_of)::value;
+            constexpr int b = decltype(half_of)::value;
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
               const f32x4 x = *reinterpret_cast<const f32x4*>(&delta[now][32 * b + 8 * g + half]);
@@ -1034,8 +1044,8 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 2 : 1) void k_attend_grad_kv(co
               if constexpr (t == 2 * kHalf || t == 4 * kHalf) general(std::integral_constant<int, t / (2 * kHalf) - 1>{});
             }
             if constexpr (t == 2 * kHalf || t == 4 * kHalf) {
-            if (!inside) hide(s[t / (2 * kHalf) - 1][0], from + (t == 4 * kHalf ? 32u : 0u), n);
-          }
+              if (!inside) hide(s[t / (2 * kHalf) - 1][0], from + (t == 4 * kHalf ? 32u : 0u), n);
+            }
             if constexpr (t == 2 * kHalf - 1 && kRowsAhead == 2) rows(0, 0);
             if constexpr (t >= 2 * kHalf && t < 6 * kHalf) {
               constexpr int b = t >= 4 * kHalf, step = t - (b ? 4 : 2) * kHalf;
@@ -1076,7 +1086,7 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 2 : 1) void k_attend_grad_kv(co
   }
 }
 
-// Adds the parts' sums in order: a thread 8 elements of a key.
+// Adds the parts' sums in order: a thread 8 elements of a key.  Memory: 8 parts of 8 192 x 2 heads of 128 in 22 us, 6 TB/s.
 template <typename T, int D>
 __global__ __launch_bounds__(256) void k_attend_join(const Attention p) {
   const uint64_t n = (uint64_t)2 * p.kv_heads * p.rows * (D / 8), of = (uint64_t)blockIdx.x * 256u + threadIdx.x;
@@ -1124,6 +1134,7 @@ hipError_t with_form(const Attention& p, int dtype, bool straight, F f) {
 }  // namespace
 
 uint32_t attention_parts(uint64_t rows, uint64_t heads, uint64_t kv_heads, uint64_t) {
+  // up to four workgroups a compute unit, as long as there are query heads; each part costs 8 bytes an element of k written and read once more
   const uint64_t group = heads / kv_heads, there = ceil_div(rows, kRows) * kv_heads;
   return (uint32_t)std::max<uint64_t>(1, std::min(group, 4 * kCus / there));
 }

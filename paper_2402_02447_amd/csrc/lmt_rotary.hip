@@ -19,7 +19,8 @@ __device__ __forceinline__ float2 turn_of(int64_t position, float frequency, flo
 }
 
 // A workgroup takes `tokens` rows: their turns go to LDS, made once for all heads, then `across` lanes (a power of two) take a head's pieces of 8
-// elements: HALF: 8 pairs from two places, else 4 pairs in a row; behind them what is only copied.
+// elements: 8 pairs from two places or, NEIGHBOURS, 4 pairs in a row; behind them what is only copied.
+// Memory bounds it: 32 768 rows of 32 heads of 64 in bf16 in 48 us, 5.6 TB/s.  (Streaming stores 59.6 -> 61 us among other calls and, where a batch stays in the Infinity Cache, 15.8 -> 24; streaming loads 63.)
 template <typename T, typename I, bool NEIGHBOURS>
 __global__ __launch_bounds__(kThreads) void k_rotary(const Rotary p, uint32_t tokens, uint32_t across, uint32_t pieces, uint32_t copies) {
   __shared__ float2 turns[kTurns];
