@@ -311,6 +311,11 @@ struct Row {
       }
     }
   }
+  // Waits until it is there.  The compiler would wait where it is used first, in every round of a loop, and with it for the tiles that are on their way behind it.
+  __device__ __forceinline__ void wait() {
+#pragma unroll
+    for (int c = 0; c < D / 16; ++c) asm volatile("" : "+v"(w[c]));
+  }
 };
 template <int D>
 struct Along {
@@ -400,7 +405,7 @@ struct Score {
   float by, cap, to_cap, slope;  // by: scale * log2(e);  cap, slope: in units of log 2;  to_cap: scale / the cap
   __device__ __forceinline__ void set(const Attention& p, uint32_t head) {
     by = p.scale * kLog2e, cap = p.cap * kLog2e, to_cap = p.cap != 0.f ? p.scale / p.cap : 0.f;
-    slope = p.slopes ? load1(p.slopes + head) * kLog2e : 0.f;
+    slope = p.slopes ? __uint_as_float(uniform(__float_as_uint(load1(p.slopes + head)))) * kLog2e : 0.f;  // here and now, as Row::wait
   }
   static __device__ __forceinline__ float series(float x) {
     const float y = x * x;
@@ -787,6 +792,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_attend_grad_q(const Attention p
   }
   const float lse = subtracted(load1(p.lse + (uint64_t)head * p.rows + held));
   find_seen<false>(p, block, seen);
+  q.wait(), go.wait();
   Span span;
   span.read(seen, row);
   const bool some = span.some();
@@ -960,6 +966,7 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 2 : 1) void k_attend_grad_kv(co
   Row<T, D> k, v;
   k.read(row_of(head_of<T>(p.k, kv), p.k, held), p.size), v.read(row_of(head_of<T>(p.v, kv), p.v, held), p.size);
   find_seen<true>(p, block, seen);
+  k.wait(), v.wait();
   Span span;
   span.read(seen, row);
   const int first = __builtin_amdgcn_readfirstlane(seen.first), last = __builtin_amdgcn_readfirstlane(seen.last);
