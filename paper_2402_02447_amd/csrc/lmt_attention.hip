@@ -311,7 +311,8 @@ struct Row {
       }
     }
   }
-  // Waits until it is there.  The compiler would wait where it is used first, in every round of a loop, and with it for the tiles that are on their way behind it.
+  // Waits until it is there.  The compiler would wait where it is used first, in every round of a loop, and with it for the tiles that are on their way behind it
+  // (16 heads of 8 192 rows of 128, both gradients 1 920 us for 1 780).
   __device__ __forceinline__ void wait() {
 #pragma unroll
     for (int c = 0; c < D / 16; ++c) asm volatile("" : "+v"(w[c]));
@@ -764,7 +765,7 @@ __device__ __forceinline__ float subtracted(float lse) { return lse == -kInf ? k
 // Gradient of q and, for the next kernel, delta = grad_out . out of every row: as the forward pass, scores and products with v from a tile of each, d into the
 // sums with k across.  One half tile's exponentials stand beside the other one's products.  Three products here and four in the next kernel instead of five in
 // one: sums of both kinds do not fit a wavefront's registers, and one kernel would have to add one of them to memory from many workgroups, in no order.  16 heads of 8 192 rows
-// of 128, causal: 392 us, matrix cores busy 67 % of the time; 128 sequences of up to 512, 16 heads of 64: 153.  (The general form of heads of 128 keeps 20 bytes in
+// of 128, causal: 386 us, matrix cores busy 67 % of the time; 128 sequences of up to 512, 16 heads of 64: 155.  (The general form of heads of 128 keeps 20 bytes in
 // scratch: with an operand less ahead it does not, and takes 297 us for 281.)
 template <typename T, int D, bool PLAIN, bool DIRECT>
 __global__ __launch_bounds__(kThreads, 2) void k_attend_grad_q(const Attention p, uint32_t tiles) {
@@ -951,8 +952,8 @@ __device__ __forceinline__ void grad_kv_row(const Attention& p, uint32_t kv, uin
 
 // Gradients of k and v: a lane has a key, the rows that see it come by in tiles, for one query head after the other.  Scores as Q K^T, so that
 // what a lane has of them is an operand of dO^T P and Q^T d.  With heads of 128 the sums and the key's rows take more than half the registers: one wavefront a SIMD, and
-// what its instructions wait for each other is not filled by another's: 16 heads of 8 192 rows of 128, causal 610 us, matrix cores busy 38 % of the time, vector issue 28 %, 41 % waiting
-// (operands 5 or 7 instructions early instead of 3: no difference).  Heads of 64, two wavefronts: 128 sequences of up to 512, 16 heads 212 us.
+// what its instructions wait for each other is not filled by another's: 16 heads of 8 192 rows of 128, causal 600 us, matrix cores busy 45 % of the time, vector issue 35 %, 31 % waiting
+// (operands 5 or 7 instructions early instead of 3: no difference).  Heads of 64, two wavefronts: 128 sequences of up to 512, 16 heads 204 us.
 template <typename T, int D, bool PLAIN, bool DIRECT>
 __global__ __launch_bounds__(kThreads, D == 64 ? 2 : 1) void k_attend_grad_kv(const Attention p, uint32_t tiles) {
   __shared__ __align__(16) uint8_t queries[2][kTile * D * 2], grads[2][kTile * D * 2];
