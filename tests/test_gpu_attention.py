@@ -325,6 +325,35 @@ def test_the_same_call_gives_the_same_bits_and_a_graph_follows_its_inputs():
             assert torch.equal(x, y) and torch.equal(x, z)
 
 
+def test_calls_on_two_streams_at_once():
+    """Calls that share their inputs and nothing else give what they give one after the other."""
+    T, H, G, D = 2000, 12, 4, 128
+    q, go = (torch.randn(T, H, D, device="cuda").bfloat16() for _ in range(2))
+    k, v = (torch.randn(T, G, D, device="cuda").bfloat16() for _ in range(2))
+    starts = [device(x, torch.int32) for x in ([0, T], [0, 100, 700, 701, 1900])]
+
+    def call(s, stream=None):
+        o, lse, gq, gk, gv = torch.zeros_like(q), torch.zeros(H, T, device="cuda"), torch.zeros_like(q), torch.zeros_like(k), torch.zeros_like(v)
+        workspace = torch.empty(lmt.attention_grad_workspace(T, H, G, D), dtype=torch.uint8, device="cuda")
+        torch.cuda.synchronize()
+
+        def enqueue():
+            lmt.attention(q, k, v, o, lse, s, scale=0.1, causal=True, stream=stream)
+            lmt.attention_grad(go, q, k, v, o, lse, gq, gk, gv, workspace, s, scale=0.1, causal=True, stream=stream)
+        return enqueue, (o, lse, gq, gk, gv), workspace
+    alone = [call(s) for s in starts]
+    for enqueue, _, _ in alone:
+        enqueue()
+        torch.cuda.synchronize()
+    at_once = [call(s, torch.cuda.Stream()) for s in starts]
+    for _ in range(3):
+        for enqueue, _, _ in at_once:
+            enqueue()
+    torch.cuda.synchronize()
+    for (_, want, _), (_, got, _) in zip(alone, at_once):
+        assert all(torch.equal(x, y) for x, y in zip(want, got))
+
+
 def test_offsets_beyond_32_bits():
     """70 rows 2^26 elements apart: the last one lies 8.6 GiB behind the first."""
     step, T, D = 1 << 26, 70, 64
