@@ -203,7 +203,7 @@ int lmt_attention(const lmt_attend* a, const lmt_heads* q, const lmt_heads* k, c
  *   d[j] = p[j] (grad_out[i] . v[j] - grad_out[i] . out[i]),  p[j] = exp(s[j] - lse),  times 1 - (s / cap)^2 behind a cap
  *   grad_q[i] = scale * sum over j of d[j] k[j];  grad_k[j] = scale * sum over i of d[j] q[i];  grad_v[j] = sum over i of p[j] grad_out[i]
  * A key head's gradients are sums over the query heads that use it.  Rows of no sequence get zeros.  p and d are rounded to `dtype`
- * before they are multiplied (fp16: d scaled by a power of two that follows its size).  workspace: DEVICE, 16-byte aligned, at least
+ * before they are multiplied (fp16: d scaled by a power of two that follows the largest of its row, of q for grad_q and of k for grad_k).  workspace: DEVICE, 16-byte aligned, at least
  * lmt_attention_grad_workspace bytes, contents of no concern; not shared by calls that overlap in time. */
 uint64_t lmt_attention_grad_workspace(uint64_t rows, uint64_t heads, uint64_t kv_heads, uint64_t size);
 int lmt_attention_grad(const lmt_attend* a, const lmt_heads* grad_out, const lmt_heads* q, const lmt_heads* k, const lmt_heads* v,

@@ -698,27 +698,31 @@ __global__ __launch_bounds__(kThreads, D == 64 && DIRECT ? 3 : 2) void k_attend(
 
 // ---- gradient -------------------------------------------------------------------------------------
 
-// What a wavefront's d are multiplied by before they are rounded to fp16: a power of two that brings the largest so far to 2^14 or below.  The sums
-// follow when it changes.  bf16 has fp32's range.
+// What d are multiplied by before they are rounded to fp16: a power of two of the lane's own row (of q, or of k), that brings the largest so far to
+// between 2^13 and 2^14 when it has left fp16's range, so that others are exact to 2^-38 of it; the row's sums, which are the lane's too, follow.  Rows of
+// the same wavefront that have come beyond 2^14 go with it, which halves how often that happens (9 of 256 half tiles instead of 21 for normal numbers).  One power for all rows of a
+// wavefront would cost less (16 heads of 8 192 rows of 128 in fp16: 2 072 us for 2 098), but take bits, or everything, from rows beside one with much larger d, in another sequence or in none.  Lanes
+// whose row sees nothing have no scale: in tiles that are inside of all others' intervals their d are not hidden, and grow with whatever the rows hold.  What is
+// not finite has none either: its sums are not, and are computed once more.  bf16 has fp32's range.
+constexpr float kHalfMost = 65504.f;
 template <typename T>
 struct Range {
   float by = 1.f;
   __device__ __forceinline__ void begin() {
     if constexpr (sizeof(T) == 2 && kShift<T> != 0.f) by = 0x1p60f;
   }
-  // True if x, times by, are too large: then `by` is smaller, x and the sums have followed.
+  // Where x, times by, are too large: then `by` is smaller, x and the sums have followed.
   template <int N, int M>
-  __device__ __forceinline__ void fit(f32x16 (&x)[N], f32x16 (&sums)[M]) {
+  __device__ __forceinline__ void fit(f32x16 (&x)[N], f32x16 (&sums)[M], bool some) {
     if constexpr (kShift<T> != 0.f) {
       float top = 0;
 #pragma unroll
       for (int b = 0; b < N; ++b)
 #pragma unroll
         for (int e = 0; e < 16; ++e) top = fmaxf(top, __builtin_fabsf(x[b][e]));
-      if (any(top > 0x1p15f)) {
-        top = wave_max(top);
-        if (!(top < kInf)) top = 0x1p15f;  // it goes wrong anyway, and is computed once more
-        const float down = __uint_as_float((127u + 14u + 127u - (__float_as_uint(top) >> 23)) << 23);
+      if (any(some && top > kHalfMost)) {
+        top = halves_max(top);
+        const float down = some && top >= 0x1p14f && top < kInf ? __uint_as_float((127u + 13u + 127u - (__float_as_uint(top) >> 23)) << 23) : 1.f;
         by *= down;
 #pragma unroll
         for (int b = 0; b < N; ++b) x[b] *= down;
@@ -864,7 +868,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_attend_grad_q(const Attention p
 #pragma unroll
             for (int e = step * 16 / n_steps; e < (step + 1) * 16 / n_steps; ++e) element(b, e);
             if constexpr (step + 1 == n_steps) {
-              range.fit(s[b], sum);
+              range.fit(s[b], sum, some);
               w[b][0] = packed<T>(s[b][0], 0), w[b][1] = packed<T>(s[b][0], 1);
             }
           }
@@ -970,6 +974,7 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 2 : 1) void k_attend_grad_kv(co
   k.wait(), v.wait();
   Span span;
   span.read(seen, row);
+  const bool some = span.some();
   const int first = __builtin_amdgcn_readfirstlane(seen.first), last = __builtin_amdgcn_readfirstlane(seen.last);
   Along<D> along;
   Across<D> across;
@@ -1064,7 +1069,7 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 2 : 1) void k_attend_grad_kv(co
               }
               if constexpr (step + 1 == 2 * kHalf) {
                 if constexpr (b == 0 && kRowsAhead == 2) rows(1, 0);
-                range.fit(d[b], dk);
+                range.fit(d[b], dk, some);
 #pragma unroll
                 for (int c = 0; c < 2; ++c) w[b][c] = packed<T>(s[b][0], c), x[b][c] = packed<T>(d[b][0], c);
               }
@@ -1077,7 +1082,6 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 2 : 1) void k_attend_grad_kv(co
       arrived();
     }
   }
-  const bool some = span.some();
   const uint64_t rows_again = __builtin_amdgcn_ballot_w64(some && !(finite<D>(dk) && finite<D>(dv)));
   const uint32_t redo = (uint32_t)rows_again | (uint32_t)(rows_again >> 32);
   if (!some) {
