@@ -143,8 +143,9 @@ int lmt_cross_entropy(const void* logits /*DEVICE*/, int dtype, uint64_t rows, u
  *   l[i][j] = sum over m of x[i][m] table[j][m];  lse, loss as above;  g[i][j] = w (exp(l[i][j] - lse[i]) - [j == t])
  *   grad_x = g table;  grad_table = (old grad_table, with LMT_ACCUMULATE) + g^T x
  * x: [rows][x_ld], table: [classes][table_ld], both of `dtype`, LMT_F16 or LMT_BF16; rows, classes and width are up to LMT_MAX_WIDTH.  Logits, losses and
- * sums are in fp32; elements of g are rounded to `dtype` (fp16: scaled by powers of two, so that none gets lost below its range) before
- * they are multiplied.  loss, lse (DEVICE [rows], fp32), grad_x (of `dtype`, [rows][grad_x_ld]) and grad_table (of grad_table_dtype,
+ * sums are in fp32; elements of g are rounded to `dtype` before they are multiplied (fp16: scaled by powers of two, for grad_x in front of the row's weight and for
+ * grad_table with it, and never off by more than 2^-39 of the row's weight in the one and 2^-38 of the largest in the other beside a rounding); with up to 256 rows what that
+ * leaves is multiplied too.  loss, lse (DEVICE [rows], fp32), grad_x (of `dtype`, [rows][grad_x_ld]) and grad_table (of grad_table_dtype,
  * `dtype` or LMT_F32, [classes][grad_table_ld]) may each be NULL.  Ignored rows have no loss, a grad_x of zeros and no part in grad_table, whatever they
  * hold; their lse is that of any row.
  * Infinities and NaN in a row of x or in its weight are in that row's results and in grad_table; those in a row of the table are in everything.

@@ -97,7 +97,8 @@ struct Product {
   const RowOf* rows;
   float2* sums;      // kStats: [tile of n][m]: maximum and sum of exp(x - maximum)
   float* hit;        // kStats: logit of the row's target
-  void *gw, *left, *g;  // kGrad: [rows in whole blocks][g_ld], columns up to `cols`: times the row's weight; what rounding that leaves, or as it is; or nullptr
+  // kGrad: [rows in whole blocks][g_ld], columns up to `cols`: g times its row's weight, and as it is, each with what rounding it leaves; or nullptr
+  void *gw, *gw_left, *g, *g_left;
   uint64_t g_ld;
   uint32_t first_class, cols, classes;
   const uint32_t* largest;  // kGrad: bits of the largest weight
@@ -110,8 +111,8 @@ enum Mode { kStats, kGrad, kSum };
 
 // bf16 has fp32's range: g has its row's weight in it, for both gradients.  In fp16 small weights would lose bits, so that there are two: without weights, times
 // 2^14 (it is at most 1), for grad_x, whose rows get theirs at the end, and with them, times a power of two that brings the largest to 2^14, for grad_table.
-// With few rows the rounding of g's few large elements is not averaged away, and the products are small: what it leaves is kept and multiplied too, in
-// which fp16 has bits enough.
+// With few rows the products are small, and what rounding g leaves is kept and multiplied too: of both in fp16, where there are weights (76 rows, 2 003 classes,
+// 257 columns 53 -> 56 us for the second pair).
 template <typename T>
 constexpr bool kNarrow = false;
 template <>
@@ -329,53 +330,59 @@ __global__ __launch_bounds__(S::threads, 2) void k_linear(const Product p) {
   if constexpr (MODE == kGrad) {
     // 64 rows of 64 classes at a time through the wavefront's part of LDS, in 16 bits, so that they leave by whole lines; 16-byte pieces of a row change
     // places by its number
-    uint8_t *weighted = stage + wave * 16384u, *other = weighted + 8192u;
+    uint8_t *places[2] = {stage + wave * 16384u, stage + wave * 16384u + 8192u};
     const float columns = column_scale<T>(load1(p.largest));
     const auto turn = [](uint32_t r) { return r >> 1 & 7u; };
     const auto left = [](uint32_t w, float a, float b) { return pack2(T{}, a - to_f32(__builtin_bit_cast(T, (uint16_t)w)), b - to_f32(__builtin_bit_cast(T, (uint16_t)(w >> 16)))); };
     const uint32_t c0 = n0 + wn * 64u, half = lane >> 5;
     const bool all_classes = p.first_class + c0 + 64u <= p.classes;
+    // bf16: g times its weight, and what that leaves.  fp16: both, or with few rows one after the other, each with what it leaves.
+    const bool few = p.gw_left || p.g_left;
+#pragma unroll 1
+    for (int pass = 0; pass < (kNarrow<T> && few ? 2 : 1); ++pass) {
+      T* const to[2] = {static_cast<T*>(pass == 0 ? p.gw : p.g), static_cast<T*>(pass != 0 ? p.g_left : few ? p.gw_left : p.g)};
+      if (!to[0] && !to[1]) continue;
 #pragma unroll
-    for (int two = 0; two < S::TM / 2; ++two) {
-      const uint32_t r0 = (wm * S::TM + 2 * two) * 32u;
+      for (int two = 0; two < S::TM / 2; ++two) {
+        const uint32_t r0 = (wm * S::TM + 2 * two) * 32u;
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const uint32_t r = i * 32u + (lane & 31u);
-        const RowOf of = row_of[r0 + r];
-        const float by = of.weight * columns;
-        const uint32_t hit = (uint32_t)of.target - p.first_class - c0 - 4u * half;  // the target among this lane's classes
-        const bool none = of.target < 0;
+        for (int i = 0; i < 2; ++i) {
+          const uint32_t r = i * 32u + (lane & 31u);
+          const RowOf of = row_of[r0 + r];
+          const float by = pass == 0 ? of.weight * columns : kRowScale<T>;
+          const uint32_t hit = (uint32_t)of.target - p.first_class - c0 - 4u * half;  // the target among this lane's classes
+          const bool none = of.target < 0;
 #pragma unroll
-        for (int j = 0; j < S::TN; ++j)
+          for (int j = 0; j < S::TN; ++j)
 #pragma unroll
-          for (uint32_t g = 0; g < 4; ++g) {
-            float f[4];
+            for (uint32_t g = 0; g < 4; ++g) {
+              float f[4];
 #pragma unroll
-            for (uint32_t e = 0; e < 4; ++e) {
-              const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(acc[2 * two + i][j][4 * g + e] - of.top, kLog2e, -of.log_sum));
-              f[e] = hit == 32u * j + 8u * g + e ? w - 1.f : w;
-              if (!all_classes) f[e] = p.first_class + c0 + 4u * half + 32u * j + 8u * g + e < p.classes ? f[e] : 0.f;
+              for (uint32_t e = 0; e < 4; ++e) {
+                const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(acc[2 * two + i][j][4 * g + e] - of.top, kLog2e, -of.log_sum));
+                f[e] = hit == 32u * j + 8u * g + e ? w - 1.f : w;
+                if (!all_classes) f[e] = p.first_class + c0 + 4u * half + 32u * j + 8u * g + e < p.classes ? f[e] : 0.f;
+              }
+              const uint32_t at = r * 128u + ((j * 4u + g) ^ turn(r)) * 16u + half * 8u;
+              const u32x2 v = none ? u32x2{0, 0} : u32x2{pack2(T{}, f[0] * by, f[1] * by), pack2(T{}, f[2] * by, f[3] * by)};
+              *reinterpret_cast<u32x2*>(places[0] + at) = v;
+              if (few) *reinterpret_cast<u32x2*>(places[1] + at) = none ? u32x2{0, 0} : u32x2{left(v.x, f[0] * by, f[1] * by), left(v.y, f[2] * by, f[3] * by)};
+              else if (p.g) *reinterpret_cast<u32x2*>(places[1] + at) = none ? u32x2{0, 0} : u32x2{pack2(T{}, f[0] * kRowScale<T>, f[1] * kRowScale<T>), pack2(T{}, f[2] * kRowScale<T>, f[3] * kRowScale<T>)};
             }
-            const uint32_t at = r * 128u + ((j * 4u + g) ^ turn(r)) * 16u + half * 8u;
-            const u32x2 v = none ? u32x2{0, 0} : u32x2{pack2(T{}, f[0] * by, f[1] * by), pack2(T{}, f[2] * by, f[3] * by)};
-            *reinterpret_cast<u32x2*>(weighted + at) = v;
-            if (p.left) *reinterpret_cast<u32x2*>(other + at) = none ? u32x2{0, 0} : u32x2{left(v.x, f[0] * by, f[1] * by), left(v.y, f[2] * by, f[3] * by)};
-            else if (p.g) *reinterpret_cast<u32x2*>(other + at) = none ? u32x2{0, 0} : u32x2{pack2(T{}, f[0] * kRowScale<T>, f[1] * kRowScale<T>), pack2(T{}, f[2] * kRowScale<T>, f[3] * kRowScale<T>)};
-          }
-      }
-      __builtin_amdgcn_wave_barrier();
-#pragma unroll
-      for (int which = 0; which < 2; ++which) {
-        T* to = static_cast<T*>(which == 0 ? p.gw : p.left ? p.left : p.g);
-        if (!to) continue;
-#pragma unroll
-        for (uint32_t it = 0; it < 8; ++it) {
-          const uint32_t r = it * 8u + lane / 8u, piece = lane & 7u, i = m0 + r0 + r, j = c0 + piece * 8u;
-          const u32x4 v = *reinterpret_cast<const u32x4*>((which == 0 ? weighted : other) + r * 128u + (piece ^ turn(r)) * 16u);
-          if (i < round_up(p.m, 64) && j < p.cols) *(LMT_GLOBAL u32x4*)(to + (uint64_t)i * p.g_ld + j) = v;
         }
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int which = 0; which < 2; ++which) {
+          if (!to[which]) continue;
+#pragma unroll
+          for (uint32_t it = 0; it < 8; ++it) {
+            const uint32_t r = it * 8u + lane / 8u, piece = lane & 7u, i = m0 + r0 + r, j = c0 + piece * 8u;
+            const u32x4 v = *reinterpret_cast<const u32x4*>(places[which] + r * 128u + (piece ^ turn(r)) * 16u);
+            if (i < round_up(p.m, 64) && j < p.cols) *(LMT_GLOBAL u32x4*)(to[which] + (uint64_t)i * p.g_ld + j) = v;
+          }
+        }
+        __builtin_amdgcn_wave_barrier();
       }
-      __builtin_amdgcn_wave_barrier();
     }
     return;
   }
@@ -505,12 +512,14 @@ Choice choose(uint64_t m, uint64_t n, uint64_t blocks, bool split) {
 // Where things lie in the workspace, in bytes.
 struct Plan {
   uint64_t piece, pieces;             // classes of a piece, a multiple of 256
-  uint64_t parts;                     // of g: 2 with what rounding leaves
+  uint64_t parts, g_bytes;            // of g: 2 with what rounding leaves, one behind the other; each has so many bytes
   uint64_t x_row;                     // elements of padded rows of x and the table
   Choice stats, grad_x, grad_t;
   uint64_t rows, sums, hit, largest, x, table, counted, g, gw, part_x, part_t, end;
 };
-constexpr uint64_t kFewRows = 256;  // up to which what rounding g leaves is multiplied too
+// Up to which what rounding g leaves is multiplied too.  A rule of cost alone: the products are twice as long.  That rounding is 1.7e-3 of a bf16 gradient's 2-norm at any
+// number of rows (nearly all of it that of a weight times a target's element; the gradient's own rounding is as much again).
+constexpr uint64_t kFewRows = 256;
 constexpr uint64_t kPiece = 1ull << 27;  // elements of g at a time: 256 MB
 Plan plan_of(uint64_t n, uint64_t classes, uint64_t width, bool gradients, bool narrow) {
   Plan w = {};
@@ -531,7 +540,8 @@ Plan plan_of(uint64_t n, uint64_t classes, uint64_t width, bool gradients, bool 
   w.x = take(n * w.x_row * 2), w.table = take(classes * w.x_row * 2);
   if (gradients) {
     w.counted = take(n * w.x_row * 2);
-    w.gw = take(round_up(n, 64) * w.piece * 2), w.g = w.parts > 1 || narrow ? take(round_up(n, 64) * w.piece * 2) : 0;
+    w.g_bytes = round_up(n, 64) * w.piece * 2;
+    w.gw = take(w.parts * w.g_bytes), w.g = narrow ? take(w.parts * w.g_bytes) : 0;
     if (w.pieces * w.grad_x.t.splits > 1) w.part_x = take(w.pieces * w.grad_x.t.splits * n * width * 4);
     if (w.grad_t.t.splits > 1) w.part_t = take(w.grad_t.t.splits * w.piece * width * 4);
   }
@@ -576,15 +586,15 @@ hipError_t launch_typed(const LinearLoss& q, hipStream_t s) {
     const uint32_t first = (uint32_t)(piece * w.piece), n = (uint32_t)std::min<uint64_t>(w.piece, q.classes - first);
     Product g = p;
     g.b = p.b + (uint64_t)first * p.b_row, g.n = n, g.first_class = first, g.cols = (uint32_t)round_up(n, 64), g.g_ld = w.piece;
-    const uint64_t part = w.g - w.gw;  // bytes
     const Choice c = choose(q.rows, n, p.blocks, false);
-    const bool unweighted = kNarrow<T> && w.parts == 1;  // grad_x from g without weights
-    g.t = c.t, g.gw = unweighted && !q.grad_table ? nullptr : at(w.gw), g.left = w.parts > 1 ? at(w.g) : nullptr, g.g = unweighted && q.grad_x ? at(w.g) : nullptr;
+    const bool unweighted = kNarrow<T> && (q.weights || w.parts == 1);  // grad_x from g without weights
+    const auto made = [&](bool wanted, uint64_t place, void** whole, void** left) { *whole = wanted ? at(place) : nullptr, *left = wanted && w.parts > 1 ? at(place + w.g_bytes) : nullptr; };
+    g.t = c.t, made(q.grad_table || !unweighted, w.gw, &g.gw, &g.gw_left), made(unweighted && q.grad_x, w.g, &g.g, &g.g_left);
     launch<T, kGrad, T, false, false>(g, c, s);
     if (q.grad_x) {  // g by the table's rows
       Product d = {};
       d.a = at(unweighted ? w.g : w.gw), d.a_row = (uint32_t)(2 * w.piece), d.b = g.b, d.b_row = p.b_row;
-      d.m = q.rows, d.n = q.width, d.k = n, d.blocks = (uint32_t)w.parts * g.cols / 64, d.wrap = g.cols / 64, d.a_more = part, d.t = w.grad_x.t, d.rows = rows, d.by_row = unweighted, d.largest = unweighted ? nullptr : largest;
+      d.m = q.rows, d.n = q.width, d.k = n, d.blocks = (uint32_t)w.parts * g.cols / 64, d.wrap = g.cols / 64, d.a_more = w.g_bytes, d.t = w.grad_x.t, d.rows = rows, d.by_row = unweighted, d.largest = unweighted ? nullptr : largest;
       d.c = q.grad_x, d.ldc = q.grad_x_ld;
       const uint32_t parts = (uint32_t)w.pieces * d.t.splits;
       float* sums = reinterpret_cast<float*>(at(w.part_x));
@@ -598,7 +608,7 @@ hipError_t launch_typed(const LinearLoss& q, hipStream_t s) {
         typedef decltype(tc) TC;
         Product d = {};
         d.a = at(w.gw), d.a_row = (uint32_t)(2 * w.piece), d.b = at(w.counted), d.b_row = (uint32_t)(2 * w.x_row);
-        d.m = n, d.n = q.width, d.k = q.rows, d.wrap = (uint32_t)ceil_div(q.rows, 64), d.blocks = (uint32_t)w.parts * d.wrap, d.a_more = part, d.largest = largest, d.accumulate = q.accumulate;
+        d.m = n, d.n = q.width, d.k = q.rows, d.wrap = (uint32_t)ceil_div(q.rows, 64), d.blocks = (uint32_t)w.parts * d.wrap, d.a_more = w.g_bytes, d.largest = largest, d.accumulate = q.accumulate;
         d.t = w.grad_t.t, d.t.down = (uint32_t)ceil_div(n, w.grad_t.large ? Large::rows_m : Medium::rows_m);
         d.c = static_cast<TC*>(q.grad_table) + (uint64_t)first * q.grad_table_ld, d.ldc = q.grad_table_ld;
         if (d.t.splits > 1) d.part = reinterpret_cast<float*>(at(w.part_t));
