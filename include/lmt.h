@@ -12,7 +12,7 @@
  *                       and of weights
  *   lmt_cross_entropy   the loss of every row of logits and its gradient
  *   lmt_linear_cross_entropy  the same from the rows and the table, with the gradients of
- *                       both, the logits never kept as a whole
+ *                       both, the logits not kept
  * and these mix the rows of sequences of unlike lengths:
  *   lmt_rotary          queries and keys turned by their positions; its gradient
  *   lmt_attention       attention within each sequence of a packed or padded batch
@@ -139,7 +139,7 @@ int lmt_cross_entropy(const void* logits /*DEVICE*/, int dtype, uint64_t rows, u
                       const float* weights /*DEVICE or NULL*/, float* loss, float* lse, void* grad, uint64_t grad_ld,
                       int32_t* status, void* stream);
 
-/* lmt_cross_entropy of the logits x table^T, which are made in pieces and never kept as a whole:
+/* lmt_cross_entropy of the logits x table^T, which are not kept:
  *   l[i][j] = sum over m of x[i][m] table[j][m];  lse, loss as above;  g[i][j] = w (exp(l[i][j] - lse[i]) - [j == t])
  *   grad_x = g table;  grad_table = (old grad_table, with LMT_ACCUMULATE) + g^T x
  * x: [rows][x_ld], table: [classes][table_ld], both of `dtype`, LMT_F16 or LMT_BF16; rows, classes and width are up to LMT_MAX_WIDTH.  Logits, losses and
@@ -149,9 +149,14 @@ int lmt_cross_entropy(const void* logits /*DEVICE*/, int dtype, uint64_t rows, u
  * `dtype` or LMT_F32, [classes][grad_table_ld]) may each be NULL.  Ignored rows have no loss, a grad_x of zeros and no part in grad_table, whatever they
  * hold; their lse is that of any row.
  * Infinities and NaN in a row of x or in its weight are in that row's results and in grad_table; those in a row of the table are in everything.
- * workspace: DEVICE, 16-byte aligned, lmt_linear_cross_entropy_workspace bytes (with gradients != 0 if grad_x or grad_table is given),
- * contents of no concern; not shared by calls that overlap in time.  Without rows a grad_table that is not added to is refused. */
+ * What is kept instead of the logits is g, for at most 2^27 logits at a time (256 MB; in fp16 again without weights; with up to 256 rows again for what rounding leaves), beside
+ * fp32 sums of grad_x, a copy of the counted rows of x, and copies of x and the table where their rows do not lie as the kernels read them (width no multiple of 64, or not on 16
+ * bytes).  So the workspace does not grow with rows x classes (but for 8 bytes a row and 128 or 256 classes); below 2^27 logits it is no less than logits in 16 bits.
+ * workspace: DEVICE, 16-byte aligned, contents of no concern; not shared by calls that overlap in time.  lmt_linear_cross_entropy_workspace bytes (with gradients != 0
+ * if grad_x or grad_table is given) are enough for any call of these sizes; lmt_linear_cross_entropy_workspace_of is what one of `dtype` needs whose x and table start on 16 bytes
+ * and have strides that are multiples of 8.  Without rows a grad_table that is not added to is refused. */
 uint64_t lmt_linear_cross_entropy_workspace(uint64_t rows, uint64_t classes, uint64_t width, int gradients);
+uint64_t lmt_linear_cross_entropy_workspace_of(int dtype, uint64_t rows, uint64_t classes, uint64_t width, int gradients);
 int lmt_linear_cross_entropy(const void* x /*DEVICE*/, uint64_t x_ld, const void* table /*DEVICE*/, uint64_t table_ld, int dtype,
                              uint64_t rows, uint64_t classes, uint64_t width, const void* targets /*DEVICE*/, int target_dtype,
                              int64_t ignore, const float* weights /*DEVICE or NULL*/, float* loss, float* lse, void* grad_x,

@@ -172,6 +172,10 @@ uint64_t lmt_linear_cross_entropy_workspace(uint64_t rows, uint64_t classes, uin
   return rows > LMT_MAX_WIDTH || classes > LMT_MAX_WIDTH || width > LMT_MAX_WIDTH ? 0 : lmt::linear_loss_workspace(rows, classes, width, gradients != 0);
 }
 
+uint64_t lmt_linear_cross_entropy_workspace_of(int dtype, uint64_t rows, uint64_t classes, uint64_t width, int gradients) {
+  return (dtype != LMT_F16 && dtype != LMT_BF16) || rows > LMT_MAX_WIDTH || classes > LMT_MAX_WIDTH || width > LMT_MAX_WIDTH ? 0 : lmt::linear_loss_workspace_of(dtype, rows, classes, width, gradients != 0);
+}
+
 int lmt_linear_cross_entropy(const void* x, uint64_t x_ld, const void* table, uint64_t table_ld, int dtype, uint64_t rows, uint64_t classes,
                              uint64_t width, const void* targets, int target_dtype, int64_t ignore, const float* weights, float* loss, float* lse,
                              void* grad_x, uint64_t grad_x_ld, void* grad_table, int grad_table_dtype, uint64_t grad_table_ld, uint32_t flags,
@@ -194,9 +198,9 @@ int lmt_linear_cross_entropy(const void* x, uint64_t x_ld, const void* table, ui
   if (off(x, 2) || off(table, 2) || off(grad_x, 2) || off(grad_table, size_of(grad_table_dtype)) || off(targets, size_of(target_dtype)) || off(weights, 4) || off(loss, 4) ||
       off(lse, 4) || off(status, 4))
     return fail(LMT_ERR_ALIGN, "a pointer is not aligned to its element size");
-  if (const int rc = workspace_error(workspace, workspace_bytes, lmt::linear_loss_workspace(rows, classes, width, grad_x || grad_table))) return rc;
   const lmt::LinearLoss p{x, table, targets, weights, loss, lse, grad_x, grad_table, workspace, x_ld, table_ld, grad_x_ld, grad_table_ld, (uint32_t)rows, (uint32_t)classes,
                           (uint32_t)width, target_dtype == LMT_I64, (flags & LMT_ACCUMULATE) != 0, grad_table && grad_table_dtype == LMT_F32, ignore, status};
+  if (const int rc = workspace_error(workspace, workspace_bytes, lmt::linear_loss_workspace(p, dtype))) return rc;
   return launched("launching the loss", lmt::launch_linear_loss(p, dtype, (hipStream_t)stream));
 }
 

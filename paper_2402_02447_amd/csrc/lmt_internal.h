@@ -118,7 +118,9 @@ struct LinearLoss {
   int64_t ignore;
   int32_t* status;
 };
-uint64_t linear_loss_workspace(uint64_t rows, uint64_t classes, uint64_t width, bool gradients);
+uint64_t linear_loss_workspace(uint64_t rows, uint64_t classes, uint64_t width, bool gradients);                // of any call
+uint64_t linear_loss_workspace_of(int dtype, uint64_t rows, uint64_t classes, uint64_t width, bool gradients);  // of aligned ones
+uint64_t linear_loss_workspace(const LinearLoss& p, int dtype);                                                // of this one
 hipError_t launch_linear_loss(const LinearLoss& p, int dtype, hipStream_t s);
 
 }  // namespace lmt

@@ -3,7 +3,7 @@
 // Logits are made twice.  The first time each tile leaves its rows' maxima and sums of exponentials, which are joined to a maximum and a sum a
 // row; the second time, a piece of the classes at a time, tiles become g = w (softmax - onehot) in 16 bits, which is multiplied by the table (grad_x,
 // summed over the pieces) and, as its columns, by x (grad_table).  Four products where three would do with the logits in memory; what is kept
-// instead is one piece of g, 2 bytes an element.
+// instead is one piece of g, of 2^27 elements at most, and the sums of grad_x, to which the pieces add one after the other.
 #include "lmt_device.h"
 #include "lmt_internal.h"
 #include "lmt_tiles.h"
@@ -105,7 +105,8 @@ struct Product {
   void* c;           // kSum
   uint64_t ldc;
   bool accumulate, by_row;
-  float* part;
+  float* part;      // kSum: [split][m][n], sums that are joined later; `more`: added to those of the pieces in front
+  bool more;
 };
 enum Mode { kStats, kGrad, kSum };
 
@@ -417,7 +418,7 @@ __global__ __launch_bounds__(S::threads, 2) void k_linear(const Product p) {
       const uint32_t i = m0 + r0 + r, j = c0 + col;
       if (i >= p.m) continue;
       if (part) {
-        put<float, N>(part + (uint64_t)i * p.n, j, p.n, f, false);
+        put<float, N>(part + (uint64_t)i * p.n, j, p.n, f, p.more);
       } else {
         const float by = p.by_row ? p.rows[i].weight * (1.f / kRowScale<T>) : columns;
         const bool none = p.by_row && p.rows[i].target < 0;
@@ -520,15 +521,15 @@ struct Plan {
 // Up to which what rounding g leaves is multiplied too.  A rule of cost alone: the products are twice as long.  That rounding is 1.7e-3 of a bf16 gradient's 2-norm at any
 // number of rows (nearly all of it that of a weight times a target's element; the gradient's own rounding is as much again).
 constexpr uint64_t kFewRows = 256;
-constexpr uint64_t kPiece = 1ull << 27;  // elements of g at a time: 256 MB
-Plan plan_of(uint64_t n, uint64_t classes, uint64_t width, bool gradients, bool narrow) {
+constexpr uint64_t kPiece = 1ull << 27;  // elements of g at a time: 256 MB (in half of that 2 432 rows of 30 522 classes and 1 024 columns take 708 us for 654)
+Plan plan_of(uint64_t n, uint64_t classes, uint64_t width, bool gradients, bool narrow, bool x_copy, bool table_copy) {
   Plan w = {};
   w.x_row = round_up(width, 64);
+  w.parts = n <= kFewRows ? 2 : 1;
   w.pieces = std::max<uint64_t>(1, ceil_div(n * classes, kPiece));
   w.piece = std::min(round_up(ceil_div(classes, w.pieces), 256), round_up(classes, 256));
   w.pieces = ceil_div(classes, w.piece);
   w.stats = choose(n, classes, w.x_row / 64, false);
-  w.parts = n <= kFewRows ? 2 : 1;
   w.grad_x = choose(n, width, w.parts * w.piece / 64, true);
   w.grad_t = choose(w.piece, width, w.parts * ceil_div(n, 64), true);
   const auto take = [&](uint64_t bytes) {
@@ -537,12 +538,12 @@ Plan plan_of(uint64_t n, uint64_t classes, uint64_t width, bool gradients, bool 
     return at;
   };
   w.rows = take(n * sizeof(RowOf)), w.sums = take(w.stats.t.across * n * sizeof(float2)), w.hit = take(n * 4), w.largest = take(4);
-  w.x = take(n * w.x_row * 2), w.table = take(classes * w.x_row * 2);
+  w.x = x_copy ? take(n * w.x_row * 2) : 0, w.table = table_copy ? take(classes * w.x_row * 2) : 0;
   if (gradients) {
     w.counted = take(n * w.x_row * 2);
     w.g_bytes = round_up(n, 64) * w.piece * 2;
     w.gw = take(w.parts * w.g_bytes), w.g = narrow ? take(w.parts * w.g_bytes) : 0;
-    if (w.pieces * w.grad_x.t.splits > 1) w.part_x = take(w.pieces * w.grad_x.t.splits * n * width * 4);
+    if (w.pieces > 1 || w.grad_x.t.splits > 1) w.part_x = take(w.grad_x.t.splits * n * width * 4);
     if (w.grad_t.t.splits > 1) w.part_t = take(w.grad_t.t.splits * w.piece * width * 4);
   }
   return w;
@@ -560,16 +561,21 @@ void join(const Product& p, uint32_t parts, hipStream_t s) {
   hipLaunchKernelGGL((k_linear_join<T, TC>), dim3((uint32_t)std::min<uint64_t>(ceil_div((uint64_t)p.m * ceil_div(p.n, 4), 256), 1u << 16)), dim3(256), 0, s, p, parts);
 }
 
+// Whether rows can be read as they lie: on 16 bytes, of whole blocks.
+bool as_it_is(const LinearLoss& q, const void* x, uint64_t ld) { return q.width % 64 == 0 && ld % 8 == 0 && ((uintptr_t)x & 15u) == 0 && ld <= LMT_MAX_WIDTH; }
+Plan plan_of(const LinearLoss& q, bool narrow) {
+  return plan_of(q.rows, q.classes, q.width, q.grad_x || q.grad_table, narrow, !as_it_is(q, q.x, q.x_ld), !as_it_is(q, q.table, q.table_ld));
+}
+
 template <typename T>
 hipError_t launch_typed(const LinearLoss& q, hipStream_t s) {
   const bool gradients = q.grad_x || q.grad_table;
-  const Plan w = plan_of(q.rows, q.classes, q.width, gradients, kNarrow<T>);
+  const Plan w = plan_of(q, kNarrow<T>);
   uint8_t* base = static_cast<uint8_t*>(q.workspace);
   const auto at = [&](uint64_t offset) { return base + offset; };
   RowOf* rows = reinterpret_cast<RowOf*>(at(w.rows));
   uint32_t* largest = gradients ? reinterpret_cast<uint32_t*>(at(w.largest)) : nullptr;
-  const auto as_it_is = [&](const void* x, uint64_t ld) { return q.width % 64 == 0 && ld % 8 == 0 && ((uintptr_t)x & 15u) == 0 && ld <= LMT_MAX_WIDTH; };
-  const bool x_copy = !as_it_is(q.x, q.x_ld), table_copy = !as_it_is(q.table, q.table_ld);
+  const bool x_copy = !as_it_is(q, q.x, q.x_ld), table_copy = !as_it_is(q, q.table, q.table_ld);
   const Copy x{q.x, q.x_ld, q.rows, q.width, false, x_copy ? at(w.x) : nullptr}, table{q.table, q.table_ld, q.classes, q.width, false, table_copy ? at(w.table) : nullptr};
   const Copy counted{q.x, q.x_ld, q.rows, q.width, true, q.grad_table ? at(w.counted) : nullptr};
   const uint64_t most = std::max<uint64_t>({x_copy || q.grad_table ? (uint64_t)q.rows * w.x_row : 0, table_copy ? (uint64_t)q.classes * w.x_row : 0, 8ull * q.rows});
@@ -596,12 +602,9 @@ hipError_t launch_typed(const LinearLoss& q, hipStream_t s) {
       d.a = at(unweighted ? w.g : w.gw), d.a_row = (uint32_t)(2 * w.piece), d.b = g.b, d.b_row = p.b_row;
       d.m = q.rows, d.n = q.width, d.k = n, d.blocks = (uint32_t)w.parts * g.cols / 64, d.wrap = g.cols / 64, d.a_more = w.g_bytes, d.t = w.grad_x.t, d.rows = rows, d.by_row = unweighted, d.largest = unweighted ? nullptr : largest;
       d.c = q.grad_x, d.ldc = q.grad_x_ld;
-      const uint32_t parts = (uint32_t)w.pieces * d.t.splits;
-      float* sums = reinterpret_cast<float*>(at(w.part_x));
-      if (parts > 1) d.part = sums + piece * d.t.splits * (uint64_t)q.rows * q.width;
+      if (w.pieces > 1 || d.t.splits > 1) d.part = reinterpret_cast<float*>(at(w.part_x)), d.more = piece > 0;
       launch<T, kSum, T, false, true>(d, w.grad_x, s);
-      d.part = sums;
-      if (parts > 1 && piece + 1 == w.pieces) join<T, T>(d, parts, s);
+      if (d.part && piece + 1 == w.pieces) join<T, T>(d, d.t.splits, s);
     }
     if (q.grad_table) {  // g's columns by x's
       const auto typed = [&](auto tc) {
@@ -625,8 +628,12 @@ hipError_t launch_typed(const LinearLoss& q, hipStream_t s) {
 }  // namespace
 
 uint64_t linear_loss_workspace(uint64_t rows, uint64_t classes, uint64_t width, bool gradients) {
-  return rows && classes ? plan_of(rows, classes, width, gradients, true).end : 0;
+  return rows && classes ? std::max(plan_of(rows, classes, width, gradients, false, true, true).end, plan_of(rows, classes, width, gradients, true, true, true).end) : 0;
 }
+uint64_t linear_loss_workspace_of(int dtype, uint64_t rows, uint64_t classes, uint64_t width, bool gradients) {
+  return rows && classes ? plan_of(rows, classes, width, gradients, dtype == LMT_F16, width % 64 != 0, width % 64 != 0).end : 0;
+}
+uint64_t linear_loss_workspace(const LinearLoss& p, int dtype) { return plan_of(p, dtype == LMT_F16).end; }
 hipError_t launch_linear_loss(const LinearLoss& p, int dtype, hipStream_t s) {
   return dtype == LMT_F16 ? launch_typed<_Float16>(p, s) : launch_typed<bf16_t>(p, s);
 }

@@ -82,7 +82,7 @@ class TiedLm:
             need += [lmt.matmul_workspace(*mnk) for mnk in ((tokens, vocab, width), (tokens, width, vocab), (vocab, width, tokens))]
         else:
             self.table16, self.every_token = bf16(vocab, width), torch.arange(vocab, device="cuda")
-            need += [lmt.linear_cross_entropy_workspace(tokens, vocab, width)]
+            need += [lmt.linear_cross_entropy_workspace(tokens, vocab, width, dtype=torch.bfloat16)]
         self.heads, self.causal = heads, causal
         if heads:
             if width % (2 * heads):

@@ -23,7 +23,7 @@ _BYTES = 7                          # uint8: scales and workspaces
 
 EXPORTS = ["lmt_embed", "lmt_embed_grad", "lmt_embed_grad_workspace", "lmt_fp8_row_bytes", "lmt_scale_row_bytes",
            "lmt_quantize", "lmt_matmul_workspace", "lmt_matmul", "lmt_cross_entropy", "lmt_last_error",
-           "lmt_linear_cross_entropy_workspace", "lmt_linear_cross_entropy", "lmt_rotary", "lmt_attention", "lmt_attention_grad_workspace", "lmt_attention_grad"]
+           "lmt_linear_cross_entropy_workspace", "lmt_linear_cross_entropy_workspace_of", "lmt_linear_cross_entropy", "lmt_rotary", "lmt_attention", "lmt_attention_grad_workspace", "lmt_attention_grad"]
 
 
 class Heads(C.Structure):
@@ -64,6 +64,7 @@ def _lib():
         L.lmt_attention.argtypes = [attend, heads, heads, heads, heads, vp, vp]
         L.lmt_attention_grad.argtypes = [attend] + 5 * [heads] + [vp] + 3 * [heads] + [vp, u64, vp]
         L.lmt_linear_cross_entropy_workspace.argtypes, L.lmt_linear_cross_entropy_workspace.restype = [u64, u64, u64, i32], u64
+        L.lmt_linear_cross_entropy_workspace_of.argtypes, L.lmt_linear_cross_entropy_workspace_of.restype = [i32, u64, u64, u64, i32], u64
         L.lmt_attention_grad_workspace.argtypes, L.lmt_attention_grad_workspace.restype = [u64, u64, u64, u64], u64
         for name in ("lmt_embed_grad_workspace", "lmt_matmul_workspace"):
             getattr(L, name).argtypes, getattr(L, name).restype = [u64, u64, u64], u64
@@ -152,14 +153,20 @@ def cross_entropy(logits, targets, loss=None, lse=None, grad=None, weights=None,
     _check(_calls.lmt_cross_entropy(_table, logits, targets, loss, lse, grad, weights, ignore, status, stream))
 
 
-def linear_cross_entropy_workspace(rows: int, classes: int, width: int, gradients: bool = True) -> int:
-    """Bytes of the uint8 tensor that linear_cross_entropy works in, with or without gradients."""
-    return int(_lib().lmt_linear_cross_entropy_workspace(rows, classes, width, gradients))
+def linear_cross_entropy_workspace(rows: int, classes: int, width: int, gradients: bool = True, dtype=None) -> int:
+    """Bytes of the uint8 tensor that linear_cross_entropy works in, with or without gradients: enough for any call of these sizes, or with dtype
+    (torch.float16 or torch.bfloat16) what a call of this type needs whose x and table start on 16 bytes, with row strides of whole 16 bytes, as new tensors do."""
+    if dtype is None:
+        return int(_lib().lmt_linear_cross_entropy_workspace(rows, classes, width, gradients))
+    import torch
+    if dtype not in (torch.float16, torch.bfloat16):
+        raise ValueError("dtype: fp16 or bf16 is wanted")
+    return int(_lib().lmt_linear_cross_entropy_workspace_of(LMT_F16 if dtype == torch.float16 else LMT_BF16, rows, classes, width, gradients))
 
 
 def linear_cross_entropy(x, table, targets, workspace, loss=None, lse=None, grad_x=None, grad_table=None, weights=None, ignore: int = -100,
                          accumulate: bool = False, status=None, stream=None) -> None:
-    """cross_entropy of the logits x table^T, which are never kept as a whole, with the gradients of x and of the table (added to
+    """cross_entropy of the logits x table^T, which are not kept, with the gradients of x and of the table (added to
     grad_table with accumulate).  x: [rows, width], table: [classes, width], fp16 or bf16; grad_x: as x; grad_table: as the table, or fp32;
     each result may be None."""
     if _table is None:

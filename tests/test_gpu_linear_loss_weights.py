@@ -46,3 +46,23 @@ def test_weights_of_any_size_and_none(kind, rows):
     want, bound = A.linear_loss(x, table, t, w, IGNORE, kind)["loss"]
     within(loss.cpu().numpy(), want, bound + 2.0 ** -150)
     check(x, table, t, None, kind, f32=True, accumulate=True)
+
+
+@pytest.mark.parametrize("kind", ["f16", "bf16"])
+@pytest.mark.parametrize("rows,classes,width", [(100, 700, 64), (300, 3000, 192), (300, 900, 72), (4000, 50_000, 64)])
+def test_a_workspace_of_exactly_the_calls_size(kind, rows, classes, width):
+    """Nothing behind it is touched, and the bits are those of one that is enough for any call."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(rows)
+    x, table = torch.randn(rows, width, generator=g, device="cuda").to(DT[kind]), (torch.randn(classes, width, generator=g, device="cuda") / 4).to(DT[kind])
+    t, w = torch.randint(classes, (rows,), generator=g, device="cuda"), torch.rand(rows, generator=g, device="cuda")
+    results = []
+    for n in (lmt.linear_cross_entropy_workspace(rows, classes, width, dtype=DT[kind]), lmt.linear_cross_entropy_workspace(rows, classes, width)):
+        buffer = torch.full((n + 4096,), 0x5A, dtype=torch.uint8, device="cuda")
+        out = [torch.zeros(rows, device="cuda"), torch.zeros(rows, device="cuda"), torch.zeros_like(x), torch.zeros_like(table)]
+        torch.cuda.synchronize()
+        lmt.linear_cross_entropy(x, table, t, buffer[:n], *out, weights=w)
+        torch.cuda.synchronize()
+        assert bool((buffer[n:] == 0x5A).all())
+        results.append(out)
+    assert all(torch.equal(a, b) for a, b in zip(*results))
