@@ -152,3 +152,36 @@ def test_rows_of_unlike_sizes(kind, T, heads, kv_heads, size, causal):
     for x, (w, b) in zip(got, in_64_bits(go, q, k, v, out, lse, causal, scale, kind)):
         over = (x.double() - w).abs() - b
         assert bool(torch.isfinite(x).all()) and float(over.max()) <= 0, (int((over > 0).sum()), float(over.max()))
+
+
+@pytest.mark.parametrize("kind", ["f16", "bf16"])
+@pytest.mark.parametrize("T,heads,kv_heads,size,causal", [(3000, 8, 1, 128, True), (4100, 2, 2, 128, False), (2500, 4, 2, 64, True), (1777, 3, 3, 96, False)])
+def test_results_of_long_sequences(kind, T, heads, kv_heads, size, causal):
+    """Scores spread over some 2^20, so that the running largest of a row moves many times.  Bounds as attention_reference.py counts them."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(T)
+    q = torch.randn(T, heads, size, generator=g, device="cuda").to(DT[kind])
+    k, v = (torch.randn(T, kv_heads, size, generator=g, device="cuda").to(DT[kind]) for _ in range(2))
+    scale, unit = 4.0 / math.sqrt(size), UNIT[kind]
+    out, lse = torch.full_like(q, 7.0), torch.full((heads, T), 7.0, device="cuda")
+    torch.cuda.synchronize()
+    lmt.attention(q, k, v, out, lse, table([0, T]), scale=scale, causal=causal)
+    torch.cuda.synchronize()
+    i = torch.arange(T, device="cuda")
+    hidden = (i[None, :] > i[:, None]) & causal
+    for h in range(heads):
+        Q, K, V = (x.double() for x in (q[:, h], k[:, h * kv_heads // heads], v[:, h * kv_heads // heads]))
+        s, off = Q @ K.t().contiguous() * scale, Q.abs() @ K.abs().t().contiguous() * scale * (U32 * (size + 4))
+        off = (off + 3 * U32 * s.abs()).masked_fill(hidden, 0.0)
+        s = s.masked_fill(hidden, -math.inf)
+        top = s.amax(1, keepdim=True)
+        p = torch.exp(s - top)
+        total = p.sum(1, keepdim=True)
+        p /= total
+        worst = off.amax(1, keepdim=True) + U32 * (i[:, None] * causal + T * (not causal) + 9 + 4 * top.abs())
+        want, size_of = p @ V, p @ V.abs()
+        low = (~hidden).double() @ V.abs()
+        bound = 1.01 * (size_of * (unit + 2 * worst) + 2.0 ** -31 * low * (kind == "f16") + unit * want.abs() + TINY[kind] + 2.0 ** -126 * (low + T))
+        want_lse = (top + torch.log(total)).squeeze(1)
+        assert float(((out[:, h].double() - want).abs() - bound).max()) <= 0
+        assert float(((lse[h].double() - want_lse).abs() - 1.01 * (worst.squeeze(1) + 4 * U32 * want_lse.abs()) - 2 * U32).max()) <= 0
