@@ -200,7 +200,8 @@ typedef struct lmt_attend {
  *   out[i] = sum over j of exp(s[j] - lse) v[j];  lse[h][i] = log(sum over j of exp(s[j]))
  * q, out: rows x heads; k, v: rows x kv_heads; lse: DEVICE [heads][rows], fp32, or NULL.  Rows of no sequence, and rows all of whose
  * scores are -Inf, get zeros and an lse of -Inf.  What a row does not see has no part in its results, whatever it holds (rows that
- * infinities or NaN reach are computed once more, slowly).  Scores, weights' sums and outputs' sums are in fp32, the weights that multiply v
+ * infinities or NaN reach are computed once more, one after the other: 0.2 to 0.4 ns for each row and each that it sees, a head, twice that for the gradients; one NaN that all of a sequence of
+ * 8 192 rows and 16 heads sees, 0.2 s and 0.4 s instead of a millisecond).  Scores, weights' sums and outputs' sums are in fp32, the weights that multiply v
  * are rounded to `dtype`. */
 int lmt_attention(const lmt_attend* a, const lmt_heads* q, const lmt_heads* k, const lmt_heads* v, const lmt_heads* out,
                   float* lse, void* stream);

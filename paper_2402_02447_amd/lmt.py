@@ -177,7 +177,7 @@ def linear_cross_entropy(x, table, targets, workspace, loss=None, lse=None, grad
 def rotary_frequencies(pairs: int, base: float = 10000.0, trained: int = 0, stretch: float = 1.0, kept: float = 32.0, slowed: float = 1.0):
     """Frequencies (fp32, on the host) of `pairs` pairs of a head, base^(-f / pairs), for contexts `stretch` times as long as the `trained` positions.
     A pair that makes `kept` turns or more within `trained` positions keeps its frequency, one that makes `slowed` or fewer is slowed by
-    `stretch`, those between by as much as lies between; with trained = 0 all are slowed."""
+    `stretch`, those between by as much as lies between (the published interpolation of rotary frequencies by parts); with trained = 0 all are slowed."""
     import math
 
     import torch
